@@ -44,7 +44,11 @@ extern "C" {
 
 typedef struct dsmoe_ctx dsmoe_ctx; /* opaque; host memory owned by the library */
 
-typedef enum { DSMOE_F32 = 0, DSMOE_BF16 = 1 } dsmoe_dtype;
+typedef enum {
+  DSMOE_F32 = 0,
+  DSMOE_BF16 = 1,
+  DSMOE_F16 = 2 /* the operators beside the layer only */
+} dsmoe_dtype;
 
 typedef enum {
   DSMOE_OK = 0,
@@ -100,7 +104,7 @@ size_t dsmoe_packed_bytes(const dsmoe_ctx* ctx);
 size_t dsmoe_workspace_bytes(const dsmoe_ctx* ctx);
 
 const char* dsmoe_strerror(int status);
-/* hipError_t value of the last failed HIP call on this context (0 if none). */
+/* hipError_t value of the last failed HIP call on this context (0 if none); NULL: of this thread's last call that has no context. */
 int dsmoe_last_hip_error(const dsmoe_ctx* ctx);
 /* 1 if this context runs the bf16 MFMA kernels, 0 if it runs the full-precision kernels, which keep the
  * intermediate activation and the partial outputs in fp32 (fp32 layers, bf16 layers whose D, F/P or shared width is not a multiple of 32, or contexts whose
@@ -317,6 +321,72 @@ int dsmoe_plan_layout(const dsmoe_ctx* ctx, int64_t* out);
 #define DSMOE_NUM_KERNELS 7
 int dsmoe_profile_begin(dsmoe_ctx* ctx, int level, int max_calls);
 int dsmoe_profile_end(dsmoe_ctx* ctx, float* ms, int* calls);
+
+/*
+ * Operators beside the layer: what trains or serves experts whose weights lie as they were made, [groups][k][n], not in
+ * moe_partition_weights' layout.  They need no context.  Tensors are device memory, row-major, a row's values next to each other; strides
+ * are in values and may be any (inputs: from 0 on; outputs: at least a row, rows must not overlap).  Rows may start on any value: rows on 16
+ * bytes are faster.  dtype is that of every tensor that is not named otherwise; sums are in 32 bits whatever it is, and each output is
+ * rounded to it once.  Outputs must not overlap inputs.  All of them only enqueue kernels: no allocation, no host synchronisation, no
+ * atomics on results (the same inputs give the same bits), and they may be captured into a graph.  After DSMOE_EHIP
+ * dsmoe_last_hip_error(NULL) gives the calling thread's last error.
+ *
+ * Products over groups of rows (the experts' products, Eq. 4, with nothing fused to them).  offsets device int32 [groups + 1]: group g
+ * owns the rows offsets[g] .. offsets[g + 1] - 1 of x, y and dy; groups may be empty.  Rows before the first offset and from the last one
+ * on belong to no group.  A table that is out of order or out of range is an error of the caller's that the device cannot report: offsets
+ * count as clamped to [0, rows] and to the largest before them, and nothing outside the tensors is read or written.
+ *   moe_grouped_matmul      transposed 0: y[r] = x[r] W[g]      x [rows][k], y [rows][n]
+ *                           transposed 1: y[r] = x[r] W[g]^T    x [rows][n], y [rows][k]   (the gradient of x, with x for that of y)
+ *                           rows of no group: zeros
+ *   moe_grouped_matmul_dw   dw[g] = sum over the group's rows of x[r]^T dy[r]    x [rows][k], dy [rows][n], dw [groups][k][n];
+ *                           a group without rows: zeros
+ * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
+ */
+int moe_grouped_matmul(const void* x, int64_t x_stride, const void* w, int64_t w_group_stride, int64_t w_row_stride,
+                       const int32_t* offsets, int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t transposed, int32_t dtype,
+                       void* y, int64_t y_stride, void* stream);
+int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offsets, int32_t rows,
+                          int32_t groups, int32_t k, int32_t n, int32_t dtype, void* dw, int64_t dw_group_stride, int64_t dw_row_stride,
+                          void* stream);
+
+/*
+ * Products in 8-bit integers, with a scale for each token and each output channel: s = max|x[r]| / 127 in fp32, q = x[r] / s rounded to
+ * the nearest integer (ties to even) and clamped to +-127, y[r][c] = s * w_scale[g][c] * sum over k of q w[g][c], the sum exact in int32.
+ *   w device int8 [groups][n][k], a row for each output channel; w_scale device float [groups][n] (a group's next to each other);
+ *   offsets as above, or NULL for one group of all rows (groups = 1).  k at most 2^17.
+ *   A row of zeros gives zeros, a row with a NaN or an infinity NaN in all its outputs, rows of no group zeros.
+ *   workspace device, dsmoe_int8_workspace_bytes(rows, k) bytes, 256-byte aligned: the rows in 8 bits and their scales.
+ */
+size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t k);
+int moe_int8_matmul(const void* x, int64_t x_stride, const int8_t* w, int64_t w_group_stride, int64_t w_row_stride, const float* w_scale,
+                    int64_t w_scale_group_stride, const int32_t* offsets, int32_t rows, int32_t groups, int32_t k, int32_t n,
+                    int32_t dtype, void* y, int64_t y_stride, void* workspace, void* stream);
+
+/*
+ * The norms around a block (the layer, or any other branch of a residual stream), fused with the block's gate and residual scale:
+ *   y = x + scale * gate * (branch * rsqrt(mean(branch^2) + eps) * (branch_weight + weight_offset))
+ *   h = y * rsqrt(mean(y^2) + eps) * (weight + weight_offset)        (y unrounded)
+ * x, branch, y, h [tokens][d], branch_weight, weight [d].  weight_offset is 1 for models that hold their weights less one.
+ *   gate_kind 0: none (gate = NULL)   1: a value for each token   2: for each channel, [d]   3: for each value, [tokens][d]
+ *   stats device float [2][tokens], or NULL: the rows' reciprocal roots, which the backward pass takes.
+ *   y and h are written without gaps between rows, and so are the gradients.
+ * Backward: from dy and dh, the gradients of y and h, those of x, branch, gate (none if gate_kind is 0; the sums over what the gate is
+ * broadcast over), branch_weight and weight.  workspace device, dsmoe_block_norm_workspace_bytes(args) bytes, 256-byte aligned.
+ * tokens 0 .. 2^23, d 1 .. 2^24.
+ */
+typedef struct {
+  int32_t tokens, d, dtype, gate_kind;
+  float scale, weight_offset, eps;
+  int32_t pad; /* 0 */
+  int64_t x_stride, branch_stride, gate_stride; /* gate_kind 1: from token to token; 3: from row to row */
+  int64_t dy_stride, dh_stride;                 /* backward only */
+} dsmoe_block_norm_args;
+int moe_block_norm(const dsmoe_block_norm_args* args, const void* x, const void* branch, const void* branch_weight, const void* gate,
+                   const void* weight, void* y, void* h, float* stats, void* stream);
+size_t dsmoe_block_norm_workspace_bytes(const dsmoe_block_norm_args* args);
+int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, const void* dh, const void* x, const void* branch,
+                            const void* branch_weight, const void* gate, const void* weight, const float* stats, void* dx, void* dbranch,
+                            void* dbranch_weight, void* dgate, void* dweight, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

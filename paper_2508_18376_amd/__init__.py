@@ -37,7 +37,14 @@ _BINDING_NAMES = (
     "dsmoe_router_packed_bytes",
     "lib_path",
 )
-__all__ = list(_BINDING_NAMES)
+_OPERATOR_NAMES = (
+    "moe_grouped_matmul",
+    "moe_grouped_matmul_dw",
+    "moe_int8_matmul",
+    "moe_block_norm",
+    "moe_block_norm_backward",
+)
+__all__ = list(_BINDING_NAMES + _OPERATOR_NAMES)
 
 
 def __getattr__(name):
@@ -46,4 +53,9 @@ def __getattr__(name):
     if name in _BINDING_NAMES or name == "binding":
         mod = importlib.import_module(".binding", __name__)
         return mod if name == "binding" else getattr(mod, name)
+    if name in _OPERATOR_NAMES or name == "operators":
+        mod = importlib.import_module(".operators", __name__)
+        if name != "operators":
+            globals()[name] = getattr(mod, name)  # a call on a few tokens is short enough to notice the lookup
+        return mod if name == "operators" else globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

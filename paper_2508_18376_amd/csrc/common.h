@@ -151,6 +151,8 @@ struct PerDeviceOnce {
   }
 };
 
+int& no_ctx_hip_error();  // the calling thread's last HIP error in a call without a context
+
 constexpr int kNumKernels = 7;  // router, route, plan, scatter, gemm1, gemm2, combine (the first and the fourth where there are any)
 
 struct Profile {

@@ -1,0 +1,151 @@
+// Shared by the products over groups of rows (grouped.hip, int8_matmul.hip): arguments, and the groups' rows worked out on the device.
+#pragma once
+#include "common.h"
+
+namespace dsmoe {
+
+enum ElemType : int32_t { kElemF32 = DSMOE_F32, kElemBF16 = DSMOE_BF16, kElemF16 = DSMOE_F16, kElemI8 = 100 };
+inline __host__ __device__ int elem_bytes(int t) { return t == kElemF32 ? 4 : t == kElemI8 ? 1 : 2; }
+
+// One launch of products C_g = A_g B_g.  Rows are the caller's rows (tokens); a group owns rows [off[g], off[g+1]).
+//   over rows      A [R][K] rows of the group, B_g [K][N] (or [N][K], each output column's values together), C [R][N]
+//   over weights   A [R][M], B [R][N], both summed over the group's rows, C_g [M][N]
+struct GroupedArgs {
+  const char* a;
+  const char* b;
+  char* c;
+  const int32_t* off;                             // [G + 1] on the device; nullptr: one group of all rows
+  int64_t a_row, b_row, b_group, c_row, c_group;  // strides in bytes
+  int32_t R, G, M, N, K;
+  const float* a_scale;  // 8-bit products: a factor for each row of A, and for each output column of a group
+  const float* b_scale;
+  int64_t bs_group;  // ... in values
+  int32_t out_type;
+};
+
+// Inclusive scans over the 64 lanes (DPP: shifts inside the rows of sixteen, then the last lane of a row to the next ones).
+// Identity 0: sums, and maxima of values that are not negative.
+template <bool MAX>
+__device__ __forceinline__ int wave_scan(int v) {
+#define DSMOE_SCAN_STEP(CTRL, ROWS)                                              \
+  {                                                                              \
+    const int o = __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);     \
+    v = MAX ? max(v, o) : v + o;                                                 \
+  }
+  DSMOE_SCAN_STEP(0x111, 0xf)
+  DSMOE_SCAN_STEP(0x112, 0xf)
+  DSMOE_SCAN_STEP(0x114, 0xf)
+  DSMOE_SCAN_STEP(0x118, 0xf)
+  DSMOE_SCAN_STEP(0x142, 0xa)
+  DSMOE_SCAN_STEP(0x143, 0xc)
+#undef DSMOE_SCAN_STEP
+  return v;
+}
+
+// The row space falls into G + 2 segments: rows before the first group, the groups, rows after the last one.  The first and
+// the last have no weights: their rows of C are zero.  Offsets outside [0, R] count as its ends and an offset below an earlier one as that
+// one, so that whatever the table holds, the segments are disjoint and cover the rows once.
+__device__ __forceinline__ int segment_bound(const int32_t* off, int G, int R, int i) {
+  if (i <= 0) return 0;
+  if (i > G + 1) return R;
+  return min(max(off[i - 1], 0), R);
+}
+
+struct Segment {
+  int row0, rows;
+  int group;  // -1: no weights
+  int base;   // pieces of the segments before it
+  int total;  // pieces of all segments
+};
+
+// begin and end of segment s0 + lane; carry: the largest bound before s0, updated
+__device__ __forceinline__ void lane_segment(const int32_t* off, int G, int R, int s, int& carry, int& begin, int& end) {
+  const int b = segment_bound(off, G, R, s), e = segment_bound(off, G, R, s + 1);
+  begin = max(wave_scan<true>(b), carry);
+  end = max(begin, e);
+  carry = __builtin_amdgcn_readlane(end, 63);
+}
+
+// Pieces of a launch over rows: per_tile for each BM rows of a segment.  pick(total) says which piece this workgroup takes.
+template <class Pick>
+__device__ __forceinline__ bool find_segment(const int32_t* off, int G, int R, int BM, int per_tile, Pick&& pick, int& piece, Segment& s) {
+  if (off == nullptr) {
+    s = Segment{0, R, 0, 0, (R + BM - 1) / BM * per_tile};
+    piece = pick(s.total);
+    return piece < s.total;
+  }
+  const int lane = threadIdx.x & 63, n = G + 2;
+  int begin, end, total = 0, carry = 0, scan = 0;
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    lane_segment(off, G, R, s0 + lane, carry, begin, end);
+    scan = wave_scan<false>((end - begin + BM - 1) / BM) * per_tile;
+    total += __builtin_amdgcn_readlane(scan, 63);
+  }
+  s.total = total;
+  piece = pick(total);
+  if (piece >= total) return false;
+  int base = 0;
+  carry = 0;
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    if (n > 64) {
+      lane_segment(off, G, R, s0 + lane, carry, begin, end);
+      scan = wave_scan<false>((end - begin + BM - 1) / BM) * per_tile;
+    }
+    const uint64_t beyond = __ballot(base + scan > piece);
+    if (beyond) {
+      const int l = __builtin_ctzll(beyond), q = s0 + l;
+      s.row0 = __builtin_amdgcn_readlane(begin, l);
+      s.rows = __builtin_amdgcn_readlane(end, l) - s.row0;
+      s.group = q >= 1 && q <= G ? q - 1 : -1;
+      s.base = base + __builtin_amdgcn_readlane(scan, l) - (s.rows + BM - 1) / BM * per_tile;
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(scan, 63);
+  }
+  return false;
+}
+
+// rows of group g
+__device__ __forceinline__ void group_rows(const int32_t* off, int G, int R, int g, int& row0, int& rows) {
+  int begin = 0, end = R, carry = 0;
+  if (off != nullptr) {
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 <= g + 1; s0 += 64) lane_segment(off, G, R, s0 + lane, carry, begin, end);
+    begin = __builtin_amdgcn_readlane(begin, (g + 1) & 63);
+    end = __builtin_amdgcn_readlane(end, (g + 1) & 63);
+  }
+  row0 = begin;
+  rows = end - begin;
+}
+
+// most row tiles of BM rows that R rows in G groups can give
+inline int64_t row_tiles_bound(int64_t R, int64_t G, bool grouped, int BM) {
+  if (!grouped) return (R + BM - 1) / BM;
+  const int64_t segments = G + 2 < R ? G + 2 : R;
+  return (R - segments) / BM + segments;
+}
+
+// Inside a segment the pieces go in bands of 8 row tiles, column tile by column tile: 32 neighbours (what an XCD gets at a time, see take_piece)
+// share 8 row tiles and 4 column tiles.
+constexpr int kBand = 8;
+__device__ __forceinline__ void band_tile(int id, int row_tiles, int col_tiles, int& rt, int& ct) {
+  const int band = id / (kBand * col_tiles), left = id - band * kBand * col_tiles;
+  const int h = min(kBand, row_tiles - band * kBand);
+  ct = left / h;
+  rt = band * kBand + left - ct * h;
+}
+
+// (R - segments) / BM + segments tiles: a first row in each segment, and a tile more for every BM further rows at most
+hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
+hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s);
+
+__device__ __forceinline__ float elem_to_f32(const char* p, int type) {
+  if (type == kElemF32) return *(const float*)p;
+  if (type == kElemBF16) return bf16_to_f32(*(const uint16_t*)p);
+  return (float)*(const _Float16*)p;
+}
+__device__ __forceinline__ uint16_t f32_to_16(float v, int type) {
+  return type == kElemBF16 ? f32_to_bf16(v) : __builtin_bit_cast(uint16_t, (_Float16)v);
+}
+
+}  // namespace dsmoe

@@ -1,0 +1,127 @@
+"""8-bit products against the same integers and scales worked out on the CPU: the sums are exact, so the outputs are off by three fp32
+roundings and the one to their type."""
+import pytest
+import torch
+
+from operator_util import DTYPES, U32, assert_within, offsets_of, spans
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def reference(x, w, ws, off):
+    x32 = x.float()
+    s = x32.abs().amax(1) / 127
+    q = torch.where(s[:, None] > 0, torch.round(x32 / s[:, None]).clamp(-127, 127), torch.zeros_like(x32)).double()
+    y = torch.zeros(x.shape[0], w.shape[1], dtype=torch.float64)
+    for g, (lo, hi) in enumerate(spans(off.tolist(), x.shape[0]) if off is not None else [(0, x.shape[0])]):
+        y[lo:hi] = (q[lo:hi] @ w[g].double().t()) * ws[g].double() * s[lo:hi, None].double()
+    return y
+
+
+def make(R, G, k, n, dtype, seed, pad=0):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(R, k, generator=gen) * torch.exp(2 * torch.randn(R, 1, generator=gen))
+    w = torch.randint(-127, 128, (G, n, k + pad), generator=gen, dtype=torch.int8)
+    return x.to(dtype), w[:, :, :k], torch.rand(G, n, generator=gen) * 1e-3 + 1e-4
+
+
+# counts, rows before and after, k, n, padding of the weights' rows
+SHAPES = {
+    "dense_one": (None, 0, 1, 4096, 264, 0),
+    "dense_some": (None, 0, 19, 512, 100, 0),
+    "dense_tiles": (None, 0, 300, 256, 520, 0),
+    "dense_odd": (None, 0, 67, 333, 77, 0),
+    "dense_padded": (None, 0, 67, 333, 77, 3),
+    "one_value": ([1], 0, 0, 1, 1, 0),
+    "groups": ([3, 0, 130, 1], 2, 5, 192, 136, 0),
+    "groups_odd": ([3, 0, 130, 1], 2, 5, 95, 51, 1),
+    "decode": ([1, 0, 2, 1, 0, 3, 0, 1], 0, 0, 1408, 256, 0),
+    "long_k": ([2, 6], 0, 0, 17000, 40, 8),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("name", SHAPES)
+def test_products(name, dtype):
+    from paper_2508_18376_amd import moe_int8_matmul
+    counts, before, after, k, n, pad = SHAPES[name]
+    G = 1 if counts is None else len(counts)
+    R = before + after + sum(counts or [])
+    off = None if counts is None else offsets_of(counts, before)
+    x, w, ws = make(R, G, k, n, DTYPES[dtype], 3, pad)
+    print(name, dtype, R, G, k, n, flush=True)
+    wd = torch.empty(G, n, k + pad, dtype=torch.int8, device=DEV)[:, :, :k]
+    wd.copy_(w)
+    y = moe_int8_matmul(x.to(DEV), wd, ws.to(DEV), None if off is None else off.to(DEV))
+    torch.cuda.synchronize()
+    ref = reference(x, w, ws, off)
+    assert y.dtype == x.dtype
+    assert_within(y, ref, 4 * U32 * ref.abs(), "y")
+
+
+def test_ties_signs_and_largest_values():
+    """Halves round to even; the largest magnitude is 127 whatever its sign."""
+    from paper_2508_18376_amd import moe_int8_matmul
+    x = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5, -127.0], [-127.0, 126.5, 125.5, -126.5, -125.5, 0.25, -0.75, 63.5]])
+    w = torch.eye(8, dtype=torch.int8)[None]
+    y = moe_int8_matmul(x.to(DEV), w.to(DEV), torch.ones(1, 8, device=DEV))
+    assert y.cpu().tolist() == [[127, 0, 2, 2, 0, -2, -2, -127], [-127, 126, 126, -126, -126, 0, -1, 64]]
+
+
+def test_largest_sums_are_exact():
+    from paper_2508_18376_amd import moe_int8_matmul
+    k = 1 << 17
+    x = torch.ones(2, k, dtype=torch.float32, device=DEV)
+    w = torch.full((1, 3, k), 127, dtype=torch.int8, device=DEV)
+    w[0, 1] = -127
+    y = moe_int8_matmul(x, w, torch.ones(1, 3, device=DEV)).cpu().double()
+    s = float(torch.tensor(1.0) / 127)
+    want = torch.tensor([127 * 127 * k * s] * 2 + [0.0])[None] * torch.tensor([1.0, -1.0, 1.0])
+    assert ((y[:, :2] - want[:, :2].double()).abs() <= 4 * U32 * want[:, :2].abs()).all() and (y[:, 2] == y[:, 0]).all()
+
+
+@pytest.mark.parametrize("k", [64, 61])
+def test_zero_and_nonfinite_rows(k):
+    from paper_2508_18376_amd import moe_int8_matmul
+    x, w, ws = make(140, 1, k, 40, torch.bfloat16, 5)
+    x[3] = 0
+    x[7, 5], x[8, 0], x[9, 1] = float("nan"), float("inf"), float("-inf")
+    y = moe_int8_matmul(x.to(DEV), w.to(DEV), ws.to(DEV)).cpu()
+    assert (y[3] == 0).all() and torch.isnan(y[7:10]).all()
+    keep = [i for i in range(140) if i not in (7, 8, 9)]
+    ref = reference(x[keep], w, ws, None)
+    assert_within(y[keep], ref, 4 * U32 * ref.abs(), "y")
+
+
+def test_strided_rows_stream_and_graph():
+    from paper_2508_18376_amd import moe_int8_matmul
+    x, w, ws = make(45, 1, 160, 96, torch.bfloat16, 6)
+    wide = torch.zeros(45, 171, dtype=torch.bfloat16, device=DEV)
+    wide[:, 3:163] = x.to(DEV)
+    out = torch.full((45, 101), 5.0, dtype=torch.bfloat16, device=DEV)
+    wd, wsd = w.to(DEV), ws.to(DEV)
+    want = moe_int8_matmul(x.to(DEV), wd, wsd)
+    got = moe_int8_matmul(wide[:, 3:163], wd, wsd, out=out[:, :96])
+    assert torch.equal(got, want) and (out[:, 96:] == 5).all()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    xd = x.to(DEV)
+    torch.cuda.synchronize()
+    y = moe_int8_matmul(xd, wd, wsd, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+    graph, sx = torch.cuda.CUDAGraph(), torch.zeros_like(xd)
+    with torch.cuda.graph(graph):
+        gy = moe_int8_matmul(sx, wd, wsd)
+    for i in range(3):
+        sx.copy_(xd if i != 1 else 2 * xd)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(gy, want if i != 1 else 2 * want) and torch.equal(moe_int8_matmul(xd, wd, wsd), want)
+
+
+def test_no_rows():
+    from paper_2508_18376_amd import moe_int8_matmul
+    y = moe_int8_matmul(torch.empty(0, 32, device=DEV), torch.ones(1, 8, 32, dtype=torch.int8, device=DEV), torch.ones(1, 8, device=DEV))
+    assert y.shape == (0, 8)

@@ -1,0 +1,190 @@
+"""CPU: calls of the operators beside the layer that do not fit their tensors are refused before anything is launched, in the Python binding and at
+the C boundary."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2508_18376_amd as ds
+from paper_2508_18376_amd import operators as ops
+from paper_2508_18376_amd.binding import _lib
+
+I32, BF = torch.int32, torch.bfloat16
+
+
+def z(*shape, dtype=BF):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def off(n):
+    return torch.zeros(n, dtype=I32)
+
+
+GROUPED = {
+    "x of 3 dimensions": lambda: ds.moe_grouped_matmul(z(1, 4, 8), z(2, 8, 6), off(3)),
+    "w of 2 dimensions": lambda: ds.moe_grouped_matmul(z(4, 8), z(8, 6), off(3)),
+    "widths differ": lambda: ds.moe_grouped_matmul(z(4, 7), z(2, 8, 6), off(3)),
+    "widths differ, transposed": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(3), w_transposed=True),
+    "types differ": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6, dtype=torch.float16), off(3)),
+    "integers": lambda: ds.moe_grouped_matmul(z(4, 8, dtype=torch.int8), z(2, 8, 6, dtype=torch.int8), off(3)),
+    "64-bit values": lambda: ds.moe_grouped_matmul(z(4, 8, dtype=torch.float64), z(2, 8, 6, dtype=torch.float64), off(3)),
+    "64-bit offsets": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(3).long()),
+    "offsets too short": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(2)),
+    "offsets too long": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(4)),
+    "offsets with gaps": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(6)[::2]),
+    "x by columns": lambda: ds.moe_grouped_matmul(z(8, 4).t(), z(2, 8, 6), off(3)),
+    "w by columns": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 6, 8).transpose(1, 2), off(3)),
+    "not on a GPU": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 6), off(3)),
+    "dw: rows differ": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(5, 6), off(3)),
+    "dw: types differ": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(4, 6, dtype=torch.float16), off(3)),
+    "dw: one offset": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(4, 6), off(1)),
+    "dw: dy by columns": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(6, 4).t(), off(3)),
+    "dw: not on a GPU": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(4, 6), off(3)),
+    "int8: w in bf16": lambda: ds.moe_int8_matmul(z(4, 8), z(1, 6, 8), z(1, 6, dtype=torch.float32)),
+    "int8: x in int8": lambda: ds.moe_int8_matmul(z(4, 8, dtype=torch.int8), z(1, 6, 8, dtype=torch.int8), z(1, 6, dtype=torch.float32)),
+    "int8: widths differ": lambda: ds.moe_int8_matmul(z(4, 9), z(1, 6, 8, dtype=torch.int8), z(1, 6, dtype=torch.float32)),
+    "int8: scales for too few channels": lambda: ds.moe_int8_matmul(z(4, 8), z(1, 6, 8, dtype=torch.int8), z(1, 5, dtype=torch.float32)),
+    "int8: scales in bf16": lambda: ds.moe_int8_matmul(z(4, 8), z(1, 6, 8, dtype=torch.int8), z(1, 6)),
+    "int8: groups without offsets": lambda: ds.moe_int8_matmul(z(4, 8), z(2, 6, 8, dtype=torch.int8), z(2, 6, dtype=torch.float32)),
+    "int8: not on a GPU": lambda: ds.moe_int8_matmul(z(4, 8), z(1, 6, 8, dtype=torch.int8), z(1, 6, dtype=torch.float32)),
+}
+
+
+def norm(**kw):
+    a = dict(x=z(4, 8), branch=z(4, 8), branch_weight=z(8), weight=z(8), gate=None, eps=1e-6)
+    a.update(kw)
+    return ds.moe_block_norm(a.pop("x"), **a)
+
+
+NORM = {
+    "branch of another shape": dict(branch=z(4, 9)),
+    "branch of another type": dict(branch=z(4, 8, dtype=torch.float32)),
+    "x of 1 dimension": dict(x=z(8), branch=z(8)),
+    "rows without values": dict(x=z(4, 0), branch=z(4, 0), branch_weight=z(0), weight=z(0)),
+    "short weight": dict(weight=z(7)),
+    "branch_weight by rows": dict(branch_weight=z(1, 8)),
+    "gate of 1 dimension": dict(gate=z(8)),
+    "gate of one value": dict(gate=z(1, 1)),
+    "gate for too few tokens": dict(gate=z(3, 1)),
+    "gate of another type": dict(gate=z(4, 1, dtype=torch.float32)),
+    "gate by columns": dict(gate=z(8, 4).t()),
+    "weights with gaps": dict(weight=z(16)[::2]),
+    "negative eps": dict(eps=-1e-6),
+    "integers": dict(x=z(4, 8, dtype=I32), branch=z(4, 8, dtype=I32), branch_weight=z(8, dtype=I32), weight=z(8, dtype=I32)),
+    "not on a GPU": dict(),
+}
+
+
+@pytest.mark.parametrize("case", GROUPED)
+def test_products_refuse(case):
+    with pytest.raises(ds.DsmoeError) as e:
+        GROUPED[case]()
+    assert e.value.status == -1 and "moe_" in str(e.value)
+
+
+@pytest.mark.parametrize("case", NORM)
+def test_norms_refuse(case):
+    with pytest.raises(ds.DsmoeError) as e:
+        norm(**NORM[case])
+    assert e.value.status == -1 and "moe_block_norm" in str(e.value)
+
+
+@pytest.mark.parametrize("bad", ["dy", "dh", "stats", "stats_type", "type"])
+def test_norms_backward_refuses(bad):
+    dy, dh, x, stats = z(4, 8), z(4, 8), z(4, 8), z(2, 4, dtype=torch.float32)
+    if bad == "dy":
+        dy = z(4, 7)
+    if bad == "dh":
+        dh = z(5, 8)
+    if bad == "stats":
+        stats = z(4, 2, dtype=torch.float32)
+    if bad == "stats_type":
+        stats = z(2, 4)
+    if bad == "type":
+        dy = z(4, 8, dtype=torch.float32)
+    with pytest.raises(ds.DsmoeError) as e:
+        ds.moe_block_norm_backward(dy, dh, x, stats, branch=z(4, 8), branch_weight=z(8), weight=z(8))
+    assert e.value.status == -1
+
+
+P = 1 << 20  # an address that nothing reads: every call below is refused
+
+
+def grouped(x=P, xs=64, w=P, wg=64 * 32, wr=32, o=P, rows=10, groups=2, k=64, n=32, t=0, dt=1, y=P, ys=32):
+    return _lib.moe_grouped_matmul(x, xs, w, wg, wr, o, rows, groups, k, n, t, dt, y, ys, None)
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(o=None), dict(y=None), dict(rows=-1), dict(groups=0), dict(k=0), dict(n=0), dict(t=2),
+                                dict(dt=3), dict(dt=-1), dict(xs=-1), dict(wg=-1), dict(wr=-1), dict(ys=31), dict(t=1), dict(x=P + 1), dict(y=P + 1),
+                                dict(dt=0, w=P + 2), dict(rows=(1 << 23) + 1), dict(groups=1 << 17), dict(k=(1 << 24) + 1),
+                                dict(rows=1 << 23, n=1 << 24, ys=1 << 24)], ids=str)
+def test_grouped_boundary(kw):
+    assert grouped(**kw) == -1
+
+
+def dw(x=P, xs=64, dy=P, ds_=32, o=P, rows=10, groups=2, k=64, n=32, dt=1, out=P, og=64 * 32, orow=32):
+    return _lib.moe_grouped_matmul_dw(x, xs, dy, ds_, o, rows, groups, k, n, dt, out, og, orow, None)
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(dy=None), dict(o=None), dict(out=None), dict(rows=-1), dict(groups=0), dict(k=0), dict(n=0), dict(dt=3),
+                                dict(xs=-1), dict(ds_=-1), dict(orow=31), dict(og=64 * 32 - 1), dict(x=P + 1), dict(out=P + 1),
+                                dict(k=1 << 24, n=1 << 24, orow=1 << 24, og=1 << 39)], ids=str)
+def test_dw_boundary(kw):
+    assert dw(**kw) == -1
+
+
+def int8(x=P, xs=64, w=P, wg=64 * 32, wr=64, ws=P, wsg=32, o=P, rows=10, groups=2, k=64, n=32, dt=1, y=P, ys=32, work=P):
+    return _lib.moe_int8_matmul(x, xs, w, wg, wr, ws, wsg, o, rows, groups, k, n, dt, y, ys, work, None)
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(work=None), dict(o=None), dict(rows=-1), dict(groups=0),
+                                dict(k=0), dict(k=(1 << 17) + 1), dict(n=0), dict(dt=3), dict(xs=-1), dict(wr=-1), dict(wsg=-1), dict(ys=31),
+                                dict(work=P + 128), dict(ws=P + 2), dict(x=P + 1)], ids=str)
+def test_int8_boundary(kw):
+    assert int8(**kw) == -1
+
+
+def test_workspace_sizes():
+    assert _lib.dsmoe_int8_workspace_bytes(10, 64) >= 10 * 64 + 40
+    assert _lib.dsmoe_int8_workspace_bytes(-1, 64) == 0 and _lib.dsmoe_int8_workspace_bytes(10, 0) == 0
+    a = ops._BlockNormArgs(100, 64, 1, 2, 1.0, 0.0, 1e-6, 0, 64, 64, 0, 64, 64)
+    assert _lib.dsmoe_block_norm_workspace_bytes(a) >= 3 * 64 * 4
+    a.gate_kind = 4
+    assert _lib.dsmoe_block_norm_workspace_bytes(a) == 0 and _lib.dsmoe_block_norm_workspace_bytes(None) == 0
+
+
+NORM_ARGS = dict(tokens=4, d=8, dtype=1, gate_kind=0, scale=1.0, weight_offset=0.0, eps=1e-6, pad=0, x_stride=8, branch_stride=8, gate_stride=0, dy_stride=8,
+                 dh_stride=8)
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=-1), dict(d=0), dict(dtype=3), dict(gate_kind=-1), dict(gate_kind=4), dict(eps=-1.0), dict(eps=float("nan")),
+                                dict(x_stride=-1), dict(branch_stride=-1), dict(gate_stride=-1), dict(gate_kind=1)], ids=str)
+def test_norm_boundary(kw):
+    a = ops._BlockNormArgs(**dict(NORM_ARGS, **kw))
+    assert _lib.moe_block_norm(a, P, P, P, None, P, P, P, P, None) == -1
+    assert _lib.moe_block_norm_backward(a, P, P, P, P, P, None, P, P, P, P, P, None, P, P, None) == -1
+
+
+def test_norm_pointers():
+    a = ops._BlockNormArgs(**NORM_ARGS)
+    good = [P, P, P, None, P, P, P]
+    for i in (0, 1, 2, 4, 5, 6):
+        for bad in (None, P + 1):
+            p = list(good)
+            p[i] = bad
+            assert _lib.moe_block_norm(a, *p, P, None) == -1
+    assert _lib.moe_block_norm(a, P, P, P, P, P, P, P, P, None) == -1  # a gate where there is none
+    assert _lib.moe_block_norm(None, *good, P, None) == -1
+    good = [P, P, P, P, P, None, P, P, P, P, P, None, P, P]
+    for i in (0, 1, 2, 3, 4, 6, 7, 8, 9, 10, 12, 13):
+        p = list(good)
+        p[i] = None
+        assert _lib.moe_block_norm_backward(a, *p, None) == -1
+    p = list(good)
+    p[13] = P + 64
+    assert _lib.moe_block_norm_backward(a, *p, None) == -1
+
+
+def test_errors_without_a_context_are_kept():
+    _lib.dsmoe_last_hip_error.restype = ctypes.c_int
+    assert _lib.dsmoe_last_hip_error(None) == 0
