@@ -138,6 +138,17 @@ __device__ __forceinline__ void band_tile(int id, int row_tiles, int col_tiles, 
 // (R - segments) / BM + segments tiles: a first row in each segment, and a tile more for every BM further rows at most
 hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
 hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s);
+// the fast path of 16-bit types and 8-bit integers, where the operands lie for it
+bool grouped_mfma_fits(const GroupedArgs& g, int type, bool b_along);
+hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
+bool grouped_dw_mfma_fits(const GroupedArgs& g, int type);
+hipError_t launch_grouped_dw_mfma(const GroupedArgs& g, int type, hipStream_t s);
+inline hipError_t launch_grouped(const GroupedArgs& g, int type, bool b_along, hipStream_t s) {
+  return grouped_mfma_fits(g, type, b_along) ? launch_grouped_mfma(g, type, b_along, s) : launch_grouped_plain(g, type, b_along, s);
+}
+inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t s) {
+  return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
+}
 
 __device__ __forceinline__ float elem_to_f32(const char* p, int type) {
   if (type == kElemF32) return *(const float*)p;

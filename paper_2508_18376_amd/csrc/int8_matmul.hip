@@ -98,7 +98,7 @@ hipError_t launch_int8_matmul(const Int8Args& a, hipStream_t s) {
   g.b_scale = a.w_scale;
   g.bs_group = a.ws_group;
   g.out_type = a.type;
-  return launch_grouped_plain(g, kElemI8, true, s);
+  return launch_grouped(g, kElemI8, true, s);
 }
 
 }  // namespace dsmoe

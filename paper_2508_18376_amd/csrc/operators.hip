@@ -84,7 +84,7 @@ int moe_grouped_matmul(const void* x, int64_t x_stride, const void* w, int64_t w
   g.G = groups;
   g.N = transposed ? k : n;
   g.K = transposed ? n : k;
-  return status(launch_grouped_plain(g, dtype, transposed != 0, (hipStream_t)stream));
+  return status(launch_grouped(g, dtype, transposed != 0, (hipStream_t)stream));
 }
 
 int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offsets, int32_t rows,
@@ -110,7 +110,7 @@ int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64
   g.G = groups;
   g.M = k;
   g.N = n;
-  return status(launch_grouped_dw_plain(g, dtype, (hipStream_t)stream));
+  return status(launch_grouped_dw(g, dtype, (hipStream_t)stream));
 }
 
 size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t k) {
