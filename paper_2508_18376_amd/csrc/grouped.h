@@ -125,6 +125,13 @@ inline int64_t row_tiles_bound(int64_t R, int64_t G, bool grouped, int BM) {
   return (R - segments) / BM + segments;
 }
 
+// The piece of n that place b takes (n: none): take_piece without the free ones, for workgroups that take several.
+__device__ __forceinline__ int piece_of(int b, int n) {
+  if (b >= n) return n;
+  const int base = b & ~255, x = b & 7, i = (b & 255) >> 3, left = min(n - base, 256), q = left >> 3, r = left & 7;
+  return base + x * q + min(x, r) + i;
+}
+
 // Inside a segment the pieces go in bands of 8 row tiles, column tile by column tile: 32 neighbours (what an XCD gets at a time, see take_piece)
 // share 8 row tiles and 4 column tiles.
 constexpr int kBand = 8;
@@ -156,7 +163,7 @@ __device__ __forceinline__ float elem_to_f32(const char* p, int type) {
   return (float)*(const _Float16*)p;
 }
 __device__ __forceinline__ uint16_t f32_to_16(float v, int type) {
-  return type == kElemBF16 ? f32_to_bf16(v) : __builtin_bit_cast(uint16_t, (_Float16)v);
+  return type == kElemBF16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
 }  // namespace dsmoe

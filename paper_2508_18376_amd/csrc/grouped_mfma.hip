@@ -32,12 +32,17 @@ typedef float gf32x16 __attribute__((ext_vector_type(16)));
 typedef int gi32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kGT = 256;                       // tile edge
-constexpr int kRing = 4;                       // stages
-constexpr int kOperandStage = kGT * 64;        // bytes of an operand's stage
-constexpr int kRingStage = 2 * kOperandStage;  // A, then B
-constexpr int kRingBytes = kRing * kRingStage;
+constexpr int kUnit = kGT * 128;               // bytes of an operand's stage
+constexpr int kUnits = 5;                      // units of the ring: all of a compute unit's LDS
+constexpr int kRingBytes = kUnits * kUnit;
+constexpr int kLoads = kUnit / 16 / 256;        // a thread's loads of a unit
+constexpr int kWorkgroups = 256;                // one to a compute unit
 constexpr uint32_t kOutOfBounds = 0x80000000u;  // beyond every buffer here (extents are below 2^31)
 
+template <int V>
+struct Const {
+  static constexpr int value = V;
+};
 template <int TY>
 struct GElem {
   static constexpr int bytes = TY == kElemI8 ? 1 : 2;
@@ -58,15 +63,15 @@ __device__ __forceinline__ void mac(typename AccType<TY>::type& c, const gi32x4&
   if constexpr (TY == kElemI8) c = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
 }
 
-// 16 bytes a lane to LDS at lds + 16 * lane
-__device__ __forceinline__ void load_to_lds(const gi32x4& rsrc, uint32_t lds, uint32_t voff) {
+// 16 bytes a lane to LDS at lds + part + 16 * lane
+__device__ __forceinline__ void load_to_lds(const gi32x4& rsrc, uint32_t lds, uint32_t part, uint32_t voff) {
   asm volatile(
-      "s_mov_b32 m0, %0\n\t"
+      "s_add_u32 m0, %0, %1\n\t"
       "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, 0 offen lds"
+      "buffer_load_dwordx4 %2, %3, 0 offen lds"
       :
-      : "s"(lds), "v"(voff), "s"(rsrc)
-      : "memory");
+      : "s"(lds), "s"(part), "v"(voff), "s"(rsrc)
+      : "memory", "scc");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -75,47 +80,46 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ void stage_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)((__attribute__((address_space(3))) const char*)p); }
-__device__ __forceinline__ gi32x4 lds_read16(uint32_t at) { return *(__attribute__((address_space(3))) const gi32x4*)(uintptr_t)at; }
-__device__ __forceinline__ gs16x4 lds_read_across(uint32_t at) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) gs16x4*)(uintptr_t)at);
-}
+typedef __attribute__((address_space(3))) const char* lds_ptr;
+__device__ __forceinline__ lds_ptr lds_at(uint32_t address) { return (lds_ptr)(uintptr_t)address; }
+__device__ __forceinline__ gi32x4 lds_read16(lds_ptr p) { return *(__attribute__((address_space(3))) const gi32x4*)p; }
+__device__ __forceinline__ gs16x4 lds_read_across(lds_ptr p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) gs16x4*)p); }
 
-// An operand's way from memory to LDS.  L loads a thread and stage.
-//   along    base moves 64 bytes a stage, the offsets (row, chunk) stay
-//   across   base moves 32 rows a stage
-// bytes: the extent from the base on; shrinks along with the moves.
-template <bool ACROSS, int L>
+// position of chunk `chunk` (0..7) of row `row` in a [rows][128 bytes] tile; its own inverse.  Two rows are a turn of the banks.
+__device__ __forceinline__ int swz_wide(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
+
+// An operand's way from memory to LDS: a unit is 256 rows x 128 bytes (along) or 64 contraction rows x 512 bytes (across).
+// The lanes' offsets are the same for all tiles.  A tile has a base, which moves on by a unit's stretch of the contraction (two scalar
+// additions: scalar instructions in a row would hold up the matrix instructions), and an extent from there on, one for the last unit and
+// one for the others.
+template <bool ACROSS>
 struct Feed {
-  uint64_t base;
-  int64_t bytes;
-  int64_t step;  // per stage
-  uint32_t voff[L], tail;
-
-  // origin: first value.  across: `rows` contraction rows of `width` bytes; along: `rows` rows with `width` bytes of the contraction
-  __device__ __forceinline__ void init(const char* origin, int64_t row_bytes, int rows, int64_t width, int tid) {
-    base = (uint64_t)(uintptr_t)origin;
-    bytes = (rows - 1) * row_bytes + width;
-    step = ACROSS ? 32 * row_bytes : 64;
+  uint32_t voff[kLoads];
+  uint32_t lo, hi, extent, last_extent;
+  int64_t step;
+  __device__ __forceinline__ void lanes(int64_t row_bytes, int tid) {
+    step = ACROSS ? 64 * row_bytes : 128;
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (ACROSS) {
-        const int r = i * 8 + (tid >> 5);
-        voff[i] = (uint32_t)(r * (int)row_bytes + (((tid & 31) ^ ((r & 3) << 2)) * 16));
-      } else {
-        const int r = i * 64 + (tid >> 2);
-        voff[i] = (uint32_t)(r * (int)row_bytes + swz_chunk(r, tid & 3) * 16);
-      }
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = ACROSS ? i * 8 + (tid >> 5) : i * 32 + (tid >> 3);
+      voff[i] = (uint32_t)(r * (int)row_bytes + (ACROSS ? (tid & 31) ^ ((r & 3) << 2) : swz_wide(r, tid & 7)) * 16);
     }
-    tail = 0;
   }
-  __device__ __forceinline__ gi32x4 next() {  // the stage's buffer
-    gi32x4 r;
-    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)base);
-    r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff);
-    r[2] = __builtin_amdgcn_readfirstlane((int)(bytes < 0 ? 0 : bytes < kOutOfBounds ? bytes : kOutOfBounds));
-    r[3] = 0x00020000;
-    base += step;
-    bytes -= step;
+  // origin: the tile's first value.  along: `rows` rows, `last` bytes of the contraction in the last unit; across: rows of `rows` bytes, `last`
+  // contraction rows in the last unit
+  __device__ __forceinline__ void tile(const char* origin, int64_t row_bytes, int rows, int last) {
+    const uint64_t base = (uint64_t)(uintptr_t)origin;
+    lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)base);
+    hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32));  // (addresses have 48 bits)
+    extent = (uint32_t)__builtin_amdgcn_readfirstlane((int)(ACROSS ? 63 * row_bytes + rows : (rows - 1) * row_bytes + 128));
+    last_extent = (uint32_t)__builtin_amdgcn_readfirstlane((int)(ACROSS ? (last - 1) * row_bytes + rows : (rows - 1) * row_bytes + last));
+  }
+  __device__ __forceinline__ gi32x4 next(bool last) {  // the next unit's buffer
+    const gi32x4 r = {__builtin_amdgcn_readfirstlane((int)lo), __builtin_amdgcn_readfirstlane((int)hi),
+                      __builtin_amdgcn_readfirstlane((int)(last ? last_extent : extent)), 0x00020000};
+    const uint64_t base = ((uint64_t)hi << 32 | lo) + (uint64_t)step;
+    lo = (uint32_t)base;
+    hi = (uint32_t)(base >> 32);
     return r;
   }
 };
@@ -123,37 +127,37 @@ struct Feed {
 // One wavefront's reads of an operand's fragments: NB blocks of 32 rows (along) or columns (across), the first one r0.
 template <bool ACROSS, int NB>
 struct Reader {
-  uint32_t at[ACROSS ? NB : 2];
-  __device__ __forceinline__ void init(uint32_t tile, int r0, int lane) {
+  uint32_t at[4];  // across: of block b; along: of substep s
+  static constexpr int parts = ACROSS ? 2 : 1;
+  __device__ __forceinline__ void init(uint32_t ring, int r0, int lane) {
     if (ACROSS) {
       const int i = lane & 15, g = lane >> 4;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const int col = r0 + 32 * b + 16 * (g & 1) + 4 * (i & 3);
-        at[b] = tile + (8 * (g >> 1) + (i >> 2)) * 512 + (((col >> 3) ^ ((i >> 2) << 2)) * 16) + (col & 7) * 2;
+        at[b] = ring + (8 * (g >> 1) + (i >> 2)) * 512 + (((col >> 3) ^ ((i >> 2) << 2)) * 16) + (col & 7) * 2;
       }
     } else {
       const int r = r0 + (lane & 31);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) at[s] = tile + r * 64 + swz_chunk(r, 2 * s + (lane >> 5)) * 16;
+      for (int s = 0; s < 4; ++s) at[s] = ring + r * 128 + swz_wide(r, 2 * s + (lane >> 5)) * 16;
     }
   }
-  // part p of block b's fragment (across: two parts) for substep s, in the stage at `slot`
-  static constexpr int parts = ACROSS ? 2 : 1;
-  __device__ __forceinline__ void read(gi32x4 (&f)[NB], int b, int p, int s, uint32_t slot) const {
+  // part p of block b's fragment for substep s, in the unit at `unit`
+  __device__ __forceinline__ void read(gi32x4 (&f)[NB], int b, int p, int s, uint32_t unit) const {
     if constexpr (ACROSS) {
-      const gs16x4 v = lds_read_across(at[b] + slot + s * (16 * 512) + p * (4 * 512));
+      const gs16x4 v = lds_read_across(lds_at(at[b] + unit) + (s * (16 * 512) + p * (4 * 512)));
       __builtin_memcpy((char*)&f[b] + 8 * p, &v, 8);
     } else {
-      f[b] = lds_read16(at[s] + slot + b * (32 * 64));
+      f[b] = lds_read16(lds_at(at[s] + unit) + b * (32 * 128));
     }
   }
 };
 
-// A tile: MI x NI blocks of 32 x 32 a wavefront, LA + LB loads a thread and stage.
-template <int TY, bool AX, bool BX, int MI, int NI, int LA, int LB>
+// The products of a tile: MI x NI blocks of 32 x 32 a wavefront.
+template <int TY, bool AX, bool BX, int MI, int NI>
 struct Tile {
-  static constexpr int M = MI * NI, L = LA + LB, READS = MI * Reader<AX, MI>::parts + NI * Reader<BX, NI>::parts;
+  static constexpr int M = MI * NI, READS = MI * Reader<AX, MI>::parts + NI * Reader<BX, NI>::parts;
   typename AccType<TY>::type acc[MI][NI];
   struct Frags {
     gi32x4 a[MI], b[NI];
@@ -161,48 +165,40 @@ struct Tile {
   Reader<AX, MI> ra;
   Reader<BX, NI> rb;
 
-  __device__ __forceinline__ void read_k(Frags& f, int k, int s, uint32_t slot) const {
+  __device__ __forceinline__ void read_k(Frags& f, int k, int s, uint32_t ua, uint32_t ub) const {
     constexpr int PA = Reader<AX, MI>::parts, PB = Reader<BX, NI>::parts;
     // the order in which the products want them: first block of A, all of B, the rest of A
     if (k < PA)
-      ra.read(f.a, 0, k, s, slot);
+      ra.read(f.a, 0, k, s, ua);
     else if (k < PA + NI * PB)
-      rb.read(f.b, (k - PA) / PB, (k - PA) % PB, s, slot);
+      rb.read(f.b, (k - PA) / PB, (k - PA) % PB, s, ub);
     else
-      ra.read(f.a, (k - NI * PB) / PA, (k - NI * PB) % PA, s, slot);
+      ra.read(f.a, (k - NI * PB) / PA, (k - NI * PB) % PA, s, ua);
   }
 
-  // the products of one substep; between them, early, the reads of the next substep and, if LOADS, the loads of a later stage
-  template <bool LOADS, class One>
-  __device__ __forceinline__ void substep(const Frags& cur, Frags& nxt, bool reads, int nxt_s, uint32_t nxt_slot, One&& one) {
-    constexpr int EARLY = M >= 8 ? M / 2 : M;  // products among which the reads go
+  // the products of one substep; between them, early, the reads of the next one, and LOADS loads
+  template <int LOADS, class One>
+  __device__ __forceinline__ void substep(const Frags& cur, Frags& nxt, bool reads, int nxt_s, uint32_t ua, uint32_t ub, One&& one) {
+    // A product takes as long as some eight other instructions, and what lies between two of them beyond that holds up the matrix core: reads
+    // and loads are spread and pinned (8192 x 8192 x 8192 in bf16: 850 us before that and with twice the scalar instructions, 780 after).
+    constexpr int EARLY = M >= 8 ? M / 2 : M;
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       mac<TY>(acc[m / NI][m % NI], cur.b[m % NI], cur.a[m / NI]);
       if (reads && m < EARLY) {
 #pragma unroll
-        for (int k = m * READS / EARLY; k < (m + 1) * READS / EARLY; ++k) read_k(nxt, k, nxt_s, nxt_slot);
+        for (int k = m * READS / EARLY; k < (m + 1) * READS / EARLY; ++k) read_k(nxt, k, nxt_s, ua, ub);
       }
-      if (LOADS) {
 #pragma unroll
-        for (int q = m * L / M; q < (m + 1) * L / M; ++q) one(q);
-      }
-      if ((m & 1) || M < 4) __builtin_amdgcn_sched_barrier(0);
+      for (int q = m * LOADS / M; q < (m + 1) * LOADS / M; ++q) one(q);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
-  static __device__ __forceinline__ void wait_stages(int k) {  // all but the last k stages of this thread's loads are there
-    if (k <= 0)
-      wait_loads<0>();
-    else if (k == 1)
-      wait_loads<L>();
-    else
-      wait_loads<2 * L>();
-  }
-
-  // n stages; begin(): the next stage's buffers; one(q): its q-th load, into the ring slot `slot`
-  template <class Begin, class One>
-  __device__ __forceinline__ void run(int n, Begin&& begin, One&& one) {
+  // n stages, of which the units A0 B0 A1 B1 (as far as there are any) are in the ring's first four places, for every wavefront.
+  // load_a / load_b (last): the next unit of A / B, its buffer; one_a / one_b(q, place): its q-th load.
+  template <class LoadA, class LoadB, class OneA, class OneB>
+  __device__ __forceinline__ void run(int n, LoadA&& load_a, LoadB&& load_b, OneA&& one_a, OneB&& one_b) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -210,163 +206,198 @@ struct Tile {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
     if (n <= 0) return;
-    constexpr int PD = kRing - 1;
     Frags f0, f1;
+    auto nothing = [](int) {};
 #pragma unroll
-    for (int s = 0; s < PD; ++s)
-      if (s < n) {
-        begin(s);
-#pragma unroll
-        for (int q = 0; q < L; ++q) one(q);
-      }
-    wait_stages((n < PD ? n : PD) - 1);
-    stage_barrier();
-#pragma unroll
-    for (int k = 0; k < READS; ++k) read_k(f0, k, 0, 0);
+    for (int k = 0; k < READS; ++k) read_k(f0, k, 0, 0, kUnit);
+    uint32_t ua = 0, ub = kUnit, free = 4 * kUnit;  // places of stage st's units, and the free one
     int st = 0;
-    for (; st + PD < n; ++st) {
-      const uint32_t cur = (uint32_t)(st % kRing) * kRingStage, nxt = (uint32_t)((st + 1) % kRing) * kRingStage;
-      substep<false>(f0, f1, true, 1, cur, one);
-      // stage st + 1 is there for every wavefront, and every wavefront has read all of stage st - 1, whose slot stage st + PD takes
-      wait_loads<(PD - 2) * L>();
+    for (; st + 2 < n; ++st) {
+      const uint32_t na = ua >= 3 * kUnit ? ua - 3 * kUnit : ua + 2 * kUnit, nb = ub >= 3 * kUnit ? ub - 3 * kUnit : ub + 2 * kUnit;
+      load_a(st + 3 == n);
+      substep<kLoads>(f0, f1, true, 1, ua, ub, [&](int q) { one_a(q, free); });
+      substep<0>(f1, f0, true, 2, ua, ub, nothing);
+      substep<0>(f0, f1, true, 3, ua, ub, nothing);
+      // stage st + 1's units are there for every wavefront (A's of stage st + 2 may still be under way), and every wavefront has read all of
+      // stage st's: B's unit of stage st + 2 takes the place of A's, A's of stage st + 3 will take that of B's
+      wait_loads<kLoads>();
       stage_barrier();
-      begin(st + PD);
-      substep<true>(f1, f0, true, 0, nxt, one);
+      load_b(st + 3 == n);
+      substep<kLoads>(f1, f0, true, 0, na, nb, [&](int q) { one_b(q, ua); });
+      free = ub;
+      ua = na;
+      ub = nb;
     }
-    for (; st < n; ++st) {  // nothing left to load
-      const uint32_t cur = (uint32_t)(st % kRing) * kRingStage, nxt = (uint32_t)((st + 1) % kRing) * kRingStage;
-      substep<false>(f0, f1, true, 1, cur, one);
+    for (; st < n; ++st) {  // the last two stages: nothing left to load
+      const uint32_t na = ua >= 3 * kUnit ? ua - 3 * kUnit : ua + 2 * kUnit, nb = ub >= 3 * kUnit ? ub - 3 * kUnit : ub + 2 * kUnit;
+      substep<0>(f0, f1, true, 1, ua, ub, nothing);
+      substep<0>(f1, f0, true, 2, ua, ub, nothing);
+      substep<0>(f0, f1, true, 3, ua, ub, nothing);
       if (st + 1 < n) {
-        wait_stages(n - 2 - st);
+        wait_loads<0>();
         stage_barrier();
       }
-      substep<false>(f1, f0, st + 1 < n, 0, nxt, one);
+      substep<0>(f1, f0, st + 1 < n, 0, na, nb, nothing);
+      ua = na;
+      ub = nb;
     }
   }
 };
 
-// 8 values of 16 bits from fp32
+// 2 values of 16 bits from fp32, rounded to nearest
 template <int TY>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
-  return (uint32_t)f32_to_16(a, TY) | (uint32_t)f32_to_16(b, TY) << 16;
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  if (TY == kElemBF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
 }
 
-struct TileAt {
-  const char *pa, *pb;  // first row (column) of the tile in A and B
-  char* pc;             // first value of the tile in C
+// What a workgroup does for one piece.
+struct Piece {
+  const char *pa, *pb;   // first row (column) of the tile in A and B
+  char* pc;              // first value of the tile in C
   const float *as, *bs;  // 8-bit: factors from the tile's first row and column on
-  int m_edge, n_edge;   // rows and columns of the tile that exist
-  int64_t K;            // contraction: values (along A) or rows (across)
+  int m_edge, n_edge;    // rows and columns of the tile that exist
+  int K;                 // contraction: values (along A) or rows (across)
 };
 
-// The whole tile, of which a wavefront has rows wm .. + 32 MI and columns wn .. + 32 NI.
-template <int TY, int OUT, bool AX, bool BX, int MI, int NI, int LA, int LB>
-__device__ __forceinline__ void do_tile(const GroupedArgs& g, const TileAt& t, char* lds, int wm, int wn) {
+// The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
+// While a tile's values leave through the fifth unit of the ring, the next tile's first four units are under way.
+template <int TY, int OUT, bool AX, bool BX, class Next>
+__device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&& piece) {
   constexpr int EB = GElem<TY>::bytes;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t ring = lds_address(lds);
-  Tile<TY, AX, BX, MI, NI, LA, LB> tile;
-  tile.ra.init(ring, wm, lane);
-  tile.rb.init(ring + kOperandStage, wn, lane);
-  Feed<AX, LA> fa;
-  Feed<BX, LB> fb;
+  Feed<AX> fa;
+  Feed<BX> fb;
+  fa.lanes(g.a_row, tid);
+  fb.lanes(g.b_row, tid);
   // (the bounds cut off whole 32-bit words: 8-bit rows whose values end inside one count it)
-  auto whole_words = [](int64_t b) { return TY == kElemI8 ? (b + 3) & ~(int64_t)3 : b; };
-  if (AX)
-    fa.init(t.pa, g.a_row, (int)t.K, (int64_t)t.m_edge * EB, tid);
-  else
-    fa.init(t.pa, g.a_row, t.m_edge, whole_words(t.K * EB), tid);
-  if (BX)
-    fb.init(t.pb, g.b_row, (int)t.K, (int64_t)t.n_edge * EB, tid);
-  else
-    fb.init(t.pb, g.b_row, t.n_edge, whole_words(t.K * EB), tid);
-  const int n = AX ? (int)((t.K + 31) / 32) : (int)((t.K * EB + 63) / 64);
-  // chunks past the contraction's end in the last stage (8 bits: A's rows are zero there, so what B has does not matter)
-  const int last_chunks = !AX && TY != kElemI8 ? (int)((t.K * EB & 63) >> 4) : 0;
-  const int chunk = swz_chunk(tid >> 2, tid & 3);
-  const uint32_t beyond = last_chunks && chunk >= last_chunks ? kOutOfBounds : 0;
-  gi32x4 rsa, rsb;
-  uint32_t slot = 0;
-  auto begin = [&](int st) {
-    rsa = fa.next();
-    rsb = fb.next();
-    slot = ring + (uint32_t)(st % kRing) * kRingStage + (uint32_t)w * 1024;
-    if (!AX) {
-      fa.tail = st == n - 1 ? beyond : 0;
-      if (!BX) fb.tail = fa.tail;
+  auto whole_words = [](int b) { return TY == kElemI8 ? (b + 3) & ~3 : b; };
+  auto stages = [&](const Piece& p) { return AX ? (p.K + 63) / 64 : (int)(((int64_t)p.K * EB + 127) / 128); };
+  uint32_t tail = 0;  // makes a lane's offset one out of bounds: chunks past the contraction's end in the last stage
+  uint32_t beyond = 0;
+  auto start = [&](const Piece& p) __attribute__((always_inline)) {
+    const int kb = (int)(((int64_t)p.K * EB + 127) & 127) + 1, kr = ((p.K + 63) & 63) + 1;  // bytes or rows of the contraction in the last unit
+    fa.tile(p.pa, g.a_row, AX ? p.m_edge * EB : p.m_edge, AX ? kr : whole_words(kb));
+    fb.tile(p.pb, g.b_row, BX ? p.n_edge * EB : p.n_edge, BX ? kr : whole_words(kb));
+    // (8 bits: A's rows are zero behind the end, so what B has there does not matter)
+    beyond = !AX && TY != kElemI8 && swz_wide(tid >> 3, tid & 7) * 16 >= kb ? kOutOfBounds : 0;
+  };
+  gi32x4 rs;
+  const uint32_t mine = ring + (uint32_t)w * 1024;
+  auto load_a = [&](bool last) __attribute__((always_inline)) {
+    rs = fa.next(last);
+    tail = !AX && last ? beyond : 0;
+  };
+  auto load_b = [&](bool last) __attribute__((always_inline)) {
+    rs = fb.next(last);
+    tail = !BX && last ? beyond : 0;
+  };
+  auto one_a = [&](int q, uint32_t place) __attribute__((always_inline)) { load_to_lds(rs, mine + place, q * 4096, AX ? fa.voff[q] : fa.voff[q] | tail); };
+  auto one_b = [&](int q, uint32_t place) __attribute__((always_inline)) { load_to_lds(rs, mine + place, q * 4096, BX ? fb.voff[q] : fb.voff[q] | tail); };
+  auto first_units = [&](const Piece& p) __attribute__((always_inline)) {
+    start(p);
+    const int n = stages(p);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (u / 2 >= n) continue;
+      if (u & 1)
+        load_b(u / 2 == n - 1);
+      else
+        load_a(u / 2 == n - 1);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) (u & 1) ? one_b(q, u * kUnit) : one_a(q, u * kUnit);
     }
   };
-  auto one = [&](int q) {
-    if (q < LB)
-      load_to_lds(rsb, slot + kOperandStage + q * 4096, BX ? fb.voff[q] : fb.voff[q] | fb.tail);
-    else
-      load_to_lds(rsa, slot + (q - LB) * 4096, AX ? fa.voff[q - LB] : fa.voff[q - LB] | fa.tail);
-  };
-  tile.run(n, begin, one);
 
-  // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
-  const int r32 = lane & 31, half = lane >> 5;
-  auto value = [&](int i, int j, int v, float as, const float* bs) -> float {
-    if constexpr (TY == kElemI8)
-      return (float)tile.acc[i][j][v] * as * bs[v & 3];
-    else
-      return tile.acc[i][j][v];
-  };
-  if constexpr (OUT == kElemF32) {
+  Piece p, nxt;
+  int i = 0;
+  bool more = piece(i, p);
+  if (!more) return;
+  first_units(p);
+  while (more) {
+    more = piece(++i, nxt);
+    // all of this wavefront's loads and stores; for all wavefronts, the fifth unit is free
+    wait_loads<0>();
+    stage_barrier();
+    auto whole = [&](auto& tile, int wm, int wn, auto MI_, auto NI_) __attribute__((always_inline)) {
+      constexpr int MI = decltype(MI_)::value, NI = decltype(NI_)::value;
+      // (an opaque copy: what follows from it is worked out here, for this tile, and not kept in registers across the others)
+      int lane = tid & 63;
+      asm volatile("" : "+v"(lane));
+      tile.ra.init(ring, wm, lane);
+      tile.rb.init(ring, wn, lane);
+      const int n = stages(p);
+      tile.run(n, load_a, load_b, one_a, one_b);
+      stage_barrier();
+      if (more) first_units(nxt);
+      // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
+      const int r32 = lane & 31, half = lane >> 5;
+      auto value = [&](int a, int b, int v, float as, const float* bs) __attribute__((always_inline)) -> float {
+        if constexpr (TY == kElemI8)
+          return (float)tile.acc[a][b][v] * as * bs[v & 3];
+        else
+          return tile.acc[a][b][v];
+      };
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int r = wm + i * 32 + r32;
-      if (r >= t.m_edge) continue;
-      const float as = t.as[r];
+      for (int a = 0; a < MI; ++a) {
+        const int r = wm + a * 32 + r32;
+        const float as = TY == kElemI8 && p.K > 0 && r < p.m_edge ? p.as[r] : 0.f;
+        // 16 bits: each wavefront turns 32 rows at a time around in its part of the fifth unit and stores 16 bytes a lane, rows of 64 NI
+        // bytes; their 16-byte chunks are rotated by the row
+        constexpr int LPR = NI * 4;  // chunks of a row
+        char* turn = lds + 4 * kUnit + w * (kUnit / 4);
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+        for (int b = 0; b < NI; ++b)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = wn + j * 32 + 8 * q + 4 * half;
-          if (c >= t.n_edge) continue;
-          float bs[4] = {0, 0, 0, 0};
-          gf32x4 v = {0, 0, 0, 0};
-          if (t.K > 0) {
-            __builtin_memcpy(bs, t.bs + c, 16);
+          for (int q = 0; q < 4; ++q) {
+            const int c = wn + b * 32 + 8 * q + 4 * half;
+            float bs[4] = {0, 0, 0, 0};
+            if (TY == kElemI8 && p.K > 0 && c < p.n_edge) __builtin_memcpy(bs, p.bs + c, 16);
+            float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = value(i, j, 4 * q + e, as, bs);
+            for (int e = 0; e < 4; ++e) v[e] = value(a, b, 4 * q + e, as, bs);
+            if constexpr (OUT == kElemF32) {
+              if (r < p.m_edge && c < p.n_edge) *(gf32x4*)(p.pc + r * g.c_row + (int64_t)c * 4) = gf32x4{v[0], v[1], v[2], v[3]};
+            } else {
+              *(uint2*)(turn + r32 * (LPR * 16) + (((b * 4 + q) ^ (r32 & (LPR - 1))) * 16) + half * 8) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
+            }
           }
-          *(gf32x4*)(t.pc + r * g.c_row + (int64_t)c * 4) = v;
+        if constexpr (OUT != kElemF32) {
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          const int ch = lane % LPR;
+#pragma unroll
+          for (int k = 0; k < 32 * LPR / 64; ++k) {
+            const int rr = k * (64 / LPR) + lane / LPR;
+            const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
+            if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
+              *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
         }
-    }
-  } else {
-  // 16 bits: each wavefront turns 32 rows at a time around in its part of the ring and stores 16 bytes a lane, rows of 64 NI bytes
-  constexpr int ROW = NI * 64 + 16, LPR = NI * 4;  // bytes of a row in LDS; lanes a row
-  stage_barrier();                                 // the ring's last readers
-  char* mine = lds + w * (kRingBytes / 4);
-#pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int r = wm + i * 32 + r32;
-    const float as = TY == kElemI8 && t.K > 0 && r < t.m_edge ? t.as[r] : 0.f;
-#pragma unroll
-    for (int j = 0; j < NI; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float bs[4] = {0, 0, 0, 0};
-        if (TY == kElemI8) {
-          const int c = wn + j * 32 + 8 * q + 4 * half;
-          if (t.K > 0 && c < t.n_edge) __builtin_memcpy(bs, t.bs + c, 16);
-        }
-        *(uint2*)(mine + r32 * ROW + j * 64 + q * 16 + half * 8) = make_uint2(
-            pack2<OUT>(value(i, j, 4 * q, as, bs), value(i, j, 4 * q + 1, as, bs)), pack2<OUT>(value(i, j, 4 * q + 2, as, bs), value(i, j, 4 * q + 3, as, bs)));
       }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int cc = (lane % LPR) * 8;
-#pragma unroll
-    for (int k = 0; k < 32 * LPR / 64; ++k) {
-      const int rr = k * (64 / LPR) + lane / LPR;
-      const gi32x4 v = *(const gi32x4*)(mine + rr * ROW + cc * 2);
-      if (wm + i * 32 + rr < t.m_edge && wn + cc < t.n_edge) *(gi32x4*)(t.pc + (wm + i * 32 + rr) * g.c_row + (int64_t)(wn + cc) * 2) = v;
+    };
+    if (p.m_edge > 128) {
+      Tile<TY, AX, BX, 4, 4> t;
+      whole(t, (w & 1) * 128, (w >> 1) * 128, Const<4>(), Const<4>());
+    } else if (AX || p.m_edge > 64) {
+      Tile<TY, AX, BX, 2, 4> t;
+      whole(t, (w & 1) * 64, (w >> 1) * 128, Const<2>(), Const<4>());
+    } else if constexpr (!AX) {
+      if (p.m_edge > 32) {
+        Tile<TY, AX, BX, 2, 2> t;
+        whole(t, 0, w * 64, Const<2>(), Const<2>());
+      } else {
+        Tile<TY, AX, BX, 1, 2> t;
+        whole(t, 0, w * 64, Const<1>(), Const<2>());
+      }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
+    p = nxt;
   }
 }
 
@@ -376,31 +407,24 @@ __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
   extern __shared__ __align__(16) char ring[];
   constexpr int EB = GElem<TY>::bytes;
   const int NT = (g.N + kGT - 1) / kGT;
-  int piece;
-  Segment s;
-  if (!find_segment(g.off, g.G, g.R, kGT, NT, [](int n) { return take_piece<false>(n, nullptr, nullptr); }, piece, s)) return;
-  int rt, nt;
-  band_tile(piece - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
-  const int m0 = rt * kGT, n0 = nt * kGT, grp = max(s.group, 0);
-  const int64_t row = s.row0 + m0;
-  TileAt t;
-  t.pa = g.a + row * g.a_row;
-  t.pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * EB : n0 * g.b_row);
-  t.pc = g.c + row * g.c_row + (int64_t)n0 * elem_bytes(OUT);
-  t.as = TY == kElemI8 ? g.a_scale + row : nullptr;
-  t.bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
-  t.m_edge = min(kGT, s.rows - m0);
-  t.n_edge = min(kGT, g.N - n0);
-  t.K = s.group < 0 ? 0 : g.K;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (t.m_edge > 128)
-    do_tile<TY, OUT, false, BX, 4, 4, 4, 4>(g, t, ring, (w & 1) * 128, (w >> 1) * 128);
-  else if (t.m_edge > 64)
-    do_tile<TY, OUT, false, BX, 2, 4, 2, 4>(g, t, ring, (w & 1) * 64, (w >> 1) * 128);
-  else if (t.m_edge > 32)
-    do_tile<TY, OUT, false, BX, 2, 2, 1, 4>(g, t, ring, 0, w * 64);
-  else
-    do_tile<TY, OUT, false, BX, 1, 2, 1, 4>(g, t, ring, 0, w * 64);
+  do_pieces<TY, OUT, false, BX>(g, ring, [&](int i, Piece& p) {
+    int piece;
+    Segment s;
+    if (!find_segment(g.off, g.G, g.R, kGT, NT, [&](int n) { return piece_of(blockIdx.x + i * kWorkgroups, n); }, piece, s)) return false;
+    int rt, nt;
+    band_tile(piece - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
+    const int m0 = rt * kGT, n0 = nt * kGT, grp = max(s.group, 0);
+    const int64_t row = s.row0 + m0;
+    p.pa = g.a + row * g.a_row;
+    p.pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * EB : n0 * g.b_row);
+    p.pc = g.c + row * g.c_row + (int64_t)n0 * elem_bytes(OUT);
+    p.as = TY == kElemI8 ? g.a_scale + row : nullptr;
+    p.bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
+    p.m_edge = min(kGT, s.rows - m0);
+    p.n_edge = min(kGT, g.N - n0);
+    p.K = s.group < 0 ? 0 : g.K;
+    return true;
+  });
 }
 
 // dW = X^T dY
@@ -408,26 +432,23 @@ template <int TY>
 __global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, int pieces) {
   extern __shared__ __align__(16) char ring[];
   const int MT = (g.M + kGT - 1) / kGT, NT = (g.N + kGT - 1) / kGT;
-  const int piece = take_piece<false>(pieces, nullptr, nullptr);
-  if (piece >= pieces) return;
-  const int grp = piece / (MT * NT);
-  int mt, nt, row0, rows;
-  band_tile(piece - grp * MT * NT, MT, NT, mt, nt);
-  group_rows(g.off, g.G, g.R, grp, row0, rows);
-  const int m0 = mt * kGT, n0 = nt * kGT;
-  TileAt t;
-  t.pa = g.a + row0 * g.a_row + (int64_t)m0 * 2;
-  t.pb = g.b + row0 * g.b_row + (int64_t)n0 * 2;
-  t.pc = g.c + grp * g.c_group + m0 * g.c_row + (int64_t)n0 * 2;
-  t.as = t.bs = nullptr;
-  t.m_edge = min(kGT, g.M - m0);
-  t.n_edge = min(kGT, g.N - n0);
-  t.K = rows;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (t.m_edge > 128)
-    do_tile<TY, TY, true, true, 4, 4, 4, 4>(g, t, ring, (w & 1) * 128, (w >> 1) * 128);
-  else
-    do_tile<TY, TY, true, true, 2, 4, 4, 4>(g, t, ring, (w & 1) * 64, (w >> 1) * 128);
+  do_pieces<TY, TY, true, true>(g, ring, [&](int i, Piece& p) {
+    const int piece = piece_of(blockIdx.x + i * kWorkgroups, pieces);
+    if (piece >= pieces) return false;
+    const int grp = piece / (MT * NT);
+    int mt, nt, row0, rows;
+    band_tile(piece - grp * MT * NT, MT, NT, mt, nt);
+    group_rows(g.off, g.G, g.R, grp, row0, rows);
+    const int m0 = mt * kGT, n0 = nt * kGT;
+    p.pa = g.a + row0 * g.a_row + (int64_t)m0 * 2;
+    p.pb = g.b + row0 * g.b_row + (int64_t)n0 * 2;
+    p.pc = g.c + grp * g.c_group + m0 * g.c_row + (int64_t)n0 * 2;
+    p.as = p.bs = nullptr;
+    p.m_edge = min(kGT, g.M - m0);
+    p.n_edge = min(kGT, g.N - n0);
+    p.K = rows;
+    return true;
+  });
 }
 
 template <class K>
@@ -440,8 +461,8 @@ hipError_t launch_rows(const GroupedArgs& g, hipStream_t s) {
   static PerDeviceOnce once;
   const hipError_t e = prepare(grouped_mfma_kernel<TY, OUT, BX>, once);
   if (e != hipSuccess) return e;
-  const int64_t blocks = row_tiles_bound(g.R, g.G, g.off != nullptr, kGT) * ((g.N + kGT - 1) / kGT);
-  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)blocks), dim3(256), kRingBytes, s>>>(g);
+  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kGT) * ((g.N + kGT - 1) / kGT);
+  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(pieces < kWorkgroups ? pieces : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
   return hipGetLastError();
 }
 
@@ -451,7 +472,7 @@ hipError_t launch_dw(const GroupedArgs& g, hipStream_t s) {
   const hipError_t e = prepare(grouped_dw_mfma_kernel<TY>, once);
   if (e != hipSuccess) return e;
   const int pieces = g.G * ((g.M + kGT - 1) / kGT) * ((g.N + kGT - 1) / kGT);
-  grouped_dw_mfma_kernel<TY><<<dim3((unsigned)pieces), dim3(256), kRingBytes, s>>>(g, pieces);
+  grouped_dw_mfma_kernel<TY><<<dim3((unsigned)(pieces < kWorkgroups ? pieces : kWorkgroups)), dim3(256), kRingBytes, s>>>(g, pieces);
   return hipGetLastError();
 }
 

@@ -65,7 +65,8 @@ hipError_t quantize(const Int8Args& a, int8_t* q, int64_t q_row, float* scale, h
   return hipGetLastError();
 }
 
-inline int64_t quantized_row(int K) { return ((int64_t)K + 63) / 64 * 64; }
+// (a stage of the products takes 128 values: zeros to there)
+inline int64_t quantized_row(int K) { return ((int64_t)K + 127) / 128 * 128; }
 inline int64_t scale_offset(int64_t R, int K) { return (R * quantized_row(K) + 255) / 256 * 256; }
 
 }  // namespace

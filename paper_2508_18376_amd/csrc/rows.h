@@ -41,7 +41,7 @@ __device__ __forceinline__ void load8(const void* p, int64_t i, int left, float 
 
 template <int TY>
 __device__ __forceinline__ uint16_t narrow(float v) {
-  return TY == DSMOE_BF16 ? f32_to_bf16(v) : __builtin_bit_cast(uint16_t, (_Float16)v);
+  return TY == DSMOE_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
 template <int TY>
