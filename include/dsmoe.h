@@ -340,14 +340,18 @@ int dsmoe_profile_end(dsmoe_ctx* ctx, float* ms, int* calls);
  *                           rows of no group: zeros
  *   moe_grouped_matmul_dw   dw[g] = sum over the group's rows of x[r]^T dy[r]    x [rows][k], dy [rows][n], dw [groups][k][n];
  *                           a group without rows: zeros
+ * workspace device, 256-byte aligned, of the size that the _workspace_bytes function gives for the same arguments (0: none is needed), or NULL:
+ * calls of few or unevenly many tiles split the sums among more compute units with it.
  * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
  */
 int moe_grouped_matmul(const void* x, int64_t x_stride, const void* w, int64_t w_group_stride, int64_t w_row_stride,
                        const int32_t* offsets, int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t transposed, int32_t dtype,
-                       void* y, int64_t y_stride, void* stream);
+                       void* y, int64_t y_stride, void* workspace, void* stream);
+size_t dsmoe_grouped_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t transposed, int32_t dtype);
 int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offsets, int32_t rows,
                           int32_t groups, int32_t k, int32_t n, int32_t dtype, void* dw, int64_t dw_group_stride, int64_t dw_row_stride,
-                          void* stream);
+                          void* workspace, void* stream);
+size_t dsmoe_grouped_dw_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t dtype);
 
 /*
  * Products in 8-bit integers, with a scale for each token and each output channel: s = max|x[r]| / 127 in fp32, q = x[r] / s rounded to
@@ -355,9 +359,9 @@ int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64
  *   w device int8 [groups][n][k], a row for each output channel; w_scale device float [groups][n] (a group's next to each other);
  *   offsets as above, or NULL for one group of all rows (groups = 1).  k at most 2^17.
  *   A row of zeros gives zeros, a row with a NaN or an infinity NaN in all its outputs, rows of no group zeros.
- *   workspace device, dsmoe_int8_workspace_bytes(rows, k) bytes, 256-byte aligned: the rows in 8 bits and their scales.
+ *   workspace device, dsmoe_int8_workspace_bytes(...) bytes, 256-byte aligned: the rows in 8 bits and their scales, and what splits work.
  */
-size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t k);
+size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n);
 int moe_int8_matmul(const void* x, int64_t x_stride, const int8_t* w, int64_t w_group_stride, int64_t w_row_stride, const float* w_scale,
                     int64_t w_scale_group_stride, const int32_t* offsets, int32_t rows, int32_t groups, int32_t k, int32_t n,
                     int32_t dtype, void* y, int64_t y_stride, void* workspace, void* stream);

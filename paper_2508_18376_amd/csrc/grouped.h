@@ -7,6 +7,10 @@ namespace dsmoe {
 enum ElemType : int32_t { kElemF32 = DSMOE_F32, kElemBF16 = DSMOE_BF16, kElemF16 = DSMOE_F16, kElemI8 = 100 };
 inline __host__ __device__ int elem_bytes(int t) { return t == kElemF32 ? 4 : t == kElemI8 ? 1 : 2; }
 
+struct SplitRoom {
+  int32_t tiles, parts;  // tiles that may be split, and parts of all of them
+};
+
 // One launch of products C_g = A_g B_g.  Rows are the caller's rows (tokens); a group owns rows [off[g], off[g+1]).
 //   over rows      A [R][K] rows of the group, B_g [K][N] (or [N][K], each output column's values together), C [R][N]
 //   over weights   A [R][M], B [R][N], both summed over the group's rows, C_g [M][N]
@@ -21,6 +25,8 @@ struct GroupedArgs {
   const float* b_scale;
   int64_t bs_group;  // ... in values
   int32_t out_type;
+  char* partial;  // workspace for tiles whose contraction is split (grouped_workspace_bytes), or nullptr
+  SplitRoom room;
 };
 
 // Inclusive scans over the 64 lanes (DPP: shifts inside the rows of sixteen, then the last lane of a row to the next ones).
@@ -148,11 +154,22 @@ hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s
 // the fast path of 16-bit types and 8-bit integers, where the operands lie for it
 bool grouped_mfma_fits(const GroupedArgs& g, int type, bool b_along);
 hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
+// workspace that splits work (0: none does); what g's pointers and strides are does not matter
+size_t grouped_split_bytes(const GroupedArgs& g, int type);
+size_t grouped_dw_split_bytes(const GroupedArgs& g);
 bool grouped_dw_mfma_fits(const GroupedArgs& g, int type);
 hipError_t launch_grouped_dw_mfma(const GroupedArgs& g, int type, hipStream_t s);
+// groups of few rows, any alignment
+bool grouped_stream_fits(const GroupedArgs& g, int type, bool b_along);
+hipError_t launch_grouped_stream(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
 inline hipError_t launch_grouped(const GroupedArgs& g, int type, bool b_along, hipStream_t s) {
+  if (grouped_stream_fits(g, type, b_along)) return launch_grouped_stream(g, type, b_along, s);
   return grouped_mfma_fits(g, type, b_along) ? launch_grouped_mfma(g, type, b_along, s) : launch_grouped_plain(g, type, b_along, s);
 }
+inline size_t grouped_workspace_bytes(const GroupedArgs& g, int type, bool b_along) {
+  return type == kElemF32 || g.R == 0 || grouped_stream_fits(g, type, b_along) ? 0 : grouped_split_bytes(g, type);
+}
+inline size_t grouped_dw_workspace_bytes(const GroupedArgs& g, int type) { return type == kElemF32 ? 0 : grouped_dw_split_bytes(g); }
 inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t s) {
   return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
 }

@@ -17,6 +17,8 @@
 // Reads beyond an operand are cut off by the buffer's bounds and give zeros: rows past a tile's last one, columns past the last one, and
 // (where the contraction runs over rows) rows past the group's last one.  Where it does not, chunks past the contraction's end
 // in the last stage get an offset out of bounds.
+#include <math.h>
+
 #include "grouped.h"
 
 namespace dsmoe {
@@ -261,7 +263,74 @@ struct Piece {
   const float *as, *bs;  // 8-bit: factors from the tile's first row and column on
   int m_edge, n_edge;    // rows and columns of the tile that exist
   int K;                 // contraction: values (along A) or rows (across)
+  char* partial;         // where the sums go as they are, if the contraction is split (else nullptr)
 };
+
+// A launch's last, partly filled round of tiles leaves compute units idle for a whole tile's time, and few tiles leave them idle altogether.  So
+// the tiles beyond whole rounds of 256 are split along the contraction into `parts` pieces of work each, whose sums go to a workspace as they
+// are; a second launch adds them up in order and stores C.  A stage of 128 bytes takes about 1.2 us, a partial tile's way out and back about
+// 0.1 us of the whole card's bandwidth, the second launch 5 us: parts is what makes stages / parts * 1.2 + tiles * parts * 0.1 least, if that saves
+// the 5 us.  (8192 rows on 8 experts, y = x W^T with 4096 columns and 14336 values to sum: 576 tiles, the last 64 in 4 parts.)
+struct Split {
+  int whole;  // tiles that are not split
+  int parts;  // of each of the others (1: none is)
+};
+// room: what the workspace and the second launch have room for.  Times are in tenths of a microsecond.
+__host__ __device__ inline Split split_of(int tiles, int stages, const SplitRoom& room) {
+  const int rest = tiles % kWorkgroups;
+  Split s = {tiles, 1};
+  if (rest == 0 || rest > room.tiles) return s;
+  int least = 12 * stages - 50;
+  for (int parts = 2; parts <= 16 && parts * rest <= room.parts && 2 * parts <= stages; ++parts) {
+    const int cost = 12 * stages / parts + rest * parts;
+    if (cost < least) {
+      least = cost;
+      s.whole = tiles - rest;
+      s.parts = parts;
+    }
+  }
+  return s;
+}
+// No more tiles than 2 sqrt(12 stages tiles) < 12 stages - 50 allows, and not many more parts than the least cost has: sqrt(12 stages / tiles).
+inline SplitRoom split_room(int64_t most_tiles, int stages) {
+  if (stages < 9) return SplitRoom{0, 0};
+  const int64_t gain = 12ll * stages - 50;
+  int64_t rest = gain * gain / (48ll * stages);
+  if (rest > kWorkgroups / 2) rest = kWorkgroups / 2;
+  if (rest > most_tiles) rest = most_tiles;
+  int64_t parts = (int64_t)sqrt(12. * stages * rest) + 2 * rest;
+  if (parts > kWorkgroups) parts = kWorkgroups;
+  return SplitRoom{(int)rest, (int)parts};
+}
+constexpr int64_t kPartialBytes = (int64_t)kGT * kGT * 4;
+// the i-th piece of work of workgroup b: its tile and part, false if there is none
+__device__ __forceinline__ bool work_of(const Split& s, int tiles, int b, int i, int& tile, int& part) {
+  const int rest = tiles - s.whole, n = s.whole + rest * s.parts, id = piece_of(b + i * kWorkgroups, n);
+  part = 0;
+  tile = id;
+  if (id >= n) return false;
+  if (id >= s.whole) {  // neighbours have the same part of neighbouring tiles
+    part = (id - s.whole) / rest;
+    tile = id - part * rest;
+  }
+  return true;
+}
+// the part's stretch of the contraction, whole stages of `stage` values
+__device__ __forceinline__ void part_of(const Split& s, int part, int K, int stage, int& first, int& count) {
+  const int n = (K + stage - 1) / stage;
+  first = (int)((int64_t)n * part / s.parts) * stage;
+  const int end = part + 1 == s.parts ? K : (int)((int64_t)n * (part + 1) / s.parts) * stage;
+  count = end > first ? end - first : 0;
+}
+
+// How the four wavefronts share a tile with m_edge rows: MI x NI blocks of 32 x 32 each, from (wm, wn) on.
+__device__ __forceinline__ void tile_shape(int m_edge, bool across, int w, int& mi, int& ni, int& wm, int& wn) {
+  const bool tall = across || m_edge > 64;
+  mi = m_edge > 128 ? 4 : tall || m_edge > 32 ? 2 : 1;
+  ni = tall ? 4 : 2;
+  wm = tall ? (w & 1) * 32 * mi : 0;
+  wn = tall ? (w >> 1) * 128 : w * 64;
+}
 
 // The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
 // While a tile's values leave through the fifth unit of the ring, the next tile's first four units are under way.
@@ -334,6 +403,22 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       tile.run(n, load_a, load_b, one_a, one_b);
       stage_barrier();
       if (more) first_units(nxt);
+      if (p.partial != nullptr) {  // in the order of the registers: the second launch knows where they belong
+        char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
+#pragma unroll
+        for (int a = 0; a < MI; ++a)
+#pragma unroll
+          for (int b = 0; b < NI; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              typedef typename AccType<TY>::type acc_t;
+              const acc_t& c = tile.acc[a][b];
+              typedef decltype(c[0] + c[0]) value_t;
+              typedef value_t value4 __attribute__((ext_vector_type(4)));
+              *(value4*)(to + ((a * NI + b) * 4 + q) * 1024) = value4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+            }
+        return;
+      }
       // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
       const int r32 = lane & 31, half = lane >> 5;
       auto value = [&](int a, int b, int v, float as, const float* bs) __attribute__((always_inline)) -> float {
@@ -382,19 +467,21 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
         }
       }
     };
-    if (p.m_edge > 128) {
+    int mi, ni, wm, wn;
+    tile_shape(p.m_edge, AX, w, mi, ni, wm, wn);
+    if (mi == 4) {
       Tile<TY, AX, BX, 4, 4> t;
-      whole(t, (w & 1) * 128, (w >> 1) * 128, Const<4>(), Const<4>());
-    } else if (AX || p.m_edge > 64) {
+      whole(t, wm, wn, Const<4>(), Const<4>());
+    } else if (ni == 4) {
       Tile<TY, AX, BX, 2, 4> t;
-      whole(t, (w & 1) * 64, (w >> 1) * 128, Const<2>(), Const<4>());
+      whole(t, wm, wn, Const<2>(), Const<4>());
     } else if constexpr (!AX) {
-      if (p.m_edge > 32) {
+      if (mi == 2) {
         Tile<TY, AX, BX, 2, 2> t;
-        whole(t, 0, w * 64, Const<2>(), Const<2>());
+        whole(t, wm, wn, Const<2>(), Const<2>());
       } else {
         Tile<TY, AX, BX, 1, 2> t;
-        whole(t, 0, w * 64, Const<1>(), Const<2>());
+        whole(t, wm, wn, Const<1>(), Const<2>());
       }
     }
     p = nxt;
@@ -403,16 +490,24 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
 
 // y = x W (BX) or x W^T (B along), and the 8-bit products
 template <int TY, int OUT, bool BX>
-__global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
-  extern __shared__ __align__(16) char ring[];
-  constexpr int EB = GElem<TY>::bytes;
-  const int NT = (g.N + kGT - 1) / kGT;
-  do_pieces<TY, OUT, false, BX>(g, ring, [&](int i, Piece& p) {
-    int piece;
+struct RowsWork {
+  static constexpr int EB = GElem<TY>::bytes, STAGE = 128 / EB;
+  int tiles, part;
+  Split split;
+  // the piece that pick(tiles) names, if there is one
+  template <class Pick>
+  __device__ __forceinline__ bool find(const GroupedArgs& g, Piece& p, Pick&& pick) {
+    const int NT = (g.N + kGT - 1) / kGT;
+    int tile;
     Segment s;
-    if (!find_segment(g.off, g.G, g.R, kGT, NT, [&](int n) { return piece_of(blockIdx.x + i * kWorkgroups, n); }, piece, s)) return false;
+    auto pick_tile = [&](int n) {
+      tiles = n;
+      split = split_of(n, (g.K + STAGE - 1) / STAGE, g.room);
+      return pick(*this);
+    };
+    if (!find_segment(g.off, g.G, g.R, kGT, NT, pick_tile, tile, s)) return false;
     int rt, nt;
-    band_tile(piece - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
+    band_tile(tile - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
     const int m0 = rt * kGT, n0 = nt * kGT, grp = max(s.group, 0);
     const int64_t row = s.row0 + m0;
     p.pa = g.a + row * g.a_row;
@@ -423,32 +518,118 @@ __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
     p.m_edge = min(kGT, s.rows - m0);
     p.n_edge = min(kGT, g.N - n0);
     p.K = s.group < 0 ? 0 : g.K;
+    p.partial = nullptr;
+    if (tile >= split.whole) {
+      p.partial = g.partial + ((tile - split.whole) * split.parts + part) * kPartialBytes;
+      int first;
+      part_of(split, part, p.K, STAGE, first, p.K);
+      p.pa += (int64_t)first * EB;
+      p.pb += BX ? first * g.b_row : (int64_t)first * EB;
+    }
     return true;
+  }
+};
+
+template <int TY, int OUT, bool BX>
+__global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
+  extern __shared__ __align__(16) char ring[];
+  do_pieces<TY, OUT, false, BX>(g, ring, [&](int i, Piece& p) {
+    RowsWork<TY, OUT, BX> work;
+    return work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) {
+      int tile;
+      return work_of(w.split, w.tiles, blockIdx.x, i, tile, w.part) ? tile : w.tiles;
+    });
   });
 }
 
-// dW = X^T dY
+// dW = X^T dY.  The groups' rows differ; what is split is split for all of them alike.
 template <int TY>
-__global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, int pieces) {
-  extern __shared__ __align__(16) char ring[];
-  const int MT = (g.M + kGT - 1) / kGT, NT = (g.N + kGT - 1) / kGT;
-  do_pieces<TY, TY, true, true>(g, ring, [&](int i, Piece& p) {
-    const int piece = piece_of(blockIdx.x + i * kWorkgroups, pieces);
-    if (piece >= pieces) return false;
-    const int grp = piece / (MT * NT);
+struct DwWork {
+  __device__ __forceinline__ static void find(const GroupedArgs& g, const Split& split, int tile, int part, Piece& p) {
+    const int MT = (g.M + kGT - 1) / kGT, NT = (g.N + kGT - 1) / kGT, grp = tile / (MT * NT);
     int mt, nt, row0, rows;
-    band_tile(piece - grp * MT * NT, MT, NT, mt, nt);
+    band_tile(tile - grp * MT * NT, MT, NT, mt, nt);
     group_rows(g.off, g.G, g.R, grp, row0, rows);
     const int m0 = mt * kGT, n0 = nt * kGT;
+    p.K = rows;
+    p.partial = nullptr;
+    if (tile >= split.whole) {
+      p.partial = g.partial + ((tile - split.whole) * split.parts + part) * kPartialBytes;
+      int first;
+      part_of(split, part, rows, 64, first, p.K);
+      row0 += first;
+    }
     p.pa = g.a + row0 * g.a_row + (int64_t)m0 * 2;
     p.pb = g.b + row0 * g.b_row + (int64_t)n0 * 2;
     p.pc = g.c + grp * g.c_group + m0 * g.c_row + (int64_t)n0 * 2;
     p.as = p.bs = nullptr;
     p.m_edge = min(kGT, g.M - m0);
     p.n_edge = min(kGT, g.N - n0);
-    p.K = rows;
+  }
+};
+
+template <int TY>
+__global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, int tiles, Split split) {
+  extern __shared__ __align__(16) char ring[];
+  do_pieces<TY, TY, true, true>(g, ring, [&](int i, Piece& p) {
+    int tile, part;
+    if (!work_of(split, tiles, blockIdx.x, i, tile, part)) return false;
+    DwWork<TY>::find(g, split, tile, part, p);
     return true;
   });
+}
+
+// Adds up the parts of the split tiles, in order: a wavefront for each block of 32 x 32 (blockIdx.x: the tile; blockIdx.y: sixteenths of its blocks).
+template <int TY, int OUT, bool AX, bool BX>
+__global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, int dw_tiles, Split dw_split) {
+  typedef typename AccType<TY>::type acc_t;
+  typedef decltype(acc_t{}[0] + acc_t{}[0]) value_t;
+  typedef value_t value4 __attribute__((ext_vector_type(4)));
+  Piece p;
+  Split split = dw_split;
+  int tile;
+  if constexpr (AX) {
+    tile = split.whole + blockIdx.x;
+    if (tile >= dw_tiles) return;
+    DwWork<TY>::find(g, split, tile, 0, p);
+  } else {
+    RowsWork<TY, OUT, BX> work;
+    work.part = 0;
+    if (!work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) { return w.split.whole + (int)blockIdx.x; })) return;
+    split = work.split;
+    tile = split.whole + blockIdx.x;
+  }
+  const int lane = threadIdx.x & 63, block = blockIdx.y * 4 + (threadIdx.x >> 6);
+  int mi, ni, wm, wn;
+  tile_shape(p.m_edge, AX, 0, mi, ni, wm, wn);
+  if (block >= 4 * mi * ni) return;
+  tile_shape(p.m_edge, AX, block / (mi * ni), mi, ni, wm, wn);
+  const int ab = block % (mi * ni), r = wm + ab / ni * 32 + (lane & 31);
+  const char* from = p.partial + block * 4096 + lane * 16;
+  value4 v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = *(const value4*)(from + q * 1024);
+  for (int s = 1; s < split.parts; ++s) {
+    from += kPartialBytes;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] += *(const value4*)(from + q * 1024);
+  }
+  if (r >= p.m_edge) return;
+  const float as = TY == kElemI8 ? p.as[r] : 1.f;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int c = wn + ab % ni * 32 + 8 * q + 4 * (lane >> 5);
+    if (c >= p.n_edge) continue;
+    float f[4], bs[4] = {1, 1, 1, 1};
+    if (TY == kElemI8) __builtin_memcpy(bs, p.bs + c, 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = TY == kElemI8 ? (float)v[q][e] * as * bs[e] : (float)v[q][e];
+    char* to = p.pc + r * g.c_row + (int64_t)c * elem_bytes(OUT);
+    if constexpr (OUT == kElemF32)
+      *(gf32x4*)to = gf32x4{f[0], f[1], f[2], f[3]};
+    else
+      *(uint2*)to = make_uint2(pack2<OUT>(f[0], f[1]), pack2<OUT>(f[2], f[3]));
+  }
 }
 
 template <class K>
@@ -456,23 +637,37 @@ hipError_t prepare(K kernel, PerDeviceOnce& once) {
   return once.run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kRingBytes); });
 }
 
+inline int row_stages(const GroupedArgs& g, int type) { return (int)(((int64_t)g.K * elem_bytes(type) + 127) / 128); }
+inline int64_t most_tiles(const GroupedArgs& g) { return row_tiles_bound(g.R, g.G, g.off != nullptr, kGT) * ((g.N + kGT - 1) / kGT); }
+inline int dw_tiles(const GroupedArgs& g) { return g.G * ((g.M + kGT - 1) / kGT) * ((g.N + kGT - 1) / kGT); }
+inline int dw_stages(const GroupedArgs& g) { return (g.R / g.G + 63) / 64; }  // (groups differ: the mean decides)
+
 template <int TY, int OUT, bool BX>
-hipError_t launch_rows(const GroupedArgs& g, hipStream_t s) {
+hipError_t launch_rows(GroupedArgs g, hipStream_t s) {
   static PerDeviceOnce once;
-  const hipError_t e = prepare(grouped_mfma_kernel<TY, OUT, BX>, once);
+  hipError_t e = prepare(grouped_mfma_kernel<TY, OUT, BX>, once);
   if (e != hipSuccess) return e;
-  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kGT) * ((g.N + kGT - 1) / kGT);
-  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(pieces < kWorkgroups ? pieces : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
+  const int64_t tiles = most_tiles(g);
+  if (g.partial != nullptr) g.room = split_room(tiles, row_stages(g, TY));
+  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(g.room.tiles == 0 && tiles < kWorkgroups ? tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
+  e = hipGetLastError();
+  if (e != hipSuccess || g.room.tiles == 0) return e;
+  grouped_join_kernel<TY, OUT, false, BX><<<dim3(g.room.tiles, 16), dim3(256), 0, s>>>(g, 0, Split{0, 1});
   return hipGetLastError();
 }
 
 template <int TY>
 hipError_t launch_dw(const GroupedArgs& g, hipStream_t s) {
   static PerDeviceOnce once;
-  const hipError_t e = prepare(grouped_dw_mfma_kernel<TY>, once);
+  hipError_t e = prepare(grouped_dw_mfma_kernel<TY>, once);
   if (e != hipSuccess) return e;
-  const int pieces = g.G * ((g.M + kGT - 1) / kGT) * ((g.N + kGT - 1) / kGT);
-  grouped_dw_mfma_kernel<TY><<<dim3((unsigned)(pieces < kWorkgroups ? pieces : kWorkgroups)), dim3(256), kRingBytes, s>>>(g, pieces);
+  const int tiles = dw_tiles(g);
+  const Split split = split_of(tiles, dw_stages(g), g.partial != nullptr ? split_room(tiles, dw_stages(g)) : SplitRoom{0, 0});
+  const int pieces = split.whole + (tiles - split.whole) * split.parts;
+  grouped_dw_mfma_kernel<TY><<<dim3(pieces < kWorkgroups ? pieces : kWorkgroups), dim3(256), kRingBytes, s>>>(g, tiles, split);
+  e = hipGetLastError();
+  if (e != hipSuccess || split.whole == tiles) return e;
+  grouped_join_kernel<TY, TY, true, true><<<dim3(tiles - split.whole, 16), dim3(256), 0, s>>>(g, tiles, split);
   return hipGetLastError();
 }
 
@@ -495,6 +690,12 @@ hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hip
                                      : launch_rows<kElemI8, kElemF16, false>(g, s);
   if (type == kElemBF16) return b_along ? launch_rows<kElemBF16, kElemBF16, false>(g, s) : launch_rows<kElemBF16, kElemBF16, true>(g, s);
   return b_along ? launch_rows<kElemF16, kElemF16, false>(g, s) : launch_rows<kElemF16, kElemF16, true>(g, s);
+}
+
+size_t grouped_split_bytes(const GroupedArgs& g, int type) { return (size_t)(split_room(most_tiles(g), row_stages(g, type)).parts * kPartialBytes); }
+size_t grouped_dw_split_bytes(const GroupedArgs& g) {
+  const Split s = split_of(dw_tiles(g), dw_stages(g), split_room(dw_tiles(g), dw_stages(g)));
+  return (size_t)((s.parts > 1 ? dw_tiles(g) - s.whole : 0) * s.parts * kPartialBytes);
 }
 
 bool grouped_dw_mfma_fits(const GroupedArgs& g, int type) {

@@ -1,0 +1,344 @@
+// Products over groups of few rows (decode steps, short prompts): the weights' stream is all there is, so this path loads each weight
+// once, straight into registers, with as many loads under way as fit, and does the rest in the shadow of that.
+//
+// A workgroup of 8 or 16 wavefronts takes 64 columns of C for up to 32 rows of a group.  The wavefronts deal the contraction out among
+// themselves in steps of 32 values (8-bit: 64) and add their sums up through LDS at the end.  Products are 16 x 16 matrix instructions with the
+// weights as the first operand:
+//   along   (the weights of a column follow each other along the contraction: gradients of x, 8 bits) a lane's 16 bytes of a column are
+//           what the instruction takes
+//   across  (y = x W) lane i of sixteen loads columns 4 i .. 4 i + 3 of eight contraction rows; instruction j takes the j-th of the four
+//           columns from each lane, i.e. columns j, 4 + j, 8 + j ..: the turning around is one byte permutation for two values
+// Both operands may start on any value.  Rows past the last one are the last one again (their sums are not stored).
+#include "grouped.h"
+
+namespace dsmoe {
+
+namespace {
+
+typedef __bf16 sbf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 sf16x8 __attribute__((ext_vector_type(8)));
+typedef int si32x4 __attribute__((ext_vector_type(4)));
+typedef float sf32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kStreamTile = 32;  // rows of a workgroup
+// a row of sums in LDS, for J x 16 columns: the four extra ones keep sixteen rows out of each other's banks
+constexpr int row_floats(int J) { return 16 * J + 4; }
+
+constexpr int kWordsAhead = 76;  // registers of a lane for the loads under way
+
+// A step is 32 values of the contraction across, and 128 bytes of it along: whole lines.
+template <int TY, bool BX>
+struct SElem {
+  static constexpr int bytes = TY == kElemF32 ? 4 : TY == kElemI8 ? 1 : 2;
+  static constexpr int parts = BX || TY == kElemF32 ? 1 : 2;              // matrix instructions a step (fp32: 8, of one part)
+  static constexpr int step = parts * (TY == kElemI8 ? 64 : 32);          // values a step
+  static constexpr int lane = step / 4 / parts;                           // ... of a lane and part, one after the other in memory
+  static constexpr int words = lane * bytes / 4, lane_words = parts * words;  // 32-bit words of these
+};
+template <int TY>
+struct SAcc {
+  typedef sf32x4 type;
+};
+template <>
+struct SAcc<kElemI8> {
+  typedef si32x4 type;
+};
+
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
+
+// W words from p, of which `left` values of SZ bytes exist (zeros behind them)
+template <int W, int SZ, bool GUARD, bool ONCE>
+__device__ __forceinline__ void load_words(uint32_t* v, const char* p, int left) {
+  typedef uint32_t words_t __attribute__((ext_vector_type(W < 4 ? W : 4), aligned(1)));
+  if (!GUARD || left >= W * 4 / SZ) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const words_t x = ONCE ? __builtin_nontemporal_load((const words_t*)(p + 4 * i)) : *(const words_t*)(p + 4 * i);
+      __builtin_memcpy(v + i, &x, sizeof(x));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    v[i] = 0;
+#pragma unroll
+    for (int b = 0; b < 4 / SZ; ++b) {
+      const int e = i * (4 / SZ) + b;
+      if (e < left) {
+        uint32_t x;
+        if (SZ == 4) x = *(const uint32_t*)(p + 4 * e);
+        if (SZ == 2) x = *(const uint16_t*)(p + 2 * e);
+        if (SZ == 1) x = *(const uint8_t*)(p + e);
+        v[i] |= x << (8 * SZ * b);
+      }
+    }
+  }
+}
+
+// What a lane holds of one step: the weights as they lie in memory, and its part of NR x 16 rows of A.
+template <int TY, bool BX, int NR, int J>
+struct Step {
+  using E = SElem<TY, BX>;
+  // along: J columns' chunks; across: 8 contraction rows of J columns
+  static constexpr int RW = J * E::bytes / 4, WW = BX ? 8 * RW : J * E::lane_words;
+  uint32_t w[WW], a[NR][E::lane_words];
+};
+
+template <int TY, bool BX, int NR, int J, int W, bool ONCE>
+__device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, const char* pa, const char* pb, int rows, int cols, int K,
+                                            typename SAcc<TY>::type (&acc)[NR][J]) {
+  using E = SElem<TY, BX>;
+  using S = Step<TY, BX, NR, J>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+  // offsets from bases that are the same for the whole wavefront (the launch checks that they fit)
+  uint32_t a_at[NR], b_at[BX ? 1 : J];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) a_at[r] = (uint32_t)min(r * 16 + i, rows - 1) * (uint32_t)g.a_row + q * (E::lane * E::bytes);
+#pragma unroll
+  for (int j = 0; j < (BX ? 1 : J); ++j)
+    b_at[j] = BX ? (uint32_t)(q * 8) * (uint32_t)g.b_row + i * (J * E::bytes) : (uint32_t)min(16 * j + i, cols - 1) * (uint32_t)g.b_row + q * (E::lane * E::bytes);
+
+  auto load = [&](S& s, int step, auto guard) __attribute__((always_inline)) {
+    constexpr bool GUARD = decltype(guard)::value;
+    const int k0 = step * E::step;
+    const int left = K - k0 - q * E::lane;  // values of the contraction from the lane's first on
+    if (BX) {
+      const char* p = pb + k0 * g.b_row;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        load_words<S::RW, E::bytes, GUARD, ONCE>(s.w + e * S::RW, p + b_at[0], e < left ? cols - J * i : 0);
+        p += g.b_row;
+      }
+    } else {
+      const char* p = pb + (int64_t)k0 * E::bytes;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int h = 0; h < E::parts; ++h)
+          load_words<E::words, E::bytes, GUARD, ONCE>(s.w + j * E::lane_words + h * E::words, p + b_at[j] + h * 64, left - h * (E::step / 2));
+    }
+    const char* p = pa + (int64_t)k0 * E::bytes;
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int h = 0; h < E::parts; ++h) load_words<E::words, E::bytes, GUARD, false>(s.a[r] + h * E::words, p + a_at[r] + h * 64, left - h * (E::step / 2));
+  };
+  auto multiply = [&](const S& s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if constexpr (TY == kElemF32) {
+        // 8 instructions of 4 contraction values, each lane's e-th
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(BX ? s.w[e * S::RW + j] : s.w[j * 8 + e]), __uint_as_float(s.a[r][e]), acc[r][j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int h = 0; h < E::parts; ++h) {
+          si32x4 f;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            f[d] = BX ? (int)__builtin_amdgcn_perm(s.w[(2 * d + 1) * S::RW + (j >> 1)], s.w[2 * d * S::RW + (j >> 1)], j & 1 ? 0x07060302u : 0x05040100u)
+                      : (int)s.w[j * E::lane_words + h * 4 + d];
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const si32x4 x = {(int)s.a[r][h * 4], (int)s.a[r][h * 4 + 1], (int)s.a[r][h * 4 + 2], (int)s.a[r][h * 4 + 3]};
+            if constexpr (TY == kElemBF16)
+              acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(sbf16x8, f), __builtin_bit_cast(sbf16x8, x), acc[r][j], 0, 0, 0);
+            if constexpr (TY == kElemF16)
+              acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(sf16x8, f), __builtin_bit_cast(sf16x8, x), acc[r][j], 0, 0, 0);
+            if constexpr (TY == kElemI8) acc[r][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f, x, acc[r][j], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+  const int whole = K / E::step;
+  if (!BX || cols == 16 * J) {
+    // the wavefronts deal the steps out among themselves, DEPTH of each under way
+    constexpr int DEPTH = kWordsAhead * (J / 4) / (S::WW + NR * E::lane_words) > 1 ? kWordsAhead * (J / 4) / (S::WW + NR * E::lane_words) : 1;
+    const int n = whole > wave ? (whole - wave + W - 1) / W : 0;
+    S s[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (d < n) load(s[d], wave + d * W, No());
+    int t = 0;
+    for (; t + 2 * DEPTH <= n; t += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        multiply(s[d]);
+        load(s[d], wave + (t + DEPTH + d) * W, No());
+      }
+    }
+    for (; t < n; t += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        if (t + d < n) {
+          multiply(s[d]);
+          if (t + DEPTH + d < n) load(s[d], wave + (t + DEPTH + d) * W, No());
+        }
+      }
+    }
+    if (K % E::step != 0 && wave == W - 1) {
+      S s1;
+      load(s1, whole, Yes());
+      multiply(s1);
+    }
+  } else {
+    for (int t = wave; t * E::step < K; t += W) {  // columns past the last one: value by value
+      S s1;
+      load(s1, t, Yes());
+      multiply(s1);
+    }
+  }
+}
+
+template <int TY, int OUT, bool BX, int NR, int J, int W, bool ONCE>
+__device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, const char* pa, const char* pb, char* pc, const float* as,
+                                            const float* bs, int rows, int cols, int K) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+  typedef typename SAcc<TY>::type acc_t;
+  acc_t acc[NR][J];
+#pragma unroll
+  for (int r = 0; r < NR; ++r)
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[r][j] = acc_t{0, 0, 0, 0};
+  if (K > 0) stream_tile<TY, BX, NR, J, W, ONCE>(g, (float*)lds, pa, pb, rows, cols, K, acc);
+  // A lane's sums: row lane % 16 of sixteen; along: columns 16 j + 4 q .. + 3 from acc[.][j]; across: columns J (4 q + v) + j from acc[.][j][v].
+  typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+  constexpr int COLS = 16 * J, RF = row_floats(J);
+  uint32_t* mine = (uint32_t*)lds + wave * (16 * RF);
+  constexpr int OB = OUT == kElemF32 ? 4 : 2, PT = 16 * COLS / (64 * W);  // outputs a thread
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    if (r > 0) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      word4 v;  // j-th of the lane's quadruples of columns
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int ja = BX ? j % (J / 4) * 4 + e : j, va = BX ? j / (J / 4) : e;
+        if constexpr (TY == kElemI8)
+          v[e] = (uint32_t)acc[r][ja][va];
+        else
+          v[e] = __float_as_uint(acc[r][ja][va]);
+      }
+      *(word4*)(mine + i * RF + (BX ? J * (4 * q + j / (J / 4)) + j % (J / 4) * 4 : 16 * j + 4 * q)) = v;
+    }
+    __syncthreads();
+    const int o = threadIdx.x * PT, row = o / COLS, col = o % COLS, rr = r * 16 + row;
+    float out[PT];
+#pragma unroll
+    for (int p = 0; p < PT; ++p) {
+      const uint32_t* at = (const uint32_t*)lds + row * RF + col + p;
+      if constexpr (TY == kElemI8) {
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) sum += (int)at[w * (16 * RF)];
+        out[p] = K > 0 && rr < rows && col + p < cols ? (float)sum * as[rr] * bs[col + p] : 0.f;
+      } else {
+        out[p] = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) out[p] += __uint_as_float(at[w * (16 * RF)]);
+      }
+    }
+    if (rr < rows) {
+      char* c = pc + rr * g.c_row + (int64_t)col * OB;
+#pragma unroll
+      for (int p = 0; p < PT; ++p)
+        if (col + p < cols) {
+          if (OUT == kElemF32)
+            ((float*)c)[p] = out[p];
+          else
+            ((uint16_t*)c)[p] = f32_to_16(out[p], OUT);
+        }
+    }
+  }
+}
+
+template <int TY, int OUT, bool BX, int J, int W, bool ONCE>
+__global__ __launch_bounds__(64 * W, J == 8 ? 2 : 4) void grouped_stream_kernel(GroupedArgs g) {
+  extern __shared__ __align__(16) char lds[];
+  using E = SElem<TY, BX>;
+  constexpr int COLS = 16 * J;
+  const int NT = (g.N + COLS - 1) / COLS;
+  int piece;
+  Segment s;
+  if (!find_segment(g.off, g.G, g.R, kStreamTile, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
+  int rt, nt;
+  band_tile(piece - s.base, (s.rows + kStreamTile - 1) / kStreamTile, NT, rt, nt);
+  const int m0 = rt * kStreamTile, n0 = nt * COLS, grp = max(s.group, 0);
+  const int64_t row = s.row0 + m0;
+  const char* pa = g.a + row * g.a_row;
+  const char* pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * E::bytes : n0 * g.b_row);
+  char* pc = g.c + row * g.c_row + (int64_t)n0 * (OUT == kElemF32 ? 4 : 2);
+  const float* as = TY == kElemI8 ? g.a_scale + row : nullptr;
+  const float* bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
+  const int rows = min(kStreamTile, s.rows - m0), cols = min(COLS, g.N - n0), K = s.group < 0 ? 0 : g.K;
+  if (rows <= 16)
+    stream_rows<TY, OUT, BX, 1, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, cols, K);
+  else
+    stream_rows<TY, OUT, BX, 2, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, cols, K);
+}
+
+template <int TY, int OUT, bool BX, int J, int W, bool ONCE>
+hipError_t launch(const GroupedArgs& g, hipStream_t s) {
+  constexpr int bytes = W * 16 * row_floats(J) * 4;
+  if (bytes > 64 * 1024) {
+    static PerDeviceOnce once;
+    const hipError_t e =
+        once.run([] { return hipFuncSetAttribute((const void*)grouped_stream_kernel<TY, OUT, BX, J, W, ONCE>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    if (e != hipSuccess) return e;
+  }
+  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 16 * J - 1) / (16 * J));
+  grouped_stream_kernel<TY, OUT, BX, J, W, ONCE><<<dim3((unsigned)pieces), dim3(64 * W), bytes, s>>>(g);
+  return hipGetLastError();
+}
+
+// The weights that a call can touch against the last-level cache (256 MiB): those that do not fit are loaded past it.
+// 64 tokens on 8 experts of 4096 x 14336 (0.94 GB) 179 -> 167 us; one token on 64 experts of 2048 x 1024 (34 MB, again and again) would lose, 9.8 ->
+// 12.4, as would 333 on 64 of 2048 x 1408 in 8 bits.
+constexpr int64_t kLastLevelBytes = 256ll << 20;
+// Few pieces: 16 wavefronts to each, so that all of the weights are under way at once (one token on 64 experts of 2048 x 1024, 128 pieces:
+// 9.8 us).  Many: whole 256-byte rows of 128 columns across the contraction, in workgroups of 4 wavefronts of which two share a
+// compute unit, so that one's beginning and end lie in the other's stream (64 tokens on 8 of 4096 x 14336: 8 wavefronts 171, 4 167; 64
+// columns 176).
+template <int TY, int OUT, bool BX>
+hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
+  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
+  if (pieces < 512) return launch<TY, OUT, BX, 4, 16, false>(g, s);
+  constexpr bool WIDE = BX && TY != kElemF32;
+  const bool once = (int64_t)(g.G < g.R ? g.G : g.R) * g.K * g.N * SElem<TY, BX>::bytes > kLastLevelBytes;
+  return once ? launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, true>(g, s) : launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, false>(g, s);
+}
+
+}  // namespace
+
+// Up to 16 rows a group on average (8 where 16-bit weights lie along the contraction): beyond that the tiles of grouped_mfma.hip, which read weights
+// through LDS, are as fast.  Forward, streams -> tiles, us: 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 37 / 57 / 68 -> 44 / 54 / 54, 8 of
+// 4096 x 14336 at 4 / 16 / 24 rows 133 / 163 / 196 -> 171 / 182 / 184, 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 61 / 77 -> 85 / 86 / 88;
+// gradient of x 32 / 53 / 64 -> 41 / 52 / 53, 177 / 210 / 300 -> 250 / 263 / 264, 79 / 84 / 116 -> 70 / 72 / 76; 8 bits 23 / 32 / 41 -> 23 / 31 / 33,
+// 83 / 104 / 133 -> 105 / 116 / 118, 44 / 48 / 61 -> 55 / 58 / 62.
+bool grouped_stream_fits(const GroupedArgs& g, int type, bool b_along) {
+  const int64_t most = (int64_t)1 << 24;  // 64 rows of it are below 2^32
+  return g.R <= (b_along && type != kElemI8 && type != kElemF32 ? 8 : 16) * (int64_t)g.G && g.a_row <= most && g.b_row <= most;
+}
+hipError_t launch_grouped_stream(const GroupedArgs& g, int type, bool b_along, hipStream_t s) {
+  switch (type) {
+    case kElemF32: return b_along ? launch_w<kElemF32, kElemF32, false>(g, s) : launch_w<kElemF32, kElemF32, true>(g, s);
+    case kElemBF16: return b_along ? launch_w<kElemBF16, kElemBF16, false>(g, s) : launch_w<kElemBF16, kElemBF16, true>(g, s);
+    case kElemF16: return b_along ? launch_w<kElemF16, kElemF16, false>(g, s) : launch_w<kElemF16, kElemF16, true>(g, s);
+    default:
+      return g.out_type == kElemF32    ? launch_w<kElemI8, kElemF32, false>(g, s)
+             : g.out_type == kElemBF16 ? launch_w<kElemI8, kElemBF16, false>(g, s)
+                                       : launch_w<kElemI8, kElemF16, false>(g, s);
+  }
+}
+
+}  // namespace dsmoe

@@ -18,7 +18,7 @@ struct Int8Args {
   char* workspace;
 };
 
-size_t int8_workspace_bytes(int64_t R, int K);
+size_t int8_workspace_bytes(int R, int G, int K, int N);
 hipError_t launch_int8_matmul(const Int8Args& a, hipStream_t s);
 
 }  // namespace dsmoe

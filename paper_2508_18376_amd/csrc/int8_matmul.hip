@@ -71,7 +71,18 @@ inline int64_t scale_offset(int64_t R, int K) { return (R * quantized_row(K) + 2
 
 }  // namespace
 
-size_t int8_workspace_bytes(int64_t R, int K) { return (size_t)(scale_offset(R, K) + R * 4); }
+inline int64_t partial_offset(int64_t R, int K) { return (scale_offset(R, K) + R * 4 + 255) / 256 * 256; }
+
+size_t int8_workspace_bytes(int R, int G, int K, int N) {
+  static const int32_t some = 0;
+  GroupedArgs g = {};
+  g.off = &some;
+  g.R = R;
+  g.G = G;
+  g.K = K;
+  g.N = N;
+  return (size_t)partial_offset(R, K) + grouped_workspace_bytes(g, kElemI8, true);
+}
 
 hipError_t launch_int8_matmul(const Int8Args& a, hipStream_t s) {
   if (a.R == 0) return hipSuccess;
@@ -99,6 +110,7 @@ hipError_t launch_int8_matmul(const Int8Args& a, hipStream_t s) {
   g.b_scale = a.w_scale;
   g.bs_group = a.ws_group;
   g.out_type = a.type;
+  g.partial = a.workspace + partial_offset(a.R, a.K);
   return launch_grouped(g, kElemI8, true, s);
 }
 

@@ -33,6 +33,18 @@ inline bool sizes_ok(int64_t rows, int64_t groups, int64_t k, int64_t n) {
   return rows >= 0 && rows <= kMostRows && groups >= 1 && groups <= kMostGroups && width_ok(k) && width_ok(n);
 }
 
+// as far as the workspaces' sizes go
+GroupedArgs sizes_of(int rows, int groups, int K, int N) {
+  static const int32_t some = 0;
+  GroupedArgs g = {};
+  g.off = &some;
+  g.R = rows;
+  g.G = groups;
+  g.M = g.K = K;
+  g.N = N;
+  return g;
+}
+
 bool norm_args_ok(const dsmoe_block_norm_args* a) {
   return a && a->tokens >= 0 && a->tokens <= kMostRows && width_ok(a->d) && float_type(a->dtype) && a->gate_kind >= 0 && a->gate_kind <= 3 &&
          a->eps >= 0.f && in_stride(a->x_stride) && in_stride(a->branch_stride) && in_stride(a->gate_stride);
@@ -64,11 +76,11 @@ extern "C" {
 
 int moe_grouped_matmul(const void* x, int64_t x_stride, const void* w, int64_t w_group_stride, int64_t w_row_stride,
                        const int32_t* offsets, int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t transposed, int32_t dtype,
-                       void* y, int64_t y_stride, void* stream) {
+                       void* y, int64_t y_stride, void* workspace, void* stream) {
   if (!sizes_ok(rows, groups, k, n) || !float_type(dtype) || transposed < 0 || transposed > 1) return DSMOE_EINVAL;
   if (!in_stride(x_stride) || !in_stride(w_group_stride) || !in_stride(w_row_stride) || !out_stride(y_stride, transposed ? k : n)) return DSMOE_EINVAL;
   if (rows == 0) return DSMOE_OK;
-  if (!x || !w || !offsets || !y || !aligned_to(x, dtype) || !aligned_to(w, dtype) || !aligned_to(y, dtype)) return DSMOE_EINVAL;
+  if (!x || !w || !offsets || !y || !aligned_to(x, dtype) || !aligned_to(w, dtype) || !aligned_to(y, dtype) || ((uintptr_t)workspace & 255) != 0) return DSMOE_EINVAL;
   if (row_tiles_bound(rows, groups, true, 128) * tiles(transposed ? k : n, 128) > kMostPieces) return DSMOE_EINVAL;
   const int64_t e = elem_bytes(dtype);
   GroupedArgs g = {};
@@ -84,13 +96,24 @@ int moe_grouped_matmul(const void* x, int64_t x_stride, const void* w, int64_t w
   g.G = groups;
   g.N = transposed ? k : n;
   g.K = transposed ? n : k;
+  g.partial = (char*)workspace;
   return status(launch_grouped(g, dtype, transposed != 0, (hipStream_t)stream));
+}
+
+size_t dsmoe_grouped_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t transposed, int32_t dtype) {
+  if (!sizes_ok(rows, groups, k, n) || !float_type(dtype) || transposed < 0 || transposed > 1) return 0;
+  return grouped_workspace_bytes(sizes_of(rows, groups, transposed ? n : k, transposed ? k : n), dtype, transposed != 0);
+}
+
+size_t dsmoe_grouped_dw_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t dtype) {
+  if (!sizes_ok(rows, groups, k, n) || !float_type(dtype) || tiles(k, 128) * tiles(n, 128) > kMostPieces / groups) return 0;
+  return grouped_dw_workspace_bytes(sizes_of(rows, groups, k, n), dtype);
 }
 
 int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64_t dy_stride, const int32_t* offsets, int32_t rows,
                           int32_t groups, int32_t k, int32_t n, int32_t dtype, void* dw, int64_t dw_group_stride, int64_t dw_row_stride,
-                          void* stream) {
-  if (!sizes_ok(rows, groups, k, n) || !float_type(dtype)) return DSMOE_EINVAL;
+                          void* workspace, void* stream) {
+  if (!sizes_ok(rows, groups, k, n) || !float_type(dtype) || ((uintptr_t)workspace & 255) != 0) return DSMOE_EINVAL;
   if (!in_stride(x_stride) || !in_stride(dy_stride) || !out_stride(dw_row_stride, n) || !out_stride(dw_group_stride, (k - 1) * dw_row_stride + n))
     return DSMOE_EINVAL;
   if (!offsets || !dw || !aligned_to(dw, dtype)) return DSMOE_EINVAL;
@@ -110,11 +133,12 @@ int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64
   g.G = groups;
   g.M = k;
   g.N = n;
+  g.partial = (char*)workspace;
   return status(launch_grouped_dw(g, dtype, (hipStream_t)stream));
 }
 
-size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t k) {
-  return rows < 0 || rows > kMostRows || k < 1 || k > 1 << 17 ? 0 : int8_workspace_bytes(rows, k);
+size_t dsmoe_int8_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n) {
+  return !sizes_ok(rows, groups, k, n) || k > 1 << 17 ? 0 : int8_workspace_bytes(rows, groups, k, n);
 }
 
 int moe_int8_matmul(const void* x, int64_t x_stride, const int8_t* w, int64_t w_group_stride, int64_t w_row_stride, const float* w_scale,

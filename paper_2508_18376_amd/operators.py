@@ -7,7 +7,7 @@ import ctypes
 
 import torch
 
-from .binding import _NO_SWITCH, DsmoeError, _lib, _raw_stream
+from .binding import DsmoeError, _lib, _raw_stream
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _EINVAL, _EHIP = -1, -4
@@ -23,14 +23,16 @@ class _BlockNormArgs(ctypes.Structure):
 def _declare(L):
     vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
     args = ctypes.POINTER(_BlockNormArgs)
-    L.moe_grouped_matmul.argtypes = [vp, i64, vp, i64, i64, vp, i32, i32, i32, i32, i32, i32, vp, i64, vp]
-    L.moe_grouped_matmul_dw.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, i64, vp]
-    L.dsmoe_int8_workspace_bytes.argtypes = [i32, i32]
+    L.moe_grouped_matmul.argtypes = [vp, i64, vp, i64, i64, vp, i32, i32, i32, i32, i32, i32, vp, i64, vp, vp]
+    L.dsmoe_grouped_workspace_bytes.argtypes = [i32] * 6
+    L.dsmoe_grouped_dw_workspace_bytes.argtypes = [i32] * 5
+    L.moe_grouped_matmul_dw.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, i64, vp, vp]
+    L.dsmoe_int8_workspace_bytes.argtypes = [i32] * 4
     L.moe_int8_matmul.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp]
     L.moe_block_norm.argtypes = [args] + [vp] * 9
     L.dsmoe_block_norm_workspace_bytes.argtypes = [args]
     L.moe_block_norm_backward.argtypes = [args] + [vp] * 15
-    for f in (L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes):
+    for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes):
         f.restype = ctypes.c_size_t
     for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward):
         f.restype = ctypes.c_int
@@ -39,48 +41,53 @@ def _declare(L):
 _declare(_lib)
 
 
-def _need(ok, where: str, what: str) -> None:
-    if not ok:
-        raise DsmoeError(_EINVAL, "%s: %s;" % (where, what))
+def _refuse(where: str, what: str) -> None:
+    raise DsmoeError(_EINVAL, "%s: %s;" % (where, what))
 
 
-def _check(rc: int, where: str) -> None:
-    if rc != 0:
-        e = DsmoeError(rc, where)
-        if rc == _EHIP:
-            e.args = (e.args[0] + " hipError=%d" % _lib.dsmoe_last_hip_error(None),)
-        raise e
+def _failed(rc: int, where: str) -> None:
+    e = DsmoeError(rc, where)
+    if rc == _EHIP:
+        e.args = (e.args[0] + " hipError=%d" % _lib.dsmoe_last_hip_error(None),)
+    raise e
 
 
-def _rows_ok(t, where, name) -> None:
-    """The values of a row lie next to each other."""
-    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, where, "%s: the values of a row must be contiguous" % name)
+# A call on a few rows takes less time on the GPU than here (one token on 64 experts of 2048 x 1024: 8 us), so the checks below read each
+# property of a tensor once and make no objects or texts unless they refuse.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _on_gpu(where, device, **tensors) -> None:
-    for name, t in tensors.items():
-        _need(t is None or (t.is_cuda and t.device == device), where, "%s: all tensors must be on one GPU" % name)
+def _no_rows(where, name):
+    _refuse(where, "%s: the values of a row must be contiguous" % name)
 
 
 def _entered(device, stream):
-    """The device, and where the call names a stream that stream, made current: allocations then belong to it."""
+    """The device, and where the call names a stream that stream, made current: allocations then belong to it.  None: they are."""
     if stream is not None:
         return torch.cuda.stream(stream)
-    return _NO_SWITCH if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return None if device == _current_device() else torch.cuda.device(device)
+
+
+def _device_of(where, x, *others) -> int:
+    d = x.get_device()
+    for t in others:
+        if t is not None and t.get_device() != d:
+            d = -1
+    if d < 0:
+        _refuse(where, "all tensors must be on one GPU")
+    return d
 
 
 def _check_offsets(offsets, groups, where) -> None:
-    _need(offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.shape[0] == groups + 1 and offsets.is_contiguous(), where,
-          "offsets must be int32 [%d], contiguous" % (groups + 1))
+    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or offsets.shape[0] != groups + 1 or not offsets.is_contiguous():
+        _refuse(where, "offsets must be int32 [%d], contiguous" % (groups + 1))
 
 
-def _output(out, shape, like, where):
-    if out is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
-    _need(tuple(out.shape) == tuple(shape) and out.dtype == like.dtype and out.device == like.device, where,
-          "out must be %s %s on the inputs' device" % (list(shape), like.dtype))
-    _rows_ok(out, where, "out")
-    return out
+def _check_out(out, shape, like, where) -> None:
+    if out.shape != shape or out.dtype != like.dtype or out.device != like.device:
+        _refuse(where, "out must be %s %s on the inputs' device" % (list(shape), like.dtype))
+    if shape[-1] > 1 and out.stride(-1) != 1:
+        _no_rows(where, "out")
 
 
 def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None):
@@ -89,21 +96,45 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
     x [rows][k] ([rows][n] with w_transposed), w [groups][k][n], offsets int32 [groups + 1] on the GPU; bf16, f16 or f32.  Rows of no group
     (before the first offset, from the last one on) come out zero.  Rows and weights may be strided, the values of a row are contiguous."""
     f = "moe_grouped_matmul"
-    _need(x.dim() == 2 and w.dim() == 3, f, "x must have 2 dimensions and w 3")
-    R, G, k, n = x.shape[0], w.shape[0], w.shape[1], w.shape[2]
-    K, N = (n, k) if w_transposed else (k, n)
-    _need(x.shape[1] == K, f, "x must have rows of %d values" % K)
-    _need(x.dtype == w.dtype and x.dtype in _DTYPES, f, "x and w must be of one type, bfloat16, float16 or float32")
+    if x.dim() != 2 or w.dim() != 3:
+        _refuse(f, "x must have 2 dimensions and w 3")
+    R, K = x.shape
+    G, k, n = w.shape
+    N = n
+    if w_transposed:
+        N, k_of_x = k, n
+    else:
+        k_of_x = k
+    if K != k_of_x:
+        _refuse(f, "x must have rows of %d values" % k_of_x)
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or w.dtype is not x.dtype:
+        _refuse(f, "x and w must be of one type, bfloat16, float16 or float32")
     _check_offsets(offsets, G, f)
-    _rows_ok(x, f, "x")
-    _rows_ok(w, f, "w")
-    _on_gpu(f, x.device, x=x, w=w, offsets=offsets)
-    with _entered(x.device, stream):
-        y = _output(out, (R, N), x, f)
-        _check(_lib.moe_grouped_matmul(x.data_ptr(), x.stride(0), w.data_ptr(), w.stride(0), w.stride(1), offsets.data_ptr(), R, G, k, n,
-                                       1 if w_transposed else 0, _DTYPES[x.dtype], y.data_ptr(), max(y.stride(0), N) if R < 2 else y.stride(0),
-                                       _raw_stream(x.device.index)), f)
-    return y
+    x_row, x_value = x.stride()
+    w_group, w_row, w_value = w.stride()
+    if x_value != 1 and K > 1:
+        _no_rows(f, "x")
+    if w_value != 1 and n > 1:
+        _no_rows(f, "w")
+    device = _device_of(f, x, w, offsets)
+    entered = _entered(device, stream)
+    if entered is not None:
+        with entered:
+            return moe_grouped_matmul(x, w, offsets, w_transposed, out)
+    if out is None:
+        out, y_row = x.new_empty(R, N), N
+    else:
+        _check_out(out, (R, N), x, f)
+        y_row = out.stride(0) if R > 1 else N
+    transposed = 1 if w_transposed else 0
+    size = _lib.dsmoe_grouped_workspace_bytes(R, G, k, n, transposed, dtype)
+    workspace = offsets.new_empty(size // 4) if size else None
+    rc = _lib.moe_grouped_matmul(x.data_ptr(), x_row, w.data_ptr(), w_group, w_row, offsets.data_ptr(), R, G, k, n, transposed, dtype,
+                                 out.data_ptr(), y_row, workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    return out
 
 
 def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
@@ -111,21 +142,41 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
 
     x [rows][k], dy [rows][n], offsets int32 [groups + 1] on the GPU; returns [groups][k][n], zeros for a group without rows."""
     f = "moe_grouped_matmul_dw"
-    _need(x.dim() == 2 and dy.dim() == 2 and offsets.dim() == 1 and offsets.shape[0] >= 2, f, "x and dy must have 2 dimensions, offsets 1")
-    R, k, n, G = x.shape[0], x.shape[1], dy.shape[1], offsets.shape[0] - 1
-    _need(dy.shape[0] == R, f, "x and dy must have the same rows")
-    _need(x.dtype == dy.dtype and x.dtype in _DTYPES, f, "x and dy must be of one type, bfloat16, float16 or float32")
+    if x.dim() != 2 or dy.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 2:
+        _refuse(f, "x and dy must have 2 dimensions, offsets 1")
+    R, k = x.shape
+    rows, n = dy.shape
+    G = offsets.shape[0] - 1
+    if rows != R:
+        _refuse(f, "x and dy must have the same rows")
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or dy.dtype is not x.dtype:
+        _refuse(f, "x and dy must be of one type, bfloat16, float16 or float32")
     _check_offsets(offsets, G, f)
-    _rows_ok(x, f, "x")
-    _rows_ok(dy, f, "dy")
-    _on_gpu(f, x.device, x=x, dy=dy, offsets=offsets)
-    with _entered(x.device, stream):
-        dw = _output(out, (G, k, n), x, f)
-        row = max(dw.stride(1), n) if k < 2 else dw.stride(1)
-        group = max(dw.stride(0), (k - 1) * row + n) if G < 2 else dw.stride(0)
-        _check(_lib.moe_grouped_matmul_dw(x.data_ptr(), x.stride(0), dy.data_ptr(), dy.stride(0), offsets.data_ptr(), R, G, k, n, _DTYPES[x.dtype],
-                                          dw.data_ptr(), group, row, _raw_stream(x.device.index)), f)
-    return dw
+    x_row, x_value = x.stride()
+    dy_row, dy_value = dy.stride()
+    if x_value != 1 and k > 1:
+        _no_rows(f, "x")
+    if dy_value != 1 and n > 1:
+        _no_rows(f, "dy")
+    device = _device_of(f, x, dy, offsets)
+    entered = _entered(device, stream)
+    if entered is not None:
+        with entered:
+            return moe_grouped_matmul_dw(x, dy, offsets, out)
+    if out is None:
+        out, row, group = x.new_empty(G, k, n), n, k * n
+    else:
+        _check_out(out, (G, k, n), x, f)
+        row = out.stride(1) if k > 1 else n
+        group = out.stride(0) if G > 1 else (k - 1) * row + n
+    size = _lib.dsmoe_grouped_dw_workspace_bytes(R, G, k, n, dtype)
+    workspace = offsets.new_empty(size // 4) if size else None
+    rc = _lib.moe_grouped_matmul_dw(x.data_ptr(), x_row, dy.data_ptr(), dy_row, offsets.data_ptr(), R, G, k, n, dtype, out.data_ptr(), group, row,
+                                    workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    return out
 
 
 def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
@@ -134,46 +185,81 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
     x [rows][k] bf16, f16 or f32; w int8 [groups][n][k]; w_scale float32 [groups][n]; offsets int32 [groups + 1] on the GPU, or None for
     one group of all rows.  y has x's type.  Weights whose rows start on 16 bytes are faster."""
     f = "moe_int8_matmul"
-    _need(x.dim() == 2 and w.dim() == 3, f, "x must have 2 dimensions and w 3")
-    R, k, G, n = x.shape[0], x.shape[1], w.shape[0], w.shape[1]
-    _need(w.shape[2] == k, f, "x must have rows of %d values" % w.shape[2])
-    _need(x.dtype in _DTYPES and w.dtype == torch.int8, f, "x must be bfloat16, float16 or float32 and w int8")
-    _need(w_scale.dtype == torch.float32 and tuple(w_scale.shape) == (G, n), f, "w_scale must be float32 [%d][%d]" % (G, n))
+    if x.dim() != 2 or w.dim() != 3:
+        _refuse(f, "x must have 2 dimensions and w 3")
+    R, k = x.shape
+    G, n, k_of_w = w.shape
+    if k != k_of_w:
+        _refuse(f, "x must have rows of %d values" % k_of_w)
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or w.dtype is not torch.int8:
+        _refuse(f, "x must be bfloat16, float16 or float32 and w int8")
+    if w_scale.dtype is not torch.float32 or w_scale.shape != (G, n):
+        _refuse(f, "w_scale must be float32 [%d][%d]" % (G, n))
     if offsets is not None:
         _check_offsets(offsets, G, f)
-    _need(offsets is not None or G == 1, f, "several groups need offsets")
-    for name, t in (("x", x), ("w", w), ("w_scale", w_scale)):
-        _rows_ok(t, f, name)
-    _on_gpu(f, x.device, x=x, w=w, w_scale=w_scale, offsets=offsets)
-    with _entered(x.device, stream):
-        y = _output(out, (R, n), x, f)
-        workspace = torch.empty(_lib.dsmoe_int8_workspace_bytes(R, k), dtype=torch.uint8, device=x.device)
-        _check(_lib.moe_int8_matmul(x.data_ptr(), x.stride(0), w.data_ptr(), w.stride(0), w.stride(1), w_scale.data_ptr(), w_scale.stride(0),
-                                    None if offsets is None else offsets.data_ptr(), R, G, k, n, _DTYPES[x.dtype], y.data_ptr(),
-                                    max(y.stride(0), n) if R < 2 else y.stride(0), workspace.data_ptr(), _raw_stream(x.device.index)), f)
-    return y
+    elif G != 1:
+        _refuse(f, "several groups need offsets")
+    x_row, x_value = x.stride()
+    w_group, w_row, w_value = w.stride()
+    s_group, s_value = w_scale.stride()
+    if x_value != 1 and k > 1:
+        _no_rows(f, "x")
+    if w_value != 1 and k > 1:
+        _no_rows(f, "w")
+    if s_value != 1 and n > 1:
+        _no_rows(f, "w_scale")
+    device = _device_of(f, x, w, w_scale, offsets)
+    entered = _entered(device, stream)
+    if entered is not None:
+        with entered:
+            return moe_int8_matmul(x, w, w_scale, offsets, out)
+    if out is None:
+        out, y_row = x.new_empty(R, n), n
+    else:
+        _check_out(out, (R, n), x, f)
+        y_row = out.stride(0) if R > 1 else n
+    size = _lib.dsmoe_int8_workspace_bytes(R, G, k, n)
+    workspace = w.new_empty(size) if size else None
+    rc = _lib.moe_int8_matmul(x.data_ptr(), x_row, w.data_ptr(), w_group, w_row, w_scale.data_ptr(), s_group,
+                              None if offsets is None else offsets.data_ptr(), R, G, k, n, dtype, out.data_ptr(), y_row,
+                              workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    return out
 
 
 def _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, eps):
-    _need(x.dim() == 2 and x.shape[1] > 0 and branch.shape == x.shape, f, "x and branch must be [tokens][d], of one shape")
-    T, D = x.shape
-    _need(branch_weight.shape == (D,) and weight.shape == (D,), f, "branch_weight and weight must be [%d]" % D)
-    kind = GATE_NONE
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2 or shape[1] < 1 or branch.shape != shape:
+        _refuse(f, "x and branch must be [tokens][d], of one shape")
+    T, D = shape
+    if branch_weight.dim() != 1 or weight.dim() != 1 or branch_weight.shape[0] != D or weight.shape[0] != D:
+        _refuse(f, "branch_weight and weight must be [%d]" % D)
+    code = _DTYPES.get(dtype)
+    if code is None or branch.dtype is not dtype or branch_weight.dtype is not dtype or weight.dtype is not dtype:
+        _refuse(f, "x, branch, gate and the weights must be of one type, bfloat16, float16 or float32")
+    kind = gate_row = 0
     if gate is not None:
-        _need(gate.dim() == 2 and gate.shape[0] in (1, T) and gate.shape[1] in (1, D), f, "gate must be [tokens][1], [1][d] or [tokens][d]")
-        kind = GATE_FULL if gate.shape == x.shape else GATE_TOKEN if gate.shape == (T, 1) else GATE_CHANNEL
-        _need(kind != GATE_CHANNEL or gate.shape == (1, D), f, "gate must be [tokens][1], [1][d] or [tokens][d]")
-        _rows_ok(gate, f, "gate")
-    _need(x.dtype in _DTYPES and all(t is None or t.dtype == x.dtype for t in (branch, branch_weight, gate, weight)), f,
-          "x, branch, gate and the weights must be of one type, bfloat16, float16 or float32")
-    for name, t in (("x", x), ("branch", branch), ("branch_weight", branch_weight), ("weight", weight)):
-        _rows_ok(t, f, name)
-    _need(eps >= 0, f, "eps must not be negative")
-    return _BlockNormArgs(T, D, _DTYPES[x.dtype], kind, scale, weight_offset, eps, 0, x.stride(0), branch.stride(0), 0 if gate is None else gate.stride(0))
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+        gs = gate.shape
+        kind = GATE_FULL if gs == shape else GATE_TOKEN if gs == (T, 1) else GATE_CHANNEL
+        if kind == GATE_CHANNEL and gs != (1, D):
+            _refuse(f, "gate must be [tokens][1], [1][d] or [tokens][d]")
+        if gate.dtype is not dtype:
+            _refuse(f, "x, branch, gate and the weights must be of one type, bfloat16, float16 or float32")
+        gate_row, gate_value = gate.stride()
+        if gate_value != 1 and gs[1] > 1:
+            _no_rows(f, "gate")
+    x_row, x_value = x.stride()
+    b_row, b_value = branch.stride()
+    if D > 1:
+        if x_value != 1 or b_value != 1:
+            _no_rows(f, "x and branch")
+        if branch_weight.stride()[0] != 1 or weight.stride()[0] != 1:
+            _no_rows(f, "branch_weight and weight")
+    if not eps >= 0:
+        _refuse(f, "eps must not be negative")
+    return _BlockNormArgs(T, D, code, kind, scale, weight_offset, eps, 0, x_row, b_row, gate_row)
 
 
 def moe_block_norm(x, *, branch, branch_weight, weight, gate=None, scale=1.0, weight_offset=0.0, eps=1e-6, want_stats=False, stream=None):
@@ -184,12 +270,19 @@ def moe_block_norm(x, *, branch, branch_weight, weight, gate=None, scale=1.0, we
     (float32 [2][tokens]) for moe_block_norm_backward."""
     f = "moe_block_norm"
     args = _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, eps)
-    _on_gpu(f, x.device, x=x, branch=branch, branch_weight=branch_weight, gate=gate, weight=weight)
-    with _entered(x.device, stream):
-        y, h = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
-        stats = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device) if want_stats else None
-        _check(_lib.moe_block_norm(args, x.data_ptr(), branch.data_ptr(), branch_weight.data_ptr(), _ptr(gate), weight.data_ptr(), y.data_ptr(),
-                                   h.data_ptr(), _ptr(stats), _raw_stream(x.device.index)), f)
+    device = _device_of(f, x, branch, branch_weight, weight, gate)
+    entered = _entered(device, stream)
+    if entered is not None:
+        with entered:
+            return moe_block_norm(x, branch=branch, branch_weight=branch_weight, weight=weight, gate=gate, scale=scale, weight_offset=weight_offset,
+                                  eps=eps, want_stats=want_stats)
+    T, D = args.tokens, args.d
+    y, h = x.new_empty(T, D), x.new_empty(T, D)
+    stats = torch.empty((2, T), dtype=torch.float32, device=x.device) if want_stats else None
+    rc = _lib.moe_block_norm(args, x.data_ptr(), branch.data_ptr(), branch_weight.data_ptr(), None if gate is None else gate.data_ptr(),
+                             weight.data_ptr(), y.data_ptr(), h.data_ptr(), stats.data_ptr() if want_stats else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
     return (y, h, stats) if want_stats else (y, h)
 
 
@@ -198,22 +291,30 @@ def moe_block_norm_backward(dy, dh, x, stats, *, branch, branch_weight, weight, 
     shape).  The other arguments are those of the forward call, stats what it returned with want_stats."""
     f = "moe_block_norm_backward"
     args = _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, eps)
-    _need(dy.shape == x.shape and dh.shape == x.shape and dy.dtype == x.dtype and dh.dtype == x.dtype, f, "dy and dh must have x's shape and type")
-    _need(stats.shape == (2, x.shape[0]) and stats.dtype == torch.float32 and stats.is_contiguous(), f, "stats must be float32 [2][%d]" % x.shape[0])
-    _rows_ok(dy, f, "dy")
-    _rows_ok(dh, f, "dh")
-    args.dy_stride, args.dh_stride = dy.stride(0), dh.stride(0)
-    _on_gpu(f, x.device, dy=dy, dh=dh, x=x, stats=stats, branch=branch, branch_weight=branch_weight, gate=gate, weight=weight)
-    with _entered(x.device, stream):
-        def empty(*shape):
-            return torch.empty(shape, dtype=x.dtype, device=x.device)
-
-        out = {"dx": empty(*x.shape), "dbranch": empty(*x.shape), "dbranch_weight": empty(x.shape[1]), "dweight": empty(x.shape[1])}
-        if gate is not None:
-            out["dgate"] = empty(*gate.shape)
-        workspace = torch.empty(_lib.dsmoe_block_norm_workspace_bytes(args), dtype=torch.uint8, device=x.device)
-        _check(_lib.moe_block_norm_backward(args, dy.data_ptr(), dh.data_ptr(), x.data_ptr(), branch.data_ptr(), branch_weight.data_ptr(), _ptr(gate),
-                                            weight.data_ptr(), stats.data_ptr(), out["dx"].data_ptr(), out["dbranch"].data_ptr(),
-                                            out["dbranch_weight"].data_ptr(), _ptr(out.get("dgate")), out["dweight"].data_ptr(),
-                                            workspace.data_ptr(), _raw_stream(x.device.index)), f)
+    T, D = args.tokens, args.d
+    if dy.shape != x.shape or dh.shape != x.shape or dy.dtype is not x.dtype or dh.dtype is not x.dtype:
+        _refuse(f, "dy and dh must have x's shape and type")
+    if stats.shape != (2, T) or stats.dtype is not torch.float32 or not stats.is_contiguous():
+        _refuse(f, "stats must be float32 [2][%d], contiguous" % T)
+    args.dy_stride, dy_value = dy.stride()
+    args.dh_stride, dh_value = dh.stride()
+    if D > 1 and (dy_value != 1 or dh_value != 1):
+        _no_rows(f, "dy and dh")
+    device = _device_of(f, x, dy, dh, stats, branch, branch_weight, weight, gate)
+    entered = _entered(device, stream)
+    if entered is not None:
+        with entered:
+            return moe_block_norm_backward(dy, dh, x, stats, branch=branch, branch_weight=branch_weight, weight=weight, gate=gate, scale=scale,
+                                           weight_offset=weight_offset, eps=eps)
+    out = {"dx": x.new_empty(T, D), "dbranch": x.new_empty(T, D), "dbranch_weight": x.new_empty(D), "dweight": x.new_empty(D)}
+    if gate is not None:
+        out["dgate"] = x.new_empty(gate.shape)
+    size = _lib.dsmoe_block_norm_workspace_bytes(args)
+    workspace = stats.new_empty((size + 3) // 4) if size else None
+    rc = _lib.moe_block_norm_backward(args, dy.data_ptr(), dh.data_ptr(), x.data_ptr(), branch.data_ptr(), branch_weight.data_ptr(),
+                                      None if gate is None else gate.data_ptr(), weight.data_ptr(), stats.data_ptr(), out["dx"].data_ptr(),
+                                      out["dbranch"].data_ptr(), out["dbranch_weight"].data_ptr(), None if gate is None else out["dgate"].data_ptr(),
+                                      out["dweight"].data_ptr(), workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
     return out

@@ -32,6 +32,10 @@ SHAPES = {
     "odd_n": ([65, 64], 0, 0, 128, 203),
     "even_not_aligned": ([90, 45], 0, 1, 130, 166),
     "no_rows_in_groups": ([0, 0, 0], 4, 9, 64, 72),
+    "split_k": ([300, 0, 40, 70], 5, 9, 4096, 264),
+    "split_n": ([300, 0, 40, 70], 5, 9, 264, 4096),
+    "split_rows": ([5000, 0, 1234], 1, 2, 264, 136),
+    "split_last_round": ([4200, 3900], 0, 60, 1024, 2304),
     "many_groups": ([i % 3 for i in range(150)], 1, 0, 64, 40),
 }
 

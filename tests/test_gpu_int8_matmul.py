@@ -37,6 +37,8 @@ SHAPES = {
     "groups": ([3, 0, 130, 1], 2, 5, 192, 136, 0),
     "groups_odd": ([3, 0, 130, 1], 2, 5, 95, 51, 1),
     "decode": ([1, 0, 2, 1, 0, 3, 0, 1], 0, 0, 1408, 256, 0),
+    "split_k": ([300, 0, 40, 70], 5, 9, 5008, 264, 0),
+    "split_dense": (None, 0, 140, 9000, 520, 8),
     "long_k": ([2, 6], 0, 0, 17000, 40, 8),
 }
 

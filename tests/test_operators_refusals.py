@@ -110,25 +110,25 @@ def test_norms_backward_refuses(bad):
 P = 1 << 20  # an address that nothing reads: every call below is refused
 
 
-def grouped(x=P, xs=64, w=P, wg=64 * 32, wr=32, o=P, rows=10, groups=2, k=64, n=32, t=0, dt=1, y=P, ys=32):
-    return _lib.moe_grouped_matmul(x, xs, w, wg, wr, o, rows, groups, k, n, t, dt, y, ys, None)
+def grouped(x=P, xs=64, w=P, wg=64 * 32, wr=32, o=P, rows=10, groups=2, k=64, n=32, t=0, dt=1, y=P, ys=32, work=None):
+    return _lib.moe_grouped_matmul(x, xs, w, wg, wr, o, rows, groups, k, n, t, dt, y, ys, work, None)
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(o=None), dict(y=None), dict(rows=-1), dict(groups=0), dict(k=0), dict(n=0), dict(t=2),
                                 dict(dt=3), dict(dt=-1), dict(xs=-1), dict(wg=-1), dict(wr=-1), dict(ys=31), dict(t=1), dict(x=P + 1), dict(y=P + 1),
                                 dict(dt=0, w=P + 2), dict(rows=(1 << 23) + 1), dict(groups=1 << 17), dict(k=(1 << 24) + 1),
-                                dict(rows=1 << 23, n=1 << 24, ys=1 << 24)], ids=str)
+                                dict(rows=1 << 23, n=1 << 24, ys=1 << 24), dict(work=P + 128)], ids=str)
 def test_grouped_boundary(kw):
     assert grouped(**kw) == -1
 
 
-def dw(x=P, xs=64, dy=P, ds_=32, o=P, rows=10, groups=2, k=64, n=32, dt=1, out=P, og=64 * 32, orow=32):
-    return _lib.moe_grouped_matmul_dw(x, xs, dy, ds_, o, rows, groups, k, n, dt, out, og, orow, None)
+def dw(x=P, xs=64, dy=P, ds_=32, o=P, rows=10, groups=2, k=64, n=32, dt=1, out=P, og=64 * 32, orow=32, work=None):
+    return _lib.moe_grouped_matmul_dw(x, xs, dy, ds_, o, rows, groups, k, n, dt, out, og, orow, work, None)
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(dy=None), dict(o=None), dict(out=None), dict(rows=-1), dict(groups=0), dict(k=0), dict(n=0), dict(dt=3),
                                 dict(xs=-1), dict(ds_=-1), dict(orow=31), dict(og=64 * 32 - 1), dict(x=P + 1), dict(out=P + 1),
-                                dict(k=1 << 24, n=1 << 24, orow=1 << 24, og=1 << 39)], ids=str)
+                                dict(k=1 << 24, n=1 << 24, orow=1 << 24, og=1 << 39), dict(work=P + 128)], ids=str)
 def test_dw_boundary(kw):
     assert dw(**kw) == -1
 
@@ -145,8 +145,12 @@ def test_int8_boundary(kw):
 
 
 def test_workspace_sizes():
-    assert _lib.dsmoe_int8_workspace_bytes(10, 64) >= 10 * 64 + 40
-    assert _lib.dsmoe_int8_workspace_bytes(-1, 64) == 0 and _lib.dsmoe_int8_workspace_bytes(10, 0) == 0
+    assert _lib.dsmoe_int8_workspace_bytes(10, 1, 64, 32) >= 10 * 64 + 40
+    assert _lib.dsmoe_int8_workspace_bytes(-1, 1, 64, 32) == 0 and _lib.dsmoe_int8_workspace_bytes(10, 1, 0, 32) == 0
+    # few rows, and sums too short to be worth it, are not split; few tiles of long sums are
+    assert _lib.dsmoe_grouped_workspace_bytes(8, 64, 2048, 1024, 0, 1) == 0 and _lib.dsmoe_grouped_workspace_bytes(4096, 8, 256, 1024, 0, 1) == 0
+    assert _lib.dsmoe_grouped_workspace_bytes(512, 1, 14336, 512, 0, 1) > 0 and _lib.dsmoe_grouped_workspace_bytes(512, 1, 14336, 512, 0, 0) == 0
+    assert _lib.dsmoe_grouped_dw_workspace_bytes(65536, 1, 256, 256, 1) > 0 and _lib.dsmoe_grouped_dw_workspace_bytes(128, 8, 256, 256, 1) == 0
     a = ops._BlockNormArgs(100, 64, 1, 2, 1.0, 0.0, 1e-6, 0, 64, 64, 0, 64, 64)
     assert _lib.dsmoe_block_norm_workspace_bytes(a) >= 3 * 64 * 4
     a.gate_kind = 4
