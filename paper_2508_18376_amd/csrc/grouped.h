@@ -174,6 +174,9 @@ inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t 
   return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
 }
 
+// position of chunk `chunk` (0..7) of row `row` in a [rows][128 bytes] tile; its own inverse.  Two rows are a turn of the banks.
+__device__ __forceinline__ int swz_wide(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
+
 __device__ __forceinline__ float elem_to_f32(const char* p, int type) {
   if (type == kElemF32) return *(const float*)p;
   if (type == kElemBF16) return bf16_to_f32(*(const uint16_t*)p);

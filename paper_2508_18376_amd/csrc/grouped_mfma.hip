@@ -87,9 +87,6 @@ __device__ __forceinline__ lds_ptr lds_at(uint32_t address) { return (lds_ptr)(u
 __device__ __forceinline__ gi32x4 lds_read16(lds_ptr p) { return *(__attribute__((address_space(3))) const gi32x4*)p; }
 __device__ __forceinline__ gs16x4 lds_read_across(lds_ptr p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) gs16x4*)p); }
 
-// position of chunk `chunk` (0..7) of row `row` in a [rows][128 bytes] tile; its own inverse.  Two rows are a turn of the banks.
-__device__ __forceinline__ int swz_wide(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
-
 // An operand's way from memory to LDS: a unit is 256 rows x 128 bytes (along) or 64 contraction rows x 512 bytes (across).
 // The lanes' offsets are the same for all tiles.  A tile has a base, which moves on by a unit's stretch of the contraction (two scalar
 // additions: scalar instructions in a row would hold up the matrix instructions), and an extent from there on, one for the last unit and

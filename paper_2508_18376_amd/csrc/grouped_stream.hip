@@ -51,15 +51,35 @@ struct No {
   static constexpr bool value = false;
 };
 
-// W words from p, of which `left` values of SZ bytes exist (zeros behind them)
+// W (a power of two) words from p, of which `left` values of SZ bytes exist (zeros behind them); `before`: values of the row in front of p.
+// A part of them is loaded up to its end and shifted down; only rows shorter than that are loaded value by value.
 template <int W, int SZ, bool GUARD, bool ONCE>
-__device__ __forceinline__ void load_words(uint32_t* v, const char* p, int left) {
+__device__ __forceinline__ void load_words(uint32_t* v, const char* p, int left, int before) {
   typedef uint32_t words_t __attribute__((ext_vector_type(W < 4 ? W : 4), aligned(1)));
-  if (!GUARD || left >= W * 4 / SZ) {
+  constexpr int FULL = W * 4 / SZ;
+  if (GUARD && left <= 0) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = 0;
+    return;
+  }
+  const int missing = GUARD && left < FULL ? FULL - left : 0;
+  if (!GUARD || missing <= before) {
+    if (GUARD) p -= missing * SZ;
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
       const words_t x = ONCE ? __builtin_nontemporal_load((const words_t*)(p + 4 * i)) : *(const words_t*)(p + 4 * i);
       __builtin_memcpy(v + i, &x, sizeof(x));
+    }
+    if (GUARD) {
+      const int bytes = missing * SZ;
+#pragma unroll
+      for (int s = W / 2; s > 0; s >>= 1)  // whole words, in powers of two
+        if (bytes / 4 & s) {
+#pragma unroll
+          for (int i = 0; i < W; ++i) v[i] = i + s < W ? v[i + s] : 0;
+        }
+#pragma unroll
+      for (int i = 0; i < W; ++i) v[i] = (uint32_t)(((uint64_t)(i + 1 < W ? v[i + 1] : 0) << 32 | v[i]) >> (bytes % 4 * 8));
     }
     return;
   }
@@ -90,7 +110,7 @@ struct Step {
 };
 
 template <int TY, bool BX, int NR, int J, int W, bool ONCE>
-__device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, const char* pa, const char* pb, int rows, int cols, int K,
+__device__ __forceinline__ void stream_tile(const GroupedArgs& g, const char* pa, const char* pb, int rows, int n0, int cols, int K,
                                             typename SAcc<TY>::type (&acc)[NR][J]) {
   using E = SElem<TY, BX>;
   using S = Step<TY, BX, NR, J>;
@@ -111,7 +131,7 @@ __device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, c
       const char* p = pb + k0 * g.b_row;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        load_words<S::RW, E::bytes, GUARD, ONCE>(s.w + e * S::RW, p + b_at[0], e < left ? cols - J * i : 0);
+        load_words<S::RW, E::bytes, GUARD, ONCE>(s.w + e * S::RW, p + b_at[0], e < left ? cols - J * i : 0, n0 + J * i);
         p += g.b_row;
       }
     } else {
@@ -120,13 +140,13 @@ __device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, c
       for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int h = 0; h < E::parts; ++h)
-          load_words<E::words, E::bytes, GUARD, ONCE>(s.w + j * E::lane_words + h * E::words, p + b_at[j] + h * 64, left - h * (E::step / 2));
+          load_words<E::words, E::bytes, GUARD, ONCE>(s.w + j * E::lane_words + h * E::words, p + b_at[j] + h * 64, left - h * (E::step / 2), K - left + h * (E::step / 2));
     }
     const char* p = pa + (int64_t)k0 * E::bytes;
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
-      for (int h = 0; h < E::parts; ++h) load_words<E::words, E::bytes, GUARD, false>(s.a[r] + h * E::words, p + a_at[r] + h * 64, left - h * (E::step / 2));
+      for (int h = 0; h < E::parts; ++h) load_words<E::words, E::bytes, GUARD, false>(s.a[r] + h * E::words, p + a_at[r] + h * 64, left - h * (E::step / 2), K - left + h * (E::step / 2));
   };
   auto multiply = [&](const S& s) __attribute__((always_inline)) {
 #pragma unroll
@@ -191,7 +211,7 @@ __device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, c
       multiply(s1);
     }
   } else {
-    for (int t = wave; t * E::step < K; t += W) {  // columns past the last one: value by value
+    for (int t = wave; t * E::step < K; t += W) {  // columns past the last one
       S s1;
       load(s1, t, Yes());
       multiply(s1);
@@ -201,7 +221,7 @@ __device__ __forceinline__ void stream_tile(const GroupedArgs& g, float* sums, c
 
 template <int TY, int OUT, bool BX, int NR, int J, int W, bool ONCE>
 __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, const char* pa, const char* pb, char* pc, const float* as,
-                                            const float* bs, int rows, int cols, int K) {
+                                            const float* bs, int rows, int n0, int cols, int K) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
   typedef typename SAcc<TY>::type acc_t;
   acc_t acc[NR][J];
@@ -209,7 +229,7 @@ __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, con
   for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[r][j] = acc_t{0, 0, 0, 0};
-  if (K > 0) stream_tile<TY, BX, NR, J, W, ONCE>(g, (float*)lds, pa, pb, rows, cols, K, acc);
+  if (K > 0) stream_tile<TY, BX, NR, J, W, ONCE>(g, pa, pb, rows, n0, cols, K, acc);
   // A lane's sums: row lane % 16 of sixteen; along: columns 16 j + 4 q .. + 3 from acc[.][j]; across: columns J (4 q + v) + j from acc[.][j][v].
   typedef uint32_t word4 __attribute__((ext_vector_type(4)));
   constexpr int COLS = 16 * J, RF = row_floats(J);
@@ -282,9 +302,9 @@ __global__ __launch_bounds__(64 * W, J == 8 ? 2 : 4) void grouped_stream_kernel(
   const float* bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
   const int rows = min(kStreamTile, s.rows - m0), cols = min(COLS, g.N - n0), K = s.group < 0 ? 0 : g.K;
   if (rows <= 16)
-    stream_rows<TY, OUT, BX, 1, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, cols, K);
+    stream_rows<TY, OUT, BX, 1, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, n0, cols, K);
   else
-    stream_rows<TY, OUT, BX, 2, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, cols, K);
+    stream_rows<TY, OUT, BX, 2, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, n0, cols, K);
 }
 
 template <int TY, int OUT, bool BX, int J, int W, bool ONCE>
