@@ -160,6 +160,7 @@ size_t grouped_dw_split_bytes(const GroupedArgs& g);
 bool grouped_dw_mfma_fits(const GroupedArgs& g, int type);
 hipError_t launch_grouped_dw_mfma(const GroupedArgs& g, int type, hipStream_t s);
 // groups of few rows, any alignment
+bool grouped_stream_sizes(const GroupedArgs& g, int type, bool b_along, bool tiles_fit);
 bool grouped_stream_fits(const GroupedArgs& g, int type, bool b_along);
 hipError_t launch_grouped_stream(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
 inline hipError_t launch_grouped(const GroupedArgs& g, int type, bool b_along, hipStream_t s) {
@@ -167,7 +168,7 @@ inline hipError_t launch_grouped(const GroupedArgs& g, int type, bool b_along, h
   return grouped_mfma_fits(g, type, b_along) ? launch_grouped_mfma(g, type, b_along, s) : launch_grouped_plain(g, type, b_along, s);
 }
 inline size_t grouped_workspace_bytes(const GroupedArgs& g, int type, bool b_along) {
-  return type == kElemF32 || g.R == 0 || grouped_stream_fits(g, type, b_along) ? 0 : grouped_split_bytes(g, type);
+  return type == kElemF32 || g.R == 0 || grouped_stream_sizes(g, type, b_along, true) ? 0 : grouped_split_bytes(g, type);
 }
 inline size_t grouped_dw_workspace_bytes(const GroupedArgs& g, int type) { return type == kElemF32 ? 0 : grouped_dw_split_bytes(g); }
 inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t s) {

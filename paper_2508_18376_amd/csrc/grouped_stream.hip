@@ -329,25 +329,41 @@ constexpr int64_t kLastLevelBytes = 256ll << 20;
 // 9.8 us).  Many: whole 256-byte rows of 128 columns across the contraction, in workgroups of 4 wavefronts of which two share a
 // compute unit, so that one's beginning and end lie in the other's stream (64 tokens on 8 of 4096 x 14336: 8 wavefronts 171, 4 167; 64
 // columns 176).
+// Rows that do not start on 16 bytes keep to 64 columns, 8 bytes a lane: loads of 16 bytes from elsewhere are slow.
 template <int TY, int OUT, bool BX>
 hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
   const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
   if (pieces < 512) return launch<TY, OUT, BX, 4, 16, false>(g, s);
   constexpr bool WIDE = BX && TY != kElemF32;
+  if (WIDE && (((uintptr_t)g.b | g.b_row | g.b_group) & 15) != 0) return launch<TY, OUT, BX, 4, 8, false>(g, s);
   const bool once = (int64_t)(g.G < g.R ? g.G : g.R) * g.K * g.N * SElem<TY, BX>::bytes > kLastLevelBytes;
   return once ? launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, true>(g, s) : launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, false>(g, s);
 }
 
 }  // namespace
 
-// Up to 16 rows a group on average (8 where 16-bit weights lie along the contraction): beyond that the tiles of grouped_mfma.hip, which read weights
-// through LDS, are as fast.  Forward, streams -> tiles, us: 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 37 / 57 / 68 -> 44 / 54 / 54, 8 of
-// 4096 x 14336 at 4 / 16 / 24 rows 133 / 163 / 196 -> 171 / 182 / 184, 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 61 / 77 -> 85 / 86 / 88;
-// gradient of x 32 / 53 / 64 -> 41 / 52 / 53, 177 / 210 / 300 -> 250 / 263 / 264, 79 / 84 / 116 -> 70 / 72 / 76; 8 bits 23 / 32 / 41 -> 23 / 31 / 33,
-// 83 / 104 / 133 -> 105 / 116 / 118, 44 / 48 / 61 -> 55 / 58 / 62.
+// Which calls these kernels take (all times: this path against the other one, us).
+//   16-bit types and 8-bit integers whose rows start on 16 bytes: up to 16 rows a group on average, 8 where 16-bit weights lie along the
+//     contraction.  Beyond, the tiles of grouped_mfma.hip, which read weights through LDS, are as fast: y = x W on 64 experts of 2048 x 1024 at 1 / 8
+//     / 16 rows 37 / 57 / 68 against 44 / 54 / 54, on 8 of 4096 x 14336 at 4 / 16 / 24 rows 133 / 163 / 196 against 171 / 182 / 184; gradient of x 32 / 53 /
+//     64 against 41 / 52 / 53 and 177 / 210 / 300 against 250 / 263 / 264; 8 bits 23 / 32 / 41 against 23 / 31 / 33 and 83 / 104 / 133 against 105 / 116 / 118.
+//     Few pieces of long sums keep too few compute units busy, which split tiles do not: 16 rows of 14336 values, 4096 columns 66 against 38;
+//     of 4096 values, 4096 columns 16 against 19.5.
+//   Rows that start elsewhere, against grouped_plain.hip: the same, and few tiles across: 256 rows, 1001 x 1409 in one group 12.6 against 19.8, 512
+//     rows 22 against 20.
+//   fp32, against grouped_plain.hip: up to 128 rows a group, or tiles that do not fill the card: 16 experts of 2048 x 1408 at 64 / 96 / 128 / 192
+//     rows 100 / 122 / 149 / 203 against 144 / 147 / 213 / 256; 64 / 256 / 512 rows of 4096 x 4096 in one group 52 / 100 / 187 against 276 / 283 / 282.
+bool grouped_stream_sizes(const GroupedArgs& g, int type, bool b_along, bool tiles_fit) {
+  const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 127) / 128);
+  if (type == kElemF32) return g.R <= 128 * (int64_t)g.G || tiles < 400;
+  const bool few = g.R <= (b_along && type != kElemI8 ? 8 : 16) * (int64_t)g.G;
+  if (!tiles_fit) return few || (!b_along && tiles < 64);
+  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
+  return few && (pieces >= 128 || (int64_t)g.K * elem_bytes(type) <= 16384);
+}
 bool grouped_stream_fits(const GroupedArgs& g, int type, bool b_along) {
   const int64_t most = (int64_t)1 << 24;  // 64 rows of it are below 2^32
-  return g.R <= (b_along && type != kElemI8 && type != kElemF32 ? 8 : 16) * (int64_t)g.G && g.a_row <= most && g.b_row <= most;
+  return g.a_row <= most && g.b_row <= most && grouped_stream_sizes(g, type, b_along, grouped_mfma_fits(g, type, b_along));
 }
 hipError_t launch_grouped_stream(const GroupedArgs& g, int type, bool b_along, hipStream_t s) {
   switch (type) {
