@@ -92,120 +92,224 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(BlockNormArgs a) {
   }
 }
 
-// Column sums: S = 2 (dbranch_weight, dweight), 3 with a gate per channel.  Each set of TPR threads keeps those of its rows in registers and
-// leaves them as a row of the partial table; NCH == 0 keeps them in that table, each thread its own columns.
-template <int TY, int TPR, int NCH, int S>
-__global__ __launch_bounds__(kThreads) void block_norm_backward_kernel(BlockNormArgs a) {
-  __shared__ float lds[12];
-  constexpr int RW = kThreads / TPR, N = NCH ? NCH : 1;
-  const int i0 = (threadIdx.x % TPR) * 8, D = a.D;
-  const int n = NCH ? NCH : (D + TPR * 8 - 1) / (TPR * 8);
+// The backward pass, TPR threads a row of up to 8 TPR values (8 a thread), S = 2 column sums (dbranch_weight, dweight), 3 with a gate per
+// channel.  Rows are dealt out to the sets of TPR threads; each set keeps its rows' column sums in registers and leaves them as a row of the partial table.
+// The two sums that a row needs depend on each other, but the second is linear in the first: with q = b' (branch_weight + offset), times the gate where that
+// varies inside the row, and d = dy + u / rms(y),
+//   sum of q dx = sum of q d - (sum of u y' / (d rms(y))) * sum of q y'
+// so one exchange between the wavefronts gives all three.  The next row's values are on their way while this one is worked on: without that and with
+// two exchanges 8192 rows of 4096 took 145 us, two thirds of it waiting.
+// A last chunk that is not whole is the row's last 8 values: what it has in common with the chunk before it comes out the same in both, and only
+// counts once in the sums.
+template <int TY>
+struct RawRow {  // 8 values as they lie in memory
+  static constexpr int W = TY == DSMOE_F32 ? 8 : 4;
+  uint32_t w[W];
+  template <bool SHORT>  // rows of fewer than 8 values, too
+  __device__ __forceinline__ void load(const void* p, int64_t i, int n) {
+    const char* q = (const char*)p + i * RowElem<TY>::bytes;
+    if (n >= 8) {
+      __builtin_memcpy(w, q, 4 * W);
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[j] = 0;
+#pragma unroll
+      for (int e = 0; e < (SHORT ? 8 : 0); ++e)
+        if (e < n) {
+          if (TY == DSMOE_F32)
+            w[e % W] = ((const uint32_t*)q)[e];
+          else
+            w[e / 2 % W] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e & 1));
+        }
+    }
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    if (TY == DSMOE_F32) return __uint_as_float(w[e % W]);
+    if (TY == DSMOE_BF16) return __uint_as_float(e & 1 ? w[e / 2 % W] & 0xffff0000u : w[e / 2 % W] << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[e / 2 % W] >> (16 * (e & 1))));
+  }
+};
+
+// what fits into 128 registers with the next row's values in them: four wavefronts to a SIMD, two workgroups of 512 threads to a compute unit
+constexpr bool lean(int type, int gate) { return type != DSMOE_F32 && gate <= kGateToken; }
+
+template <int TY, int TPR, int GATE>
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR, lean(TY, GATE) && TPR >= 256 ? 4 : 1) void block_norm_backward_kernel(BlockNormArgs a) {
+  constexpr int THREADS = TPR < kThreads ? kThreads : TPR, RW = THREADS / TPR, S = GATE == kGateChannel ? 3 : 2, NW = TPR / 64;
+  __shared__ float lds[2][3][NW];
+  const int tid = threadIdx.x % TPR, D = a.D;
+  const int n = tid * 8 >= D ? 0 : D < 8 ? D : 8;         // values of this thread
+  const int c = tid * 8 + 8 > D && D >= 8 ? D - 8 : tid * 8;  // ... from this column on
+  const int lead = n > 0 ? tid * 8 - c : 0;                  // ... of which the first ones are another thread's too
   const int set = blockIdx.x * RW + threadIdx.x / TPR, sets = gridDim.x * RW;
   const float inv_d = 1.f / D;
-  float* part = a.partial + (int64_t)set * S * D;
-  float cs[S][N][8];
+  float wb[8], wy[8], gc[8], cs[S][8];
+  {
+    RawRow<TY> rb, ry, rg;
+    rb.template load<TPR == 64>(a.branch_weight, c, n);
+    ry.template load<TPR == 64>(a.weight, c, n);
+    if (GATE == kGateChannel) rg.template load<TPR == 64>(a.gate, c, n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      wb[e] = rb[e] + a.offset;
+      wy[e] = ry[e] + a.offset;
+      gc[e] = GATE == kGateChannel ? rg[e] * a.scale : 0.f;
+    }
+  }
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int k = 0; k < N; ++k)
+    for (int e = 0; e < 8; ++e) cs[s][e] = 0.f;
+  constexpr bool AHEAD = TPR < 1024 || lean(TY, GATE);
+  RawRow<TY> b, x, dh, dy, gf;
+  float inv_b, inv_y, gt;
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
+    b.template load<TPR == 64>(a.branch, t * a.branch_row + c, n);
+    x.template load<TPR == 64>(a.x, t * a.x_row + c, n);
+    dh.template load<TPR == 64>(a.dh, t * a.dh_row + c, n);
+    dy.template load<TPR == 64>(a.dy, t * a.dy_row + c, n);
+    if (GATE == kGateFull) gf.template load<TPR == 64>(a.gate, t * a.gate_row + c, n);
+    inv_b = a.stats[t];
+    inv_y = a.stats[a.T + t];
+    gt = GATE == kGateToken ? load1<TY>(a.gate, t * a.gate_row) * a.scale : a.scale;
+  };
+  if (AHEAD && set < a.T) load(set);
+  int turn = 0;
+  for (int64_t t = set; t < a.T; t += sets, turn ^= 1) {  // (a workgroup of one row at a time, or wavefronts on their own)
+    if (!AHEAD) load(t);
+    const float ib = inv_b, iy = inv_y, g0 = gt;  // g0: the gate's factor that the whole row has
+    float bh[8], yh[8], dx[8], g[8], dhy[8], sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) cs[s][k][e] = 0.f;
-  if (!NCH)
-    for (int s = 0; s < S; ++s)
-      for (int c = i0; c < D; c += TPR * 8)
-        for (int e = 0; e < 8 && c + e < D; ++e) part[s * D + c + e] = 0.f;
+    for (int e = 0; e < 8; ++e) {
+      if (GATE == kGateChannel) g[e] = gc[e];
+      if (GATE == kGateFull) g[e] = gf[e] * a.scale;
+      if (GATE <= kGateToken) g[e] = 1.f;
+      bh[e] = b[e] * ib;
+      float q = bh[e] * wb[e];
+      if (GATE > kGateToken) q *= g[e];
+      yh[e] = (GATE > kGateToken ? x[e] + q : x[e] + g0 * q) * iy;
+      const float u = dh[e] * wy[e];
+      dhy[e] = dh[e] * yh[e];
+      dx[e] = dy[e] + iy * u;
+      const float us = e < lead ? 0.f : u, qs = e < lead ? 0.f : q;
+      sum[0] += us * yh[e];
+      sum[1] += qs * dx[e];
+      sum[2] += qs * yh[e];
+    }
+    if (AHEAD && t + sets < a.T) load(t + sets);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      sum[i] = row_sum(sum[i]);
+      sum[i] += __shfl_xor(sum[i], 16);
+      sum[i] += __shfl_xor(sum[i], 32);
+      if (NW > 1 && (threadIdx.x & 63) == 0) lds[turn][i][threadIdx.x >> 6 & (NW - 1)] = sum[i];
+    }
+    if (NW > 1) {
+      __syncthreads();  // (the other turn's sums have been read before this barrier)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        sum[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum[i] += lds[turn][i][w];
+      }
+    }
+    const float m = sum[0] * inv_d * iy, dot = sum[1] - m * sum[2];  // dot: sum of q dx
+    const float f = GATE <= kGateToken ? g0 : 1.f, mv = f * dot * inv_d * ib, fb = f * ib;
+    float db[8], dg[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dx[e] -= yh[e] * m;
+      const float first = dx[e] * bh[e], w = GATE <= kGateToken ? wb[e] : wb[e] * g[e];
+      db[e] = fb * (dx[e] * w) - bh[e] * mv;
+      cs[0][e] += (GATE <= kGateToken ? f : g[e]) * first;
+      cs[1][e] += dhy[e];
+      if (GATE > kGateToken) dg[e] = a.scale * (first * wb[e]);
+      if (S > 2) cs[S - 1][e] += dg[e];
+    }
+    if (n > 0) {
+      store8<TY>(a.dx, t * D + c, TPR == 64 ? n : 8, dx);
+      store8<TY>(a.dbranch, t * D + c, TPR == 64 ? n : 8, db);
+      if (GATE == kGateFull) store8<TY>(a.dgate, t * D + c, TPR == 64 ? n : 8, dg);
+    }
+    if (GATE == kGateToken && tid == 0) store1<TY>(a.dgate, t, a.scale * dot);
+  }
+  if (n > 0) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) store8<DSMOE_F32>(a.partial, ((int64_t)set * S + s) * D + c, TPR == 64 ? n : 8, cs[s]);
+  }
+}
 
-  for (int64_t t = set; t < a.T; t += sets) {  // (a workgroup of one row at a time, or wavefronts on their own)
+// Rows longer than 8192: read again in each step, the column sums kept in the partial table, each thread its own columns.
+template <int TY, int S>
+__global__ __launch_bounds__(kThreads) void block_norm_backward_long_kernel(BlockNormArgs a) {
+  __shared__ float lds[12];
+  const int i0 = threadIdx.x * 8, D = a.D;
+  const float inv_d = 1.f / D;
+  float* part = a.partial + (int64_t)blockIdx.x * S * D;
+  for (int s = 0; s < S; ++s)
+    for (int c = i0; c < D; c += kThreads * 8)
+      for (int e = 0; e < 8 && c + e < D; ++e) part[(int64_t)s * D + c + e] = 0.f;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     const float inv_b = a.stats[t], inv_y = a.stats[a.T + t];
-    float bh[N][8], yh[N][8], dx[N][8], w[N][8], g[N][8], dh[N][8];  // b', y', dx, then v, branch_weight + offset
+    float bh[8], yh[8], dx[8], w[8], g[8], dh[8];  // dx without the part that hangs on the row's sum; dh times y'
     float sum[1] = {0.f};
-    auto forward = [&](int k, int c) {
+    auto forward = [&](int c) __attribute__((always_inline)) {
       float x[8], wy[8];
-      load8<TY>(a.branch, t * a.branch_row + c, D - c, bh[k]);
+      load8<TY>(a.branch, t * a.branch_row + c, D - c, bh);
       load8<TY>(a.x, t * a.x_row + c, D - c, x);
-      load8<TY>(a.dh, t * a.dh_row + c, D - c, dh[k]);
-      load8<TY>(a.dy, t * a.dy_row + c, D - c, dx[k]);
-      gate8<TY>(a, t, c, D - c, g[k]);
-      load8<TY>(a.branch_weight, c, D - c, w[k]);
+      load8<TY>(a.dh, t * a.dh_row + c, D - c, dh);
+      load8<TY>(a.dy, t * a.dy_row + c, D - c, dx);
+      gate8<TY>(a, t, c, D - c, g);
+      load8<TY>(a.branch_weight, c, D - c, w);
       load8<TY>(a.weight, c, D - c, wy);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool in = c + e < D;
-        bh[k][e] = in ? bh[k][e] * inv_b : 0.f;
-        w[k][e] += a.offset;
-        yh[k][e] = in ? (x[e] + g[k][e] * (bh[k][e] * w[k][e])) * inv_y : 0.f;
-        const float u = in ? dh[k][e] * (wy[e] + a.offset) : 0.f;
-        dh[k][e] *= yh[k][e];  // from here on what dweight sums up
-        sum[0] += u * yh[k][e];
-        dx[k][e] += inv_y * u;  // the rest follows with the sum
+        bh[e] = in ? bh[e] * inv_b : 0.f;
+        w[e] += a.offset;
+        yh[e] = in ? (x[e] + g[e] * (bh[e] * w[e])) * inv_y : 0.f;
+        const float u = in ? dh[e] * (wy[e] + a.offset) : 0.f;
+        dh[e] *= yh[e];
+        sum[0] += u * yh[e];
+        dx[e] += inv_y * u;
       }
     };
-#pragma unroll N
-    for (int j = 0; j < n; ++j) forward(NCH ? j : 0, i0 + j * TPR * 8);
-    row_sums<TPR>(sum, lds);
+    for (int c = i0; c < D; c += kThreads * 8) forward(c);
+    row_sums<kThreads>(sum, lds);
     const float m = sum[0] * inv_d * inv_y;
     float two[2] = {0.f, 0.f};  // of v b', and of a gate per token
-    auto through = [&](int k) {
+    for (int c = i0; c < D; c += kThreads * 8) {
+      forward(c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dx[k][e] -= yh[k][e] * m;
-        const float db = dx[k][e] * bh[k][e], dg = db * w[k][e];
-        two[0] += g[k][e] * dg;
+        const float dg = (dx[e] - yh[e] * m) * bh[e] * w[e];
+        two[0] += g[e] * dg;
         two[1] += dg;
       }
-    };
-    if (!NCH) sum[0] = 0.f;
-#pragma unroll N
-    for (int j = 0; j < n; ++j) {
-      const int k = NCH ? j : 0, c = i0 + j * TPR * 8;
-      if (!NCH) forward(k, c);
-      through(k);
     }
-    row_sums<TPR>(two, lds + 4);
+    row_sums<kThreads>(two, lds + 4);
     const float mv = two[0] * inv_d;
-#pragma unroll N
-    for (int j = 0; j < n; ++j) {
-      const int k = NCH ? j : 0, c = i0 + j * TPR * 8;
-      if (!NCH) {
-        forward(k, c);
-        float keep[2] = {two[0], two[1]};
-        through(k);
-        two[0] = keep[0];
-        two[1] = keep[1];
-      }
+    for (int c = i0; c < D; c += kThreads * 8) {
+      forward(c);
       float db[8], dg[8], first[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        first[e] = dx[k][e] * bh[k][e];
-        dg[e] = a.scale * (first[e] * w[k][e]);
-        db[e] = inv_b * (g[k][e] * dx[k][e] * w[k][e] - bh[k][e] * mv);
-        first[e] *= g[k][e];
+        dx[e] -= yh[e] * m;
+        first[e] = dx[e] * bh[e];
+        dg[e] = a.scale * (first[e] * w[e]);
+        db[e] = inv_b * (g[e] * dx[e] * w[e] - bh[e] * mv);
+        first[e] *= g[e];
       }
-      store8<TY>(a.dx, t * D + c, D - c, dx[k]);
+      store8<TY>(a.dx, t * D + c, D - c, dx);
       store8<TY>(a.dbranch, t * D + c, D - c, db);
       if (a.gate_kind == kGateFull) store8<TY>(a.dgate, t * D + c, D - c, dg);
-      if (NCH) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          cs[0][k][e] += first[e];
-          cs[1][k][e] += dh[k][e];
-          if (S > 2) cs[S - 1][k][e] += dg[e];
-        }
-      } else {
-        for (int e = 0; e < 8 && c + e < D; ++e) {
-          part[c + e] += first[e];
-          part[D + c + e] += dh[k][e];
-          if (S > 2) part[2 * (int64_t)D + c + e] += dg[e];
-        }
+      for (int e = 0; e < 8 && c + e < D; ++e) {
+        part[c + e] += first[e];
+        part[(int64_t)D + c + e] += dh[e];
+        if (S > 2) part[2 * (int64_t)D + c + e] += dg[e];
       }
     }
     if (a.gate_kind == kGateToken && i0 == 0) store1<TY>(a.dgate, t, a.scale * two[1]);
-  }
-  if (NCH) {
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int k = 0; k < N; ++k) store8<DSMOE_F32>(part, (int64_t)s * D + i0 + k * TPR * 8, D - i0 - k * TPR * 8, cs[s][k]);
   }
 }
 
@@ -231,17 +335,21 @@ __global__ __launch_bounds__(1024) void block_norm_columns_kernel(BlockNormArgs 
   }
 }
 
-// Threads of a row, and rows of the partial table
-inline int threads_of(int D) { return D <= 512 ? 64 : kThreads; }
+// Rows of the partial table: as many sets of threads as the card holds of the kernel, but at least four rows each, so that the table does not become
+// the larger part of what is written (1001 rows of 2047: 1001 sets 24 us, 256 sets 14).
+inline int backward_threads(int D) { return D <= 512 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
 inline int partial_sets(int T, int D) {
-  const int most = D > 8192 ? 256 : D <= 512 ? 2048 : 512, rw = kThreads / threads_of(D);
-  const int sets = T < most ? T : most;
+  if (D > 8192) return T < 256 ? T : 256;
+  const int tpr = backward_threads(D), rw = tpr < kThreads ? kThreads / tpr : 1;
+  const int most = tpr == 64 ? 4096 : tpr == 256 ? 1024 : tpr == 512 ? 512 : 256, least = 256;
+  int sets = T / 4 < least ? (T < least ? T : least) : T / 4;
+  if (sets > most) sets = most;
   return (sets + rw - 1) / rw * rw;
 }
 
 template <int TY>
 hipError_t forward(const BlockNormArgs& a, hipStream_t s) {
-  const int D = a.D, rw = kThreads / threads_of(D);
+  const int D = a.D, rw = D <= 512 ? kThreads / 64 : 1;
   const dim3 grid((unsigned)((a.T + rw - 1) / rw)), block(kThreads);
   if (D <= 512)
     block_norm_kernel<TY, 64, 1><<<grid, block, 0, s>>>(a);
@@ -256,25 +364,35 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int TY, int S>
+template <int TY, int GATE>
+void launch_backward(const BlockNormArgs& a, int sets, hipStream_t s) {
+  const int D = a.D;
+  if (D <= 512)
+    block_norm_backward_kernel<TY, 64, GATE><<<dim3(sets / 4), dim3(kThreads), 0, s>>>(a);
+  else if (D <= 2048)
+    block_norm_backward_kernel<TY, 256, GATE><<<dim3(sets), dim3(256), 0, s>>>(a);
+  else if (D <= 4096)
+    block_norm_backward_kernel<TY, 512, GATE><<<dim3(sets), dim3(512), 0, s>>>(a);
+  else if (D <= 8192)
+    block_norm_backward_kernel<TY, 1024, GATE><<<dim3(sets), dim3(1024), 0, s>>>(a);
+  else
+    block_norm_backward_long_kernel<TY, GATE == kGateChannel ? 3 : 2><<<dim3(sets), dim3(kThreads), 0, s>>>(a);
+}
+
+template <int TY>
 hipError_t backward(const BlockNormArgs& a, hipStream_t s) {
-  const int D = a.D, sets = partial_sets(a.T, D), rw = kThreads / threads_of(D);
+  const int sets = partial_sets(a.T, a.D), S = a.gate_kind == kGateChannel ? 3 : 2;
   if (a.T > 0) {
-    const dim3 grid((unsigned)(sets / rw)), block(kThreads);
-    if (D <= 512)
-      block_norm_backward_kernel<TY, 64, 1, S><<<grid, block, 0, s>>>(a);
-    else if (D <= 2048)
-      block_norm_backward_kernel<TY, kThreads, 1, S><<<grid, block, 0, s>>>(a);
-    else if (D <= 4096)
-      block_norm_backward_kernel<TY, kThreads, 2, S><<<grid, block, 0, s>>>(a);
-    else if (D <= 8192)
-      block_norm_backward_kernel<TY, kThreads, 4, S><<<grid, block, 0, s>>>(a);
-    else
-      block_norm_backward_kernel<TY, kThreads, 0, S><<<grid, block, 0, s>>>(a);
+    switch (a.gate_kind) {
+      case kGateNone: launch_backward<TY, kGateNone>(a, sets, s); break;
+      case kGateToken: launch_backward<TY, kGateToken>(a, sets, s); break;
+      case kGateChannel: launch_backward<TY, kGateChannel>(a, sets, s); break;
+      default: launch_backward<TY, kGateFull>(a, sets, s);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  block_norm_columns_kernel<TY><<<dim3((unsigned)((D + 63) / 64), S), dim3(1024), 0, s>>>(a, a.T > 0 ? sets : 0, S);
+  block_norm_columns_kernel<TY><<<dim3((unsigned)((a.D + 63) / 64), S), dim3(1024), 0, s>>>(a, a.T > 0 ? sets : 0, S);
   return hipGetLastError();
 }
 
@@ -290,12 +408,7 @@ hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_block_norm_backward(const BlockNormArgs& a, hipStream_t s) {
-  const bool three = a.gate_kind == kGateChannel;
-  switch (a.type) {
-    case DSMOE_F32: return three ? backward<DSMOE_F32, 3>(a, s) : backward<DSMOE_F32, 2>(a, s);
-    case DSMOE_BF16: return three ? backward<DSMOE_BF16, 3>(a, s) : backward<DSMOE_BF16, 2>(a, s);
-    default: return three ? backward<DSMOE_F16, 3>(a, s) : backward<DSMOE_F16, 2>(a, s);
-  }
+  return a.type == DSMOE_F32 ? backward<DSMOE_F32>(a, s) : a.type == DSMOE_BF16 ? backward<DSMOE_BF16>(a, s) : backward<DSMOE_F16>(a, s);
 }
 
 }  // namespace dsmoe
