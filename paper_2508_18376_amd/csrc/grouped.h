@@ -72,57 +72,69 @@ __device__ __forceinline__ void lane_segment(const int32_t* off, int G, int R, i
   carry = __builtin_amdgcn_readlane(end, 63);
 }
 
-// Pieces of a launch over rows: per_tile for each BM rows of a segment.  pick(total) says which piece this workgroup takes.
-template <class Pick>
-__device__ __forceinline__ bool find_segment(const int32_t* off, int G, int R, int BM, int per_tile, Pick&& pick, int& piece, Segment& s) {
-  if (off == nullptr) {
-    s = Segment{0, R, 0, 0, (R + BM - 1) / BM * per_tile};
-    piece = pick(s.total);
-    return piece < s.total;
+// The segments' rows and pieces.  Up to 64 segments: worked out once and kept, one to a lane; more: again for each lookup.
+struct Segments {
+  const int32_t* off;
+  int G, R, begin, end;
+  __device__ __forceinline__ void init(const int32_t* off_, int G_, int R_) {
+    off = off_;
+    G = G_;
+    R = R_;
+    int carry = 0;
+    begin = 0;
+    end = R;
+    if (off != nullptr && G + 2 <= 64) lane_segment(off, G, R, threadIdx.x & 63, carry, begin, end);
   }
-  const int lane = threadIdx.x & 63, n = G + 2;
-  int begin, end, total = 0, carry = 0, scan = 0;
-  for (int s0 = 0; s0 < n; s0 += 64) {
-    lane_segment(off, G, R, s0 + lane, carry, begin, end);
-    scan = wave_scan<false>((end - begin + BM - 1) / BM) * per_tile;
-    total += __builtin_amdgcn_readlane(scan, 63);
-  }
-  s.total = total;
-  piece = pick(total);
-  if (piece >= total) return false;
-  int base = 0;
-  carry = 0;
-  for (int s0 = 0; s0 < n; s0 += 64) {
-    if (n > 64) {
-      lane_segment(off, G, R, s0 + lane, carry, begin, end);
-      scan = wave_scan<false>((end - begin + BM - 1) / BM) * per_tile;
+  // pieces: per_tile for each BM rows of a segment.  pick(total) says which piece this workgroup takes.
+  template <class Pick>
+  __device__ __forceinline__ bool find(int BM, int per_tile, Pick&& pick, int& piece, Segment& s) const {
+    if (off == nullptr) {
+      s = Segment{0, R, 0, 0, (R + BM - 1) / BM * per_tile};
+      piece = pick(s.total);
+      return piece < s.total;
     }
-    const uint64_t beyond = __ballot(base + scan > piece);
-    if (beyond) {
-      const int l = __builtin_ctzll(beyond), q = s0 + l;
-      s.row0 = __builtin_amdgcn_readlane(begin, l);
-      s.rows = __builtin_amdgcn_readlane(end, l) - s.row0;
-      s.group = q >= 1 && q <= G ? q - 1 : -1;
-      s.base = base + __builtin_amdgcn_readlane(scan, l) - (s.rows + BM - 1) / BM * per_tile;
-      return true;
+    const int lane = threadIdx.x & 63, n = G + 2;
+    int b = begin, e = end, total = 0, carry = 0, scan = 0;
+    for (int s0 = 0; s0 < n; s0 += 64) {
+      if (n > 64) lane_segment(off, G, R, s0 + lane, carry, b, e);
+      scan = wave_scan<false>((e - b + BM - 1) / BM) * per_tile;
+      total += __builtin_amdgcn_readlane(scan, 63);
     }
-    base += __builtin_amdgcn_readlane(scan, 63);
+    s.total = total;
+    piece = pick(total);
+    if (piece >= total) return false;
+    int base = 0;
+    carry = 0;
+    for (int s0 = 0; s0 < n; s0 += 64) {
+      if (n > 64) {
+        lane_segment(off, G, R, s0 + lane, carry, b, e);
+        scan = wave_scan<false>((e - b + BM - 1) / BM) * per_tile;
+      }
+      const uint64_t beyond = __ballot(base + scan > piece);
+      if (beyond) {
+        const int l = __builtin_ctzll(beyond), q = s0 + l;
+        s.row0 = __builtin_amdgcn_readlane(b, l);
+        s.rows = __builtin_amdgcn_readlane(e, l) - s.row0;
+        s.group = q >= 1 && q <= G ? q - 1 : -1;
+        s.base = base + __builtin_amdgcn_readlane(scan, l) - (s.rows + BM - 1) / BM * per_tile;
+        return true;
+      }
+      base += __builtin_amdgcn_readlane(scan, 63);
+    }
+    return false;
   }
-  return false;
-}
-
-// rows of group g
-__device__ __forceinline__ void group_rows(const int32_t* off, int G, int R, int g, int& row0, int& rows) {
-  int begin = 0, end = R, carry = 0;
-  if (off != nullptr) {
-    const int lane = threadIdx.x & 63;
-    for (int s0 = 0; s0 <= g + 1; s0 += 64) lane_segment(off, G, R, s0 + lane, carry, begin, end);
-    begin = __builtin_amdgcn_readlane(begin, (g + 1) & 63);
-    end = __builtin_amdgcn_readlane(end, (g + 1) & 63);
+  // rows of group g
+  __device__ __forceinline__ void group(int g, int& row0, int& rows) const {
+    int b = begin, e = end, carry = 0, l = 0;
+    if (off != nullptr) {
+      l = (g + 1) & 63;
+      if (G + 2 > 64)
+        for (int s0 = 0; s0 <= g + 1; s0 += 64) lane_segment(off, G, R, s0 + (threadIdx.x & 63), carry, b, e);
+    }
+    row0 = __builtin_amdgcn_readlane(b, l);
+    rows = __builtin_amdgcn_readlane(e, l) - row0;
   }
-  row0 = begin;
-  rows = end - begin;
-}
+};
 
 // most row tiles of BM rows that R rows in G groups can give
 inline int64_t row_tiles_bound(int64_t R, int64_t G, bool grouped, int BM) {

@@ -39,6 +39,7 @@ constexpr int kUnits = 5;                      // units of the ring: all of a co
 constexpr int kRingBytes = kUnits * kUnit;
 constexpr int kLoads = kUnit / 16 / 256;        // a thread's loads of a unit
 constexpr int kWorkgroups = 256;                // one to a compute unit
+constexpr int kTileStores = 32;                 // a thread's stores of a whole tile of 16-bit values
 constexpr uint32_t kOutOfBounds = 0x80000000u;  // beyond every buffer here (extents are below 2^31)
 
 template <int V>
@@ -264,35 +265,38 @@ struct Piece {
 };
 
 // A launch's last, partly filled round of tiles leaves compute units idle for a whole tile's time, and few tiles leave them idle altogether.  So
-// the tiles beyond whole rounds of 256 are split along the contraction into `parts` pieces of work each, whose sums go to a workspace as they
-// are; a second launch adds them up in order and stores C.  A stage of 128 bytes takes about 1.2 us, a partial tile's way out and back about
-// 0.1 us of the whole card's bandwidth, the second launch 5 us: parts is what makes stages / parts * 1.2 + tiles * parts * 0.1 least, if that saves
-// the 5 us.  (8192 rows on 8 experts, y = x W^T with 4096 columns and 14336 values to sum: 576 tiles, the last 64 in 4 parts.)
+// the tiles beyond whole rounds of 256 are cut where that pays: into two halves of their columns, which take 0.6 of a tile's time each, or along the
+// contraction into `parts` pieces of work, whose sums go to a workspace as they are and which a second launch adds up in order.  A
+// stage of 128 bytes takes about 1.2 us, a partial tile's way out and back about 0.1 us of the whole card's bandwidth, the second launch 5 us:
+// the least sum of these decides.  (8192 rows on 8 experts, y = x W^T with 4096 columns and 14336 values to sum: 576 tiles, the last 64 in 4
+// parts, 936 -> 824 us; 65536 rows on 64 experts of 2048 x 1024: 1152 tiles, the last 128 in halves.)
 struct Split {
-  int whole;  // tiles that are not split
+  int whole;  // tiles that are not cut
   int parts;  // of each of the others (1: none is)
+  int cols;   // 1: these parts are halves of the columns
 };
 // room: what the workspace and the second launch have room for.  Times are in tenths of a microsecond.
 __host__ __device__ inline Split split_of(int tiles, int stages, const SplitRoom& room) {
   const int rest = tiles % kWorkgroups;
-  Split s = {tiles, 1};
-  if (rest == 0 || rest > room.tiles) return s;
-  int least = 12 * stages - 50;
+  Split s = {tiles, 1, 0};
+  if (rest == 0 || 2 * rest > kWorkgroups) return s;
+  s = Split{tiles - rest, 2, 1};
+  int least = 36 * stages / 5 - 50;
+  if (rest > room.tiles) return s;
   for (int parts = 2; parts <= 16 && parts * rest <= room.parts && 2 * parts <= stages; ++parts) {
     const int cost = 12 * stages / parts + rest * parts;
     if (cost < least) {
       least = cost;
-      s.whole = tiles - rest;
-      s.parts = parts;
+      s = Split{tiles - rest, parts, 0};
     }
   }
   return s;
 }
-// No more tiles than 2 sqrt(12 stages tiles) < 12 stages - 50 allows, and not many more parts than the least cost has: sqrt(12 stages / tiles).
+// No more tiles than 2 sqrt(12 stages tiles) < 7.2 stages - 50 allows, and not many more parts than the least cost has: sqrt(12 stages / tiles).
 inline SplitRoom split_room(int64_t most_tiles, int stages) {
   if (stages < 9) return SplitRoom{0, 0};
-  const int64_t gain = 12ll * stages - 50;
-  int64_t rest = gain * gain / (48ll * stages);
+  const int64_t gain = 36ll * stages / 5 - 50;
+  int64_t rest = gain * gain / (48ll * stages) + 1;
   if (rest > kWorkgroups / 2) rest = kWorkgroups / 2;
   if (rest > most_tiles) rest = most_tiles;
   int64_t parts = (int64_t)sqrt(12. * stages * rest) + 2 * rest;
@@ -320,13 +324,13 @@ __device__ __forceinline__ void part_of(const Split& s, int part, int K, int sta
   count = end > first ? end - first : 0;
 }
 
-// How the four wavefronts share a tile with m_edge rows: MI x NI blocks of 32 x 32 each, from (wm, wn) on.
-__device__ __forceinline__ void tile_shape(int m_edge, bool across, int w, int& mi, int& ni, int& wm, int& wn) {
+// How the four wavefronts share a tile with m_edge rows and n_edge columns: MI x NI blocks of 32 x 32 each, from (wm, wn) on.
+__device__ __forceinline__ void tile_shape(int m_edge, int n_edge, bool across, int w, int& mi, int& ni, int& wm, int& wn) {
   const bool tall = across || m_edge > 64;
   mi = m_edge > 128 ? 4 : tall || m_edge > 32 ? 2 : 1;
-  ni = tall ? 4 : 2;
+  ni = tall && n_edge > 128 ? 4 : 2;
   wm = tall ? (w & 1) * 32 * mi : 0;
-  wn = tall ? (w >> 1) * 128 : w * 64;
+  wn = tall ? (w >> 1) * 32 * ni : w * 64;
 }
 
 // The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
@@ -384,10 +388,15 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
   bool more = piece(i, p);
   if (!more) return;
   first_units(p);
+  bool stores_behind = false;  // exactly kTileStores stores were issued after the first units' loads
   while (more) {
     more = piece(++i, nxt);
-    // all of this wavefront's loads and stores; for all wavefronts, the fifth unit is free
-    wait_loads<0>();
+    // the first units are there (memory operations are counted off in order, so the last tile's stores may still be under way), and all
+    // wavefronts are done with the fifth unit
+    if (stores_behind)
+      wait_loads<kTileStores>();
+    else
+      wait_loads<0>();
     stage_barrier();
     auto whole = [&](auto& tile, int wm, int wn, auto MI_, auto NI_) __attribute__((always_inline)) {
       constexpr int MI = decltype(MI_)::value, NI = decltype(NI_)::value;
@@ -400,6 +409,7 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       tile.run(n, load_a, load_b, one_a, one_b);
       stage_barrier();
       if (more) first_units(nxt);
+      stores_behind = MI == 4 && NI == 4 && TY != kElemI8 && p.partial == nullptr && p.m_edge == kGT && p.n_edge == kGT;
       if (p.partial != nullptr) {  // in the order of the registers: the second launch knows where they belong
         char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
 #pragma unroll
@@ -452,12 +462,21 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           __builtin_amdgcn_wave_barrier();
           const int ch = lane % LPR;
+          if (MI == 4 && NI == 4 && stores_behind) {
 #pragma unroll
-          for (int k = 0; k < 32 * LPR / 64; ++k) {
-            const int rr = k * (64 / LPR) + lane / LPR;
-            const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
-            if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
+            for (int k = 0; k < 32 * LPR / 64; ++k) {
+              const int rr = k * (64 / LPR) + lane / LPR;
+              const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
               *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32 * LPR / 64; ++k) {
+              const int rr = k * (64 / LPR) + lane / LPR;
+              const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
+              if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
+                *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+            }
           }
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           __builtin_amdgcn_wave_barrier();
@@ -465,21 +484,22 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       }
     };
     int mi, ni, wm, wn;
-    tile_shape(p.m_edge, AX, w, mi, ni, wm, wn);
-    if (mi == 4) {
+    tile_shape(p.m_edge, p.n_edge, AX, w, mi, ni, wm, wn);
+    if (mi == 4 && ni == 4) {
       Tile<TY, AX, BX, 4, 4> t;
       whole(t, wm, wn, Const<4>(), Const<4>());
+    } else if (mi == 4) {
+      Tile<TY, AX, BX, 4, 2> t;
+      whole(t, wm, wn, Const<4>(), Const<2>());
     } else if (ni == 4) {
       Tile<TY, AX, BX, 2, 4> t;
       whole(t, wm, wn, Const<2>(), Const<4>());
+    } else if (AX || mi == 2) {
+      Tile<TY, AX, BX, 2, 2> t;
+      whole(t, wm, wn, Const<2>(), Const<2>());
     } else if constexpr (!AX) {
-      if (mi == 2) {
-        Tile<TY, AX, BX, 2, 2> t;
-        whole(t, wm, wn, Const<2>(), Const<2>());
-      } else {
-        Tile<TY, AX, BX, 1, 2> t;
-        whole(t, wm, wn, Const<1>(), Const<2>());
-      }
+      Tile<TY, AX, BX, 1, 2> t;
+      whole(t, wm, wn, Const<1>(), Const<2>());
     }
     p = nxt;
   }
@@ -489,6 +509,7 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
 template <int TY, int OUT, bool BX>
 struct RowsWork {
   static constexpr int EB = GElem<TY>::bytes, STAGE = 128 / EB;
+  Segments all;
   int tiles, part;
   Split split;
   // the piece that pick(tiles) names, if there is one
@@ -502,7 +523,7 @@ struct RowsWork {
       split = split_of(n, (g.K + STAGE - 1) / STAGE, g.room);
       return pick(*this);
     };
-    if (!find_segment(g.off, g.G, g.R, kGT, NT, pick_tile, tile, s)) return false;
+    if (!all.find(kGT, NT, pick_tile, tile, s)) return false;
     int rt, nt;
     band_tile(tile - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
     const int m0 = rt * kGT, n0 = nt * kGT, grp = max(s.group, 0);
@@ -516,7 +537,17 @@ struct RowsWork {
     p.n_edge = min(kGT, g.N - n0);
     p.K = s.group < 0 ? 0 : g.K;
     p.partial = nullptr;
-    if (tile >= split.whole) {
+    if (tile >= split.whole && split.cols) {
+      const int skip = part * kGT / 2;
+      if (skip >= p.n_edge) {  // (a last column tile of half the columns or less)
+        p.n_edge = p.K = 0;
+      } else {
+        p.n_edge = min(p.n_edge - skip, kGT / 2);
+        p.pb += BX ? (int64_t)skip * EB : skip * g.b_row;
+        p.pc += (int64_t)skip * elem_bytes(OUT);
+        if (TY == kElemI8) p.bs += skip;
+      }
+    } else if (tile >= split.whole) {
       p.partial = g.partial + ((tile - split.whole) * split.parts + part) * kPartialBytes;
       int first;
       part_of(split, part, p.K, STAGE, first, p.K);
@@ -530,8 +561,9 @@ struct RowsWork {
 template <int TY, int OUT, bool BX>
 __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
   extern __shared__ __align__(16) char ring[];
+  RowsWork<TY, OUT, BX> work;
+  work.all.init(g.off, g.G, g.R);
   do_pieces<TY, OUT, false, BX>(g, ring, [&](int i, Piece& p) {
-    RowsWork<TY, OUT, BX> work;
     return work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) {
       int tile;
       return work_of(w.split, w.tiles, blockIdx.x, i, tile, w.part) ? tile : w.tiles;
@@ -542,15 +574,21 @@ __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
 // dW = X^T dY.  The groups' rows differ; what is split is split for all of them alike.
 template <int TY>
 struct DwWork {
-  __device__ __forceinline__ static void find(const GroupedArgs& g, const Split& split, int tile, int part, Piece& p) {
+  __device__ __forceinline__ static void find(const GroupedArgs& g, const Segments& all, const Split& split, int tile, int part, Piece& p) {
     const int MT = (g.M + kGT - 1) / kGT, NT = (g.N + kGT - 1) / kGT, grp = tile / (MT * NT);
     int mt, nt, row0, rows;
     band_tile(tile - grp * MT * NT, MT, NT, mt, nt);
-    group_rows(g.off, g.G, g.R, grp, row0, rows);
-    const int m0 = mt * kGT, n0 = nt * kGT;
+    all.group(grp, row0, rows);
+    const int m0 = mt * kGT;
+    int n0 = nt * kGT;
     p.K = rows;
     p.partial = nullptr;
-    if (tile >= split.whole) {
+    p.n_edge = min(kGT, g.N - n0);
+    if (tile >= split.whole && split.cols) {
+      n0 += part * kGT / 2;
+      p.n_edge = min(p.n_edge - part * kGT / 2, kGT / 2);
+      if (p.n_edge <= 0) p.n_edge = p.K = 0;
+    } else if (tile >= split.whole) {
       p.partial = g.partial + ((tile - split.whole) * split.parts + part) * kPartialBytes;
       int first;
       part_of(split, part, rows, 64, first, p.K);
@@ -561,17 +599,18 @@ struct DwWork {
     p.pc = g.c + grp * g.c_group + m0 * g.c_row + (int64_t)n0 * 2;
     p.as = p.bs = nullptr;
     p.m_edge = min(kGT, g.M - m0);
-    p.n_edge = min(kGT, g.N - n0);
   }
 };
 
 template <int TY>
 __global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, int tiles, Split split) {
   extern __shared__ __align__(16) char ring[];
+  Segments all;
+  all.init(g.off, g.G, g.R);
   do_pieces<TY, TY, true, true>(g, ring, [&](int i, Piece& p) {
     int tile, part;
     if (!work_of(split, tiles, blockIdx.x, i, tile, part)) return false;
-    DwWork<TY>::find(g, split, tile, part, p);
+    DwWork<TY>::find(g, all, split, tile, part, p);
     return true;
   });
 }
@@ -588,19 +627,23 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, int dw
   if constexpr (AX) {
     tile = split.whole + blockIdx.x;
     if (tile >= dw_tiles) return;
-    DwWork<TY>::find(g, split, tile, 0, p);
+    Segments all;
+    all.init(g.off, g.G, g.R);
+    DwWork<TY>::find(g, all, split, tile, 0, p);
   } else {
     RowsWork<TY, OUT, BX> work;
+    work.all.init(g.off, g.G, g.R);
     work.part = 0;
     if (!work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) { return w.split.whole + (int)blockIdx.x; })) return;
     split = work.split;
     tile = split.whole + blockIdx.x;
   }
+  if (split.cols) return;
   const int lane = threadIdx.x & 63, block = blockIdx.y * 4 + (threadIdx.x >> 6);
   int mi, ni, wm, wn;
-  tile_shape(p.m_edge, AX, 0, mi, ni, wm, wn);
+  tile_shape(p.m_edge, p.n_edge, AX, 0, mi, ni, wm, wn);
   if (block >= 4 * mi * ni) return;
-  tile_shape(p.m_edge, AX, block / (mi * ni), mi, ni, wm, wn);
+  tile_shape(p.m_edge, p.n_edge, AX, block / (mi * ni), mi, ni, wm, wn);
   const int ab = block % (mi * ni), r = wm + ab / ni * 32 + (lane & 31);
   const char* from = p.partial + block * 4096 + lane * 16;
   value4 v[4];
@@ -646,10 +689,10 @@ hipError_t launch_rows(GroupedArgs g, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int64_t tiles = most_tiles(g);
   if (g.partial != nullptr) g.room = split_room(tiles, row_stages(g, TY));
-  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(g.room.tiles == 0 && tiles < kWorkgroups ? tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
+  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(g.room.tiles == 0 && 2 * tiles < kWorkgroups ? 2 * tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
   e = hipGetLastError();
   if (e != hipSuccess || g.room.tiles == 0) return e;
-  grouped_join_kernel<TY, OUT, false, BX><<<dim3(g.room.tiles, 16), dim3(256), 0, s>>>(g, 0, Split{0, 1});
+  grouped_join_kernel<TY, OUT, false, BX><<<dim3(g.room.tiles, 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});
   return hipGetLastError();
 }
 
@@ -663,7 +706,7 @@ hipError_t launch_dw(const GroupedArgs& g, hipStream_t s) {
   const int pieces = split.whole + (tiles - split.whole) * split.parts;
   grouped_dw_mfma_kernel<TY><<<dim3(pieces < kWorkgroups ? pieces : kWorkgroups), dim3(256), kRingBytes, s>>>(g, tiles, split);
   e = hipGetLastError();
-  if (e != hipSuccess || split.whole == tiles) return e;
+  if (e != hipSuccess || split.whole == tiles || split.cols) return e;
   grouped_join_kernel<TY, TY, true, true><<<dim3(tiles - split.whole, 16), dim3(256), 0, s>>>(g, tiles, split);
   return hipGetLastError();
 }
@@ -692,7 +735,7 @@ hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hip
 size_t grouped_split_bytes(const GroupedArgs& g, int type) { return (size_t)(split_room(most_tiles(g), row_stages(g, type)).parts * kPartialBytes); }
 size_t grouped_dw_split_bytes(const GroupedArgs& g) {
   const Split s = split_of(dw_tiles(g), dw_stages(g), split_room(dw_tiles(g), dw_stages(g)));
-  return (size_t)((s.parts > 1 ? dw_tiles(g) - s.whole : 0) * s.parts * kPartialBytes);
+  return (size_t)((s.cols ? 0 : dw_tiles(g) - s.whole) * s.parts * kPartialBytes);
 }
 
 bool grouped_dw_mfma_fits(const GroupedArgs& g, int type) {

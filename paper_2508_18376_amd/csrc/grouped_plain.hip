@@ -182,7 +182,9 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
     const int grp = piece / (MT * NT), id = piece - grp * MT * NT;
     int mt, nt, row0;
     band_tile(id, MT, NT, mt, nt);
-    group_rows(g.off, g.G, g.R, grp, row0, K);
+    Segments all;
+    all.init(g.off, g.G, g.R);
+    all.group(grp, row0, K);
     m0 = last_tile(mt, g.M);
     n0 = last_tile(nt, g.N);
     m_edge = min(kPT, g.M - m0);
@@ -191,7 +193,9 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
     pc = g.c + grp * g.c_group;
   } else {
     Segment s;
-    if (!find_segment(g.off, g.G, g.R, kPT, NT, [](int n) { return take_piece<false>(n, nullptr, nullptr); }, piece, s)) return;
+    Segments all;
+    all.init(g.off, g.G, g.R);
+    if (!all.find(kPT, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
     int rt, nt;
     band_tile(piece - s.base, (s.rows + kPT - 1) / kPT, NT, rt, nt);
     m0 = rt * kPT;

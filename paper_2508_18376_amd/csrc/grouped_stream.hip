@@ -290,7 +290,9 @@ __global__ __launch_bounds__(64 * W, J == 8 ? 2 : 4) void grouped_stream_kernel(
   const int NT = (g.N + COLS - 1) / COLS;
   int piece;
   Segment s;
-  if (!find_segment(g.off, g.G, g.R, kStreamTile, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
+  Segments all;
+  all.init(g.off, g.G, g.R);
+  if (!all.find(kStreamTile, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
   int rt, nt;
   band_tile(piece - s.base, (s.rows + kStreamTile - 1) / kStreamTile, NT, rt, nt);
   const int m0 = rt * kStreamTile, n0 = nt * COLS, grp = max(s.group, 0);
