@@ -92,15 +92,15 @@ __device__ __forceinline__ gs16x4 lds_read_across(lds_ptr p) { return __builtin_
 // The lanes' offsets are the same for all tiles.  A tile has a base, which moves on by a unit's stretch of the contraction (two scalar
 // additions: scalar instructions in a row would hold up the matrix instructions), and an extent from there on, one for the last unit and
 // one for the others.
-template <bool ACROSS>
+template <bool ACROSS, int LOADS = kLoads>
 struct Feed {
-  uint32_t voff[kLoads];
+  uint32_t voff[LOADS];
   uint32_t lo, hi, extent, last_extent;
   int64_t step;
   __device__ __forceinline__ void lanes(int64_t row_bytes, int tid) {
     step = ACROSS ? 64 * row_bytes : 128;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < LOADS; ++i) {
       const int r = ACROSS ? i * 8 + (tid >> 5) : i * 32 + (tid >> 3);
       voff[i] = (uint32_t)(r * (int)row_bytes + (ACROSS ? (tid & 31) ^ ((r & 3) << 2) : swz_wide(r, tid & 7)) * 16);
     }
@@ -275,16 +275,21 @@ struct Split {
   int parts;  // of each of the others (1: none is)
   int cols;   // 1: these parts are halves of the columns
 };
-// room: what the workspace and the second launch have room for.  Times are in tenths of a microsecond.
-__host__ __device__ inline Split split_of(int tiles, int stages, const SplitRoom& room) {
+// room: what the workspace and the second launch have room for; rows: of a tile on average.  Times are in tenths of a microsecond.  Tiles of few rows
+// wait for their weights, and halves of them just as long (333 tokens on 64 experts of 2048 x 1408 in 8 bits 62 -> 72 us): they have no halves,
+// but smaller partial tiles.
+__host__ __device__ inline Split split_of(int tiles, int stages, int rows, const SplitRoom& room) {
   const int rest = tiles % kWorkgroups;
   Split s = {tiles, 1, 0};
   if (rest == 0 || 2 * rest > kWorkgroups) return s;
-  s = Split{tiles - rest, 2, 1};
-  int least = 36 * stages / 5 - 50;
+  int least = 12 * stages - 50;
+  if (rows > kGT / 2) {
+    s = Split{tiles - rest, 2, 1};
+    least = 36 * stages / 5 - 50;
+  }
   if (rest > room.tiles) return s;
   for (int parts = 2; parts <= 16 && parts * rest <= room.parts && 2 * parts <= stages; ++parts) {
-    const int cost = 12 * stages / parts + rest * parts;
+    const int cost = 12 * stages / parts + rest * parts * (rows < kGT ? rows : kGT) / kGT;
     if (cost < least) {
       least = cost;
       s = Split{tiles - rest, parts, 0};
@@ -292,14 +297,15 @@ __host__ __device__ inline Split split_of(int tiles, int stages, const SplitRoom
   }
   return s;
 }
-// No more tiles than 2 sqrt(12 stages tiles) < 7.2 stages - 50 allows, and not many more parts than the least cost has: sqrt(12 stages / tiles).
-inline SplitRoom split_room(int64_t most_tiles, int stages) {
+// rows: at least that many a tile.  No more tiles than 2 sqrt(12 stages tiles rows / 256) < 7.2 or 12 stages - 50 allows, and not many more parts than the least
+// cost has: sqrt(12 stages / tiles * 256 / rows).
+inline SplitRoom split_room(int64_t most_tiles, int stages, int rows) {
   if (stages < 9) return SplitRoom{0, 0};
-  const int64_t gain = 36ll * stages / 5 - 50;
-  int64_t rest = gain * gain / (48ll * stages) + 1;
+  const double share = rows < kGT ? rows < 1 ? 1. / kGT : (double)rows / kGT : 1., gain = (rows > kGT / 2 ? 7.2 : 12.) * stages - 50;
+  int64_t rest = (int64_t)(gain * gain / (48. * stages * share)) + 1;
   if (rest > kWorkgroups / 2) rest = kWorkgroups / 2;
   if (rest > most_tiles) rest = most_tiles;
-  int64_t parts = (int64_t)sqrt(12. * stages * rest) + 2 * rest;
+  int64_t parts = (int64_t)sqrt(12. * stages * rest / share) + 2 * rest;
   if (parts > kWorkgroups) parts = kWorkgroups;
   return SplitRoom{(int)rest, (int)parts};
 }
@@ -331,6 +337,84 @@ __device__ __forceinline__ void tile_shape(int m_edge, int n_edge, bool across, 
   ni = tall && n_edge > 128 ? 4 : 2;
   wm = tall ? (w & 1) * 32 * mi : 0;
   wn = tall ? (w >> 1) * 32 * ni : w * 64;
+}
+
+// Stores a tile's sums, of which this wavefront has rows wm .. + 32 MI and columns wn .. + 32 NI.  turn: 32 rows of 64 NI bytes of LDS of its own; inside:
+// all rows and columns exist.
+template <int TY, int OUT, int MI, int NI>
+__device__ __forceinline__ void write_tile(const GroupedArgs& g, const Piece& p, const typename AccType<TY>::type (&acc)[MI][NI], char* turn, int wm, int wn,
+                                           int w, int lane, bool inside) {
+  if (p.partial != nullptr) {  // in the order of the registers: the second launch knows where they belong
+    char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
+#pragma unroll
+    for (int a = 0; a < MI; ++a)
+#pragma unroll
+      for (int b = 0; b < NI; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          typedef typename AccType<TY>::type acc_t;
+          const acc_t& c = acc[a][b];
+          typedef decltype(c[0] + c[0]) value_t;
+          typedef value_t value4 __attribute__((ext_vector_type(4)));
+          *(value4*)(to + ((a * NI + b) * 4 + q) * 1024) = value4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+    return;
+  }
+  // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
+  const int r32 = lane & 31, half = lane >> 5;
+  auto value = [&](int a, int b, int v, float as, const float* bs) __attribute__((always_inline)) -> float {
+    if constexpr (TY == kElemI8)
+      return (float)acc[a][b][v] * as * bs[v & 3];
+    else
+      return acc[a][b][v];
+  };
+#pragma unroll
+  for (int a = 0; a < MI; ++a) {
+    const int r = wm + a * 32 + r32;
+    const float as = TY == kElemI8 && p.K > 0 && r < p.m_edge ? p.as[r] : 0.f;
+    // 16 bits: each wavefront turns 32 rows at a time around in its part of the fifth unit and stores 16 bytes a lane, rows of 64 NI
+    // bytes; their 16-byte chunks are rotated by the row
+    constexpr int LPR = NI * 4;  // chunks of a row
+#pragma unroll
+    for (int b = 0; b < NI; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = wn + b * 32 + 8 * q + 4 * half;
+        float bs[4] = {0, 0, 0, 0};
+        if (TY == kElemI8 && p.K > 0 && c < p.n_edge) __builtin_memcpy(bs, p.bs + c, 16);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = value(a, b, 4 * q + e, as, bs);
+        if constexpr (OUT == kElemF32) {
+          if (r < p.m_edge && c < p.n_edge) *(gf32x4*)(p.pc + r * g.c_row + (int64_t)c * 4) = gf32x4{v[0], v[1], v[2], v[3]};
+        } else {
+          *(uint2*)(turn + r32 * (LPR * 16) + (((b * 4 + q) ^ (r32 & (LPR - 1))) * 16) + half * 8) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
+        }
+      }
+    if constexpr (OUT != kElemF32) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const int ch = lane % LPR;
+      if (MI == 4 && NI == 4 && inside) {
+#pragma unroll
+        for (int k = 0; k < 32 * LPR / 64; ++k) {
+          const int rr = k * (64 / LPR) + lane / LPR;
+          const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
+          *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32 * LPR / 64; ++k) {
+          const int rr = k * (64 / LPR) + lane / LPR;
+          const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
+          if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
+            *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
 }
 
 // The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
@@ -410,78 +494,7 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       stage_barrier();
       if (more) first_units(nxt);
       stores_behind = MI == 4 && NI == 4 && TY != kElemI8 && p.partial == nullptr && p.m_edge == kGT && p.n_edge == kGT;
-      if (p.partial != nullptr) {  // in the order of the registers: the second launch knows where they belong
-        char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
-#pragma unroll
-        for (int a = 0; a < MI; ++a)
-#pragma unroll
-          for (int b = 0; b < NI; ++b)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              typedef typename AccType<TY>::type acc_t;
-              const acc_t& c = tile.acc[a][b];
-              typedef decltype(c[0] + c[0]) value_t;
-              typedef value_t value4 __attribute__((ext_vector_type(4)));
-              *(value4*)(to + ((a * NI + b) * 4 + q) * 1024) = value4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-            }
-        return;
-      }
-      // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
-      const int r32 = lane & 31, half = lane >> 5;
-      auto value = [&](int a, int b, int v, float as, const float* bs) __attribute__((always_inline)) -> float {
-        if constexpr (TY == kElemI8)
-          return (float)tile.acc[a][b][v] * as * bs[v & 3];
-        else
-          return tile.acc[a][b][v];
-      };
-#pragma unroll
-      for (int a = 0; a < MI; ++a) {
-        const int r = wm + a * 32 + r32;
-        const float as = TY == kElemI8 && p.K > 0 && r < p.m_edge ? p.as[r] : 0.f;
-        // 16 bits: each wavefront turns 32 rows at a time around in its part of the fifth unit and stores 16 bytes a lane, rows of 64 NI
-        // bytes; their 16-byte chunks are rotated by the row
-        constexpr int LPR = NI * 4;  // chunks of a row
-        char* turn = lds + 4 * kUnit + w * (kUnit / 4);
-#pragma unroll
-        for (int b = 0; b < NI; ++b)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int c = wn + b * 32 + 8 * q + 4 * half;
-            float bs[4] = {0, 0, 0, 0};
-            if (TY == kElemI8 && p.K > 0 && c < p.n_edge) __builtin_memcpy(bs, p.bs + c, 16);
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = value(a, b, 4 * q + e, as, bs);
-            if constexpr (OUT == kElemF32) {
-              if (r < p.m_edge && c < p.n_edge) *(gf32x4*)(p.pc + r * g.c_row + (int64_t)c * 4) = gf32x4{v[0], v[1], v[2], v[3]};
-            } else {
-              *(uint2*)(turn + r32 * (LPR * 16) + (((b * 4 + q) ^ (r32 & (LPR - 1))) * 16) + half * 8) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
-            }
-          }
-        if constexpr (OUT != kElemF32) {
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-          const int ch = lane % LPR;
-          if (MI == 4 && NI == 4 && stores_behind) {
-#pragma unroll
-            for (int k = 0; k < 32 * LPR / 64; ++k) {
-              const int rr = k * (64 / LPR) + lane / LPR;
-              const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
-              *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32 * LPR / 64; ++k) {
-              const int rr = k * (64 / LPR) + lane / LPR;
-              const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
-              if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
-                *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
-            }
-          }
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-        }
-      }
+      write_tile<TY, OUT, MI, NI>(g, p, tile.acc, lds + 4 * kUnit + w * (kUnit / 4), wm, wn, w, lane, stores_behind);
     };
     int mi, ni, wm, wn;
     tile_shape(p.m_edge, p.n_edge, AX, w, mi, ni, wm, wn);
@@ -505,8 +518,112 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
   }
 }
 
+// Tiles of at most 64 rows, for groups of few rows, where the weights' stream is what counts: stages of 40 KiB (64 rows of A, 256 of B), four of them in the
+// ring, so that 120 KiB are under way to a compute unit instead of some 60.  The last stage's place is where a tile turns around while the next
+// tile's first three stages arrive.
+constexpr int kShortRows = 64;
+constexpr int kShortA = kShortRows * 128, kShortStage = kShortA + kUnit, kShortLoads = kShortA / 16 / 256 + kLoads;
+static_assert(4 * kShortStage == kRingBytes, "the same allocation");
+
+template <int TY, int OUT, bool BX, class Next>
+__device__ __forceinline__ void do_short_pieces(const GroupedArgs& g, char* lds, Next&& piece) {
+  constexpr int EB = GElem<TY>::bytes, AHEAD = 3;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t ring = lds_address(lds), mine = ring + (uint32_t)w * 1024;
+  Feed<false, 2> fa;
+  Feed<BX> fb;
+  fa.lanes(g.a_row, tid);
+  fb.lanes(g.b_row, tid);
+  auto whole_words = [](int b) { return TY == kElemI8 ? (b + 3) & ~3 : b; };
+  auto stages = [&](const Piece& p) __attribute__((always_inline)) { return (int)(((int64_t)p.K * EB + 127) / 128); };
+  uint32_t beyond = 0;
+  // stage st of n, into its place
+  auto load = [&](int st, int n) __attribute__((always_inline)) {
+    const bool last = st == n - 1;
+    const uint32_t to = mine + (uint32_t)(st & 3) * kShortStage, tail = last ? beyond : 0;
+    const gi32x4 rb = fb.next(last), ra = fa.next(last);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) load_to_lds(rb, to, kShortA + q * 4096, BX ? fb.voff[q] : fb.voff[q] | tail);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) load_to_lds(ra, to, q * 4096, fa.voff[q] | tail);
+  };
+  auto first_stages = [&](const Piece& p) __attribute__((always_inline)) {
+    const int kb = (int)(((int64_t)p.K * EB + 127) & 127) + 1, kr = ((p.K + 63) & 63) + 1;
+    fa.tile(p.pa, g.a_row, p.m_edge, whole_words(kb));
+    fb.tile(p.pb, g.b_row, BX ? p.n_edge * EB : p.n_edge, BX ? kr : whole_words(kb));
+    beyond = TY != kElemI8 && swz_wide(tid >> 3, tid & 7) * 16 >= kb ? kOutOfBounds : 0;
+    const int n = stages(p);
+    for (int st = 0; st < AHEAD && st < n; ++st) load(st, n);
+  };
+  Piece p, nxt;
+  int i = 0;
+  bool more = piece(i, p);
+  if (!more) return;
+  first_stages(p);
+  while (more) {
+    more = piece(++i, nxt);
+    wait_loads<0>();
+    stage_barrier();
+    auto whole = [&](auto MI_) __attribute__((always_inline)) {
+      constexpr int MI = decltype(MI_)::value, NI = 2;
+      int lane = tid & 63;
+      asm volatile("" : "+v"(lane));
+      const int wn = w * 64, n = stages(p);
+      Reader<false, MI> ra;
+      Reader<BX, NI> rb;
+      ra.init(ring, 0, lane);
+      rb.init(ring + kShortA, wn, lane);
+      typename AccType<TY>::type acc[MI][NI];
+#pragma unroll
+      for (int a = 0; a < MI; ++a)
+#pragma unroll
+        for (int b = 0; b < NI; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[a][b][v] = 0;
+      if (AHEAD < n) load(AHEAD, n);
+      for (int st = 0; st < n; ++st) {
+        const uint32_t at = (uint32_t)(st & 3) * kShortStage;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          gi32x4 a[MI], b[NI];
+#pragma unroll
+          for (int k = 0; k < MI; ++k) ra.read(a, k, 0, s, at);
+#pragma unroll
+          for (int k = 0; k < NI; ++k)
+#pragma unroll
+            for (int q = 0; q < Reader<BX, NI>::parts; ++q) rb.read(b, k, q, s, at);
+#pragma unroll
+          for (int k = 0; k < MI; ++k)
+#pragma unroll
+            for (int q = 0; q < NI; ++q) mac<TY>(acc[k][q], b[q], a[k]);
+        }
+        if (st + 1 < n) {
+          // the next stage is there for every wavefront, and every wavefront has read this one, whose place the fourth from here takes
+          const int behind = n - 2 - st;
+          if (behind >= 2)
+            wait_loads<2 * kShortLoads>();
+          else if (behind == 1)
+            wait_loads<kShortLoads>();
+          else
+            wait_loads<0>();
+          stage_barrier();
+          if (st + 4 < n) load(st + 4, n);
+        }
+      }
+      stage_barrier();
+      if (more) first_stages(nxt);
+      write_tile<TY, OUT, MI, NI>(g, p, acc, lds + 3 * kShortStage + w * (kShortStage / 4), 0, wn, w, lane, false);
+    };
+    if (p.m_edge > 32)
+      whole(Const<2>());
+    else
+      whole(Const<1>());
+    p = nxt;
+  }
+}
+
 // y = x W (BX) or x W^T (B along), and the 8-bit products
-template <int TY, int OUT, bool BX>
+template <int TY, int OUT, bool BX, int BM>
 struct RowsWork {
   static constexpr int EB = GElem<TY>::bytes, STAGE = 128 / EB;
   Segments all;
@@ -520,20 +637,20 @@ struct RowsWork {
     Segment s;
     auto pick_tile = [&](int n) {
       tiles = n;
-      split = split_of(n, (g.K + STAGE - 1) / STAGE, g.room);
+      split = split_of(n, (g.K + STAGE - 1) / STAGE, (int)((int64_t)g.R * NT / max(n, 1)), g.room);
       return pick(*this);
     };
-    if (!all.find(kGT, NT, pick_tile, tile, s)) return false;
+    if (!all.find(BM, NT, pick_tile, tile, s)) return false;
     int rt, nt;
-    band_tile(tile - s.base, (s.rows + kGT - 1) / kGT, NT, rt, nt);
-    const int m0 = rt * kGT, n0 = nt * kGT, grp = max(s.group, 0);
+    band_tile(tile - s.base, (s.rows + BM - 1) / BM, NT, rt, nt);
+    const int m0 = rt * BM, n0 = nt * kGT, grp = max(s.group, 0);
     const int64_t row = s.row0 + m0;
     p.pa = g.a + row * g.a_row;
     p.pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * EB : n0 * g.b_row);
     p.pc = g.c + row * g.c_row + (int64_t)n0 * elem_bytes(OUT);
     p.as = TY == kElemI8 ? g.a_scale + row : nullptr;
     p.bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
-    p.m_edge = min(kGT, s.rows - m0);
+    p.m_edge = min(BM, s.rows - m0);
     p.n_edge = min(kGT, g.N - n0);
     p.K = s.group < 0 ? 0 : g.K;
     p.partial = nullptr;
@@ -548,7 +665,7 @@ struct RowsWork {
         if (TY == kElemI8) p.bs += skip;
       }
     } else if (tile >= split.whole) {
-      p.partial = g.partial + ((tile - split.whole) * split.parts + part) * kPartialBytes;
+      p.partial = g.partial + ((tile - split.whole) * split.parts + part) * (kPartialBytes / kGT * BM);
       int first;
       part_of(split, part, p.K, STAGE, first, p.K);
       p.pa += (int64_t)first * EB;
@@ -558,17 +675,21 @@ struct RowsWork {
   }
 };
 
-template <int TY, int OUT, bool BX>
+template <int TY, int OUT, bool BX, int BM>
 __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
   extern __shared__ __align__(16) char ring[];
-  RowsWork<TY, OUT, BX> work;
+  RowsWork<TY, OUT, BX, BM> work;
   work.all.init(g.off, g.G, g.R);
-  do_pieces<TY, OUT, false, BX>(g, ring, [&](int i, Piece& p) {
-    return work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) {
+  auto next = [&](int i, Piece& p) __attribute__((always_inline)) {
+    return work.find(g, p, [&](RowsWork<TY, OUT, BX, BM>& w) {
       int tile;
       return work_of(w.split, w.tiles, blockIdx.x, i, tile, w.part) ? tile : w.tiles;
     });
-  });
+  };
+  if constexpr (BM == kShortRows)
+    do_short_pieces<TY, OUT, BX>(g, ring, next);
+  else
+    do_pieces<TY, OUT, false, BX>(g, ring, next);
 }
 
 // dW = X^T dY.  The groups' rows differ; what is split is split for all of them alike.
@@ -616,7 +737,7 @@ __global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, 
 }
 
 // Adds up the parts of the split tiles, in order: a wavefront for each block of 32 x 32 (blockIdx.x: the tile; blockIdx.y: sixteenths of its blocks).
-template <int TY, int OUT, bool AX, bool BX>
+template <int TY, int OUT, bool AX, bool BX, int BM>
 __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, int dw_tiles, Split dw_split) {
   typedef typename AccType<TY>::type acc_t;
   typedef decltype(acc_t{}[0] + acc_t{}[0]) value_t;
@@ -631,10 +752,10 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, int dw
     all.init(g.off, g.G, g.R);
     DwWork<TY>::find(g, all, split, tile, 0, p);
   } else {
-    RowsWork<TY, OUT, BX> work;
+    RowsWork<TY, OUT, BX, BM> work;
     work.all.init(g.off, g.G, g.R);
     work.part = 0;
-    if (!work.find(g, p, [&](RowsWork<TY, OUT, BX>& w) { return w.split.whole + (int)blockIdx.x; })) return;
+    if (!work.find(g, p, [&](RowsWork<TY, OUT, BX, BM>& w) { return w.split.whole + (int)blockIdx.x; })) return;
     split = work.split;
     tile = split.whole + blockIdx.x;
   }
@@ -650,7 +771,7 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedArgs g, int dw
 #pragma unroll
   for (int q = 0; q < 4; ++q) v[q] = *(const value4*)(from + q * 1024);
   for (int s = 1; s < split.parts; ++s) {
-    from += kPartialBytes;
+    from += kPartialBytes / kGT * BM;
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += *(const value4*)(from + q * 1024);
   }
@@ -678,22 +799,32 @@ hipError_t prepare(K kernel, PerDeviceOnce& once) {
 }
 
 inline int row_stages(const GroupedArgs& g, int type) { return (int)(((int64_t)g.K * elem_bytes(type) + 127) / 128); }
-inline int64_t most_tiles(const GroupedArgs& g) { return row_tiles_bound(g.R, g.G, g.off != nullptr, kGT) * ((g.N + kGT - 1) / kGT); }
+// Up to 64 rows a group on average: tiles of 64 rows.
+inline bool short_tiles(const GroupedArgs& g) { return g.R <= 64 * (int64_t)g.G; }
+inline int64_t most_tiles(const GroupedArgs& g, int BM) { return row_tiles_bound(g.R, g.G, g.off != nullptr, BM) * ((g.N + kGT - 1) / kGT); }
+inline SplitRoom rows_room(const GroupedArgs& g, int type, int BM) {
+  const int64_t tiles = most_tiles(g, BM);
+  return split_room(tiles, row_stages(g, type), (int)((int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1)));
+}
 inline int dw_tiles(const GroupedArgs& g) { return g.G * ((g.M + kGT - 1) / kGT) * ((g.N + kGT - 1) / kGT); }
 inline int dw_stages(const GroupedArgs& g) { return (g.R / g.G + 63) / 64; }  // (groups differ: the mean decides)
 
-template <int TY, int OUT, bool BX>
-hipError_t launch_rows(GroupedArgs g, hipStream_t s) {
+template <int TY, int OUT, bool BX, int BM>
+hipError_t launch_tiles(GroupedArgs g, hipStream_t s) {
   static PerDeviceOnce once;
-  hipError_t e = prepare(grouped_mfma_kernel<TY, OUT, BX>, once);
+  hipError_t e = prepare(grouped_mfma_kernel<TY, OUT, BX, BM>, once);
   if (e != hipSuccess) return e;
-  const int64_t tiles = most_tiles(g);
-  if (g.partial != nullptr) g.room = split_room(tiles, row_stages(g, TY));
-  grouped_mfma_kernel<TY, OUT, BX><<<dim3((unsigned)(g.room.tiles == 0 && 2 * tiles < kWorkgroups ? 2 * tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
+  const int64_t tiles = most_tiles(g, BM);
+  if (g.partial != nullptr) g.room = rows_room(g, TY, BM);
+  grouped_mfma_kernel<TY, OUT, BX, BM><<<dim3((unsigned)(g.room.tiles == 0 && 2 * tiles < kWorkgroups ? 2 * tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
   e = hipGetLastError();
   if (e != hipSuccess || g.room.tiles == 0) return e;
-  grouped_join_kernel<TY, OUT, false, BX><<<dim3(g.room.tiles, 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});
+  grouped_join_kernel<TY, OUT, false, BX, BM><<<dim3(g.room.tiles, BM / 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});
   return hipGetLastError();
+}
+template <int TY, int OUT, bool BX>
+hipError_t launch_rows(const GroupedArgs& g, hipStream_t s) {
+  return short_tiles(g) ? launch_tiles<TY, OUT, BX, kShortRows>(g, s) : launch_tiles<TY, OUT, BX, kGT>(g, s);
 }
 
 template <int TY>
@@ -702,12 +833,12 @@ hipError_t launch_dw(const GroupedArgs& g, hipStream_t s) {
   hipError_t e = prepare(grouped_dw_mfma_kernel<TY>, once);
   if (e != hipSuccess) return e;
   const int tiles = dw_tiles(g);
-  const Split split = split_of(tiles, dw_stages(g), g.partial != nullptr ? split_room(tiles, dw_stages(g)) : SplitRoom{0, 0});
+  const Split split = split_of(tiles, dw_stages(g), kGT, g.partial != nullptr ? split_room(tiles, dw_stages(g), kGT) : SplitRoom{0, 0});
   const int pieces = split.whole + (tiles - split.whole) * split.parts;
   grouped_dw_mfma_kernel<TY><<<dim3(pieces < kWorkgroups ? pieces : kWorkgroups), dim3(256), kRingBytes, s>>>(g, tiles, split);
   e = hipGetLastError();
   if (e != hipSuccess || split.whole == tiles || split.cols) return e;
-  grouped_join_kernel<TY, TY, true, true><<<dim3(tiles - split.whole, 16), dim3(256), 0, s>>>(g, tiles, split);
+  grouped_join_kernel<TY, TY, true, true, kGT><<<dim3(tiles - split.whole, 16), dim3(256), 0, s>>>(g, tiles, split);
   return hipGetLastError();
 }
 
@@ -732,9 +863,12 @@ hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hip
   return b_along ? launch_rows<kElemF16, kElemF16, false>(g, s) : launch_rows<kElemF16, kElemF16, true>(g, s);
 }
 
-size_t grouped_split_bytes(const GroupedArgs& g, int type) { return (size_t)(split_room(most_tiles(g), row_stages(g, type)).parts * kPartialBytes); }
+size_t grouped_split_bytes(const GroupedArgs& g, int type) {
+  const int BM = short_tiles(g) ? kShortRows : kGT;
+  return (size_t)(rows_room(g, type, BM).parts * (kPartialBytes / kGT * BM));
+}
 size_t grouped_dw_split_bytes(const GroupedArgs& g) {
-  const Split s = split_of(dw_tiles(g), dw_stages(g), split_room(dw_tiles(g), dw_stages(g)));
+  const Split s = split_of(dw_tiles(g), dw_stages(g), kGT, split_room(dw_tiles(g), dw_stages(g), kGT));
   return (size_t)((s.cols ? 0 : dw_tiles(g) - s.whole) * s.parts * kPartialBytes);
 }
 
