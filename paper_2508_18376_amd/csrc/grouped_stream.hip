@@ -345,23 +345,24 @@ hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
 }  // namespace
 
 // Which calls these kernels take (all times: this path against the other one, us).
-//   16-bit types and 8-bit integers whose rows start on 16 bytes: up to 16 rows a group on average, 8 where 16-bit weights lie along the
-//     contraction.  Beyond, the tiles of grouped_mfma.hip, which read weights through LDS, are as fast: y = x W on 64 experts of 2048 x 1024 at 1 / 8
-//     / 16 rows 37 / 57 / 68 against 44 / 54 / 54, on 8 of 4096 x 14336 at 4 / 16 / 24 rows 133 / 163 / 196 against 171 / 182 / 184; gradient of x 32 / 53 /
-//     64 against 41 / 52 / 53 and 177 / 210 / 300 against 250 / 263 / 264; 8 bits 23 / 32 / 41 against 23 / 31 / 33 and 83 / 104 / 133 against 105 / 116 / 118.
+//   16-bit types and 8-bit integers whose rows start on 16 bytes, against the tiles of grouped_mfma.hip, which read weights through LDS: up to 12 rows
+//     a group on average, 2 where 16-bit weights lie along the contraction.  y = x W on 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 37 / 57 / 68
+//     against 37 / 54 / 55, on 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 62 / 77 against 71 / 74 / 76, on 8 of 4096 x 14336 at 4 / 16 rows 133 / 164 against
+//     138 / 166; gradient of x on the first 32 / 53 / 57 against 38 / 53 / 54, on the last at 4 / 16 rows 178 / 210 against 146 / 190; 8 bits on the first
+//     23 / 32 / 41 against 24 / 33 / 35, on the last 83 / 105 against 94 / 113.
 //     Few pieces of long sums keep too few compute units busy, which split tiles do not: 16 rows of 14336 values, 4096 columns 66 against 38;
 //     of 4096 values, 4096 columns 16 against 19.5.
-//   Rows that start elsewhere, against grouped_plain.hip: the same, and few tiles across: 256 rows, 1001 x 1409 in one group 12.6 against 19.8, 512
+//   Rows that start elsewhere, against grouped_plain.hip: up to 16 rows a group (8 along), and few tiles across: 256 rows, 1001 x 1409 in one group 12.6 against 19.8, 512
 //     rows 22 against 20.
 //   fp32, against grouped_plain.hip: up to 128 rows a group, or tiles that do not fill the card: 16 experts of 2048 x 1408 at 64 / 96 / 128 / 192
 //     rows 100 / 122 / 149 / 203 against 144 / 147 / 213 / 256; 64 / 256 / 512 rows of 4096 x 4096 in one group 52 / 100 / 187 against 276 / 283 / 282.
 bool grouped_stream_sizes(const GroupedArgs& g, int type, bool b_along, bool tiles_fit) {
   const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 127) / 128);
   if (type == kElemF32) return g.R <= 128 * (int64_t)g.G || tiles < 400;
-  const bool few = g.R <= (b_along && type != kElemI8 ? 8 : 16) * (int64_t)g.G;
-  if (!tiles_fit) return few || (!b_along && tiles < 64);
+  if (!tiles_fit) return g.R <= (b_along && type != kElemI8 ? 8 : 16) * (int64_t)g.G || (!b_along && tiles < 64);
+  const bool few = g.R <= (b_along && type != kElemI8 ? 2 : 12) * (int64_t)g.G;
   const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
-  return few && (pieces >= 128 || (int64_t)g.K * elem_bytes(type) <= 16384);
+  return few && ((int64_t)g.K * elem_bytes(type) <= 16384 || (!b_along && pieces >= 128));
 }
 bool grouped_stream_fits(const GroupedArgs& g, int type, bool b_along) {
   const int64_t most = (int64_t)1 << 24;  // 64 rows of it are below 2^32
