@@ -48,31 +48,26 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
-// The row space falls into G + 2 segments: rows before the first group, the groups, rows after the last one.  The first and
-// the last have no weights: their rows of C are zero.  Offsets outside [0, R] count as its ends and an offset below an earlier one as that
-// one, so that whatever the table holds, the segments are disjoint and cover the rows once.
-__device__ __forceinline__ int segment_bound(const int32_t* off, int G, int R, int i) {
-  if (i <= 0) return 0;
-  if (i > G + 1) return R;
-  return min(max(off[i - 1], 0), R);
-}
+// Where group i begins (i == G: where the last one ends).  Offsets outside [0, R] count as its ends and an offset below an earlier one as that one, so
+// that whatever the table holds, the groups are disjoint and inside.
+__device__ __forceinline__ int group_bound(const int32_t* off, int G, int R, int i) { return min(max(off[min(i, G)], 0), R); }
 
 struct Segment {
   int row0, rows;
-  int group;  // -1: no weights
-  int base;   // pieces of the segments before it
-  int total;  // pieces of all segments
+  int group;
+  int base;   // pieces of the groups before it
+  int total;  // pieces of all groups
 };
 
-// begin and end of segment s0 + lane; carry: the largest bound before s0, updated
+// begin and end of group s (of lane s mod 64; none beyond the last one); carry: the largest bound before the first lane's, updated
 __device__ __forceinline__ void lane_segment(const int32_t* off, int G, int R, int s, int& carry, int& begin, int& end) {
-  const int b = segment_bound(off, G, R, s), e = segment_bound(off, G, R, s + 1);
+  const int b = group_bound(off, G, R, s), e = group_bound(off, G, R, s + 1);
   begin = max(wave_scan<true>(b), carry);
   end = max(begin, e);
   carry = __builtin_amdgcn_readlane(end, 63);
 }
 
-// The segments' rows and pieces.  Up to 64 segments: worked out once and kept, one to a lane; more: again for each lookup.
+// The groups' rows and pieces.  Up to 64 groups: worked out once and kept, one to a lane; more: again for each lookup.
 struct Segments {
   const int32_t* off;
   int G, R, begin, end;
@@ -83,9 +78,9 @@ struct Segments {
     int carry = 0;
     begin = 0;
     end = R;
-    if (off != nullptr && G + 2 <= 64) lane_segment(off, G, R, threadIdx.x & 63, carry, begin, end);
+    if (off != nullptr && G <= 64) lane_segment(off, G, R, threadIdx.x & 63, carry, begin, end);
   }
-  // pieces: per_tile for each BM rows of a segment.  pick(total) says which piece this workgroup takes.
+  // pieces: per_tile for each BM rows of a group.  pick(total) says which piece this workgroup takes.
   template <class Pick>
   __device__ __forceinline__ bool find(int BM, int per_tile, Pick&& pick, int& piece, Segment& s) const {
     if (off == nullptr) {
@@ -93,7 +88,7 @@ struct Segments {
       piece = pick(s.total);
       return piece < s.total;
     }
-    const int lane = threadIdx.x & 63, n = G + 2;
+    const int lane = threadIdx.x & 63, n = G;
     int b = begin, e = end, total = 0, carry = 0, scan = 0;
     for (int s0 = 0; s0 < n; s0 += 64) {
       if (n > 64) lane_segment(off, G, R, s0 + lane, carry, b, e);
@@ -115,7 +110,7 @@ struct Segments {
         const int l = __builtin_ctzll(beyond), q = s0 + l;
         s.row0 = __builtin_amdgcn_readlane(b, l);
         s.rows = __builtin_amdgcn_readlane(e, l) - s.row0;
-        s.group = q >= 1 && q <= G ? q - 1 : -1;
+        s.group = q;
         s.base = base + __builtin_amdgcn_readlane(scan, l) - (s.rows + BM - 1) / BM * per_tile;
         return true;
       }
@@ -127,20 +122,38 @@ struct Segments {
   __device__ __forceinline__ void group(int g, int& row0, int& rows) const {
     int b = begin, e = end, carry = 0, l = 0;
     if (off != nullptr) {
-      l = (g + 1) & 63;
-      if (G + 2 > 64)
-        for (int s0 = 0; s0 <= g + 1; s0 += 64) lane_segment(off, G, R, s0 + (threadIdx.x & 63), carry, b, e);
+      l = g & 63;
+      if (G > 64)
+        for (int s0 = 0; s0 <= g; s0 += 64) lane_segment(off, G, R, s0 + (threadIdx.x & 63), carry, b, e);
     }
     row0 = __builtin_amdgcn_readlane(b, l);
     rows = __builtin_amdgcn_readlane(e, l) - row0;
+  }
+  // zeros in the rows of C that no group has: before the first one and after the last one, dealt out to the workgroups
+  __device__ __forceinline__ void zero_others(char* c, int64_t c_row, int row_bytes) const {
+    if (off == nullptr) return;
+    int b = begin, e = end, carry = 0;
+    if (G > 64)
+      for (int s0 = 0; s0 < G; s0 += 64) lane_segment(off, G, R, s0 + (threadIdx.x & 63), carry, b, e);
+    const int first = group_bound(off, G, R, 0), last = __builtin_amdgcn_readlane(e, 63), n = first + R - last;
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+      char* row = c + (i < first ? i : last + i - first) * c_row;
+      for (int j = threadIdx.x * 16; j < row_bytes; j += blockDim.x * 16) {
+        const uint32_t zeros[4] = {0, 0, 0, 0};
+        if (j + 16 <= row_bytes)
+          __builtin_memcpy(row + j, zeros, 16);
+        else
+          for (int k = j; k < row_bytes; k += 2) *(uint16_t*)(row + k) = 0;
+      }
+    }
   }
 };
 
 // most row tiles of BM rows that R rows in G groups can give
 inline int64_t row_tiles_bound(int64_t R, int64_t G, bool grouped, int BM) {
   if (!grouped) return (R + BM - 1) / BM;
-  const int64_t segments = G + 2 < R ? G + 2 : R;
-  return (R - segments) / BM + segments;
+  const int64_t groups = G < R ? G : R;
+  return (R - groups) / BM + groups;
 }
 
 // The piece of n that place b takes (n: none): take_piece without the free ones, for workgroups that take several.
@@ -150,7 +163,7 @@ __device__ __forceinline__ int piece_of(int b, int n) {
   return base + x * q + min(x, r) + i;
 }
 
-// Inside a segment the pieces go in bands of 8 row tiles, column tile by column tile: 32 neighbours (what an XCD gets at a time, see take_piece)
+// Inside a group the pieces go in bands of 8 row tiles, column tile by column tile: 32 neighbours (what an XCD gets at a time, see take_piece)
 // share 8 row tiles and 4 column tiles.
 constexpr int kBand = 8;
 __device__ __forceinline__ void band_tile(int id, int row_tiles, int col_tiles, int& rt, int& ct) {

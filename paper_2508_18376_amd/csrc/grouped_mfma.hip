@@ -339,11 +339,27 @@ __device__ __forceinline__ void tile_shape(int m_edge, int n_edge, bool across, 
   wn = tall ? (w >> 1) * 32 * ni : w * 64;
 }
 
-// Stores a tile's sums, of which this wavefront has rows wm .. + 32 MI and columns wn .. + 32 NI.  turn: 32 rows of 64 NI bytes of LDS of its own; inside:
-// all rows and columns exist.
+// The factors of an 8-bit tile: of row lane % 32 of each 32, and of the four columns that the lane stores of each 64.  They are loaded before the
+// next tile's first units: vector memory comes back in order, and behind those (and one by one, where they are used) they cost an 8-bit
+// product of 6007 x 1024 x 2048 half its time.
+template <bool I8, int MI, int NI>
+struct Factors {
+  float rows[I8 ? MI : 1], cols[I8 ? NI / 2 : 1][4];
+  __device__ __forceinline__ void load(const Piece& p, int wm, int wn, int lane) {
+    if constexpr (I8) {
+#pragma unroll
+      for (int a = 0; a < MI; ++a) rows[a] = p.as[min(wm + a * 32 + (lane & 31), p.m_edge - 1)];
+#pragma unroll
+      for (int b = 0; b < NI / 2; ++b) __builtin_memcpy(cols[b], p.bs + min(wn + b * 64 + (lane & 15) * 4, p.n_edge - 4), 16);
+    }
+  }
+};
+
+// Stores a tile's sums, of which this wavefront has rows wm .. + 32 MI and columns wn .. + 32 NI.  turn: kTurnBytes of LDS of its own; inside: all rows and
+// columns exist.
 template <int TY, int OUT, int MI, int NI>
-__device__ __forceinline__ void write_tile(const GroupedArgs& g, const Piece& p, const typename AccType<TY>::type (&acc)[MI][NI], char* turn, int wm, int wn,
-                                           int w, int lane, bool inside) {
+__device__ __forceinline__ void write_tile(const GroupedArgs& g, const Piece& p, const typename AccType<TY>::type (&acc)[MI][NI],
+                                           const Factors<TY == kElemI8, MI, NI>& factors, char* turn, int wm, int wn, int w, int lane, bool inside) {
   if (p.partial != nullptr) {  // in the order of the registers: the second launch knows where they belong
     char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
 #pragma unroll
@@ -360,61 +376,59 @@ __device__ __forceinline__ void write_tile(const GroupedArgs& g, const Piece& p,
         }
     return;
   }
-  // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.
-  const int r32 = lane & 31, half = lane >> 5;
-  auto value = [&](int a, int b, int v, float as, const float* bs) __attribute__((always_inline)) -> float {
-    if constexpr (TY == kElemI8)
-      return (float)acc[a][b][v] * as * bs[v & 3];
-    else
-      return acc[a][b][v];
-  };
+  // A lane has, of each 32 x 32 block, row lane % 32 and for q = 0 .. 3 the columns 8 q + 4 (lane / 32) .. + 3.  Each wavefront turns 32 rows of NB blocks
+  // at a time around in LDS, rows of up to 256 bytes whose 16-byte chunks are rotated by the row, and stores 16 bytes a lane (8-bit products: four
+  // values).  Those go through LDS as they are: converted before it, the compiler holds all 256 sums in ordinary registers and parks some in scratch
+  // memory.
+  constexpr bool WORDS = OUT == kElemF32 || TY == kElemI8;  // 32 bits a value in LDS
+  constexpr int NB = WORDS ? 2 : NI, LPR = NB * (WORDS ? 8 : 4), PER = WORDS ? 4 : 8;  // chunks of a row; values of a chunk
+  const int r32 = lane & 31, half = lane >> 5, ch = lane % LPR;
 #pragma unroll
-  for (int a = 0; a < MI; ++a) {
-    const int r = wm + a * 32 + r32;
-    const float as = TY == kElemI8 && p.K > 0 && r < p.m_edge ? p.as[r] : 0.f;
-    // 16 bits: each wavefront turns 32 rows at a time around in its part of the fifth unit and stores 16 bytes a lane, rows of 64 NI
-    // bytes; their 16-byte chunks are rotated by the row
-    constexpr int LPR = NI * 4;  // chunks of a row
+  for (int a = 0; a < MI; ++a)
 #pragma unroll
-    for (int b = 0; b < NI; ++b)
+    for (int b0 = 0; b0 < NI; b0 += NB) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = wn + b * 32 + 8 * q + 4 * half;
-        float bs[4] = {0, 0, 0, 0};
-        if (TY == kElemI8 && p.K > 0 && c < p.n_edge) __builtin_memcpy(bs, p.bs + c, 16);
-        float v[4];
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = value(a, b, 4 * q + e, as, bs);
-        if constexpr (OUT == kElemF32) {
-          if (r < p.m_edge && c < p.n_edge) *(gf32x4*)(p.pc + r * g.c_row + (int64_t)c * 4) = gf32x4{v[0], v[1], v[2], v[3]};
-        } else {
-          *(uint2*)(turn + r32 * (LPR * 16) + (((b * 4 + q) ^ (r32 & (LPR - 1))) * 16) + half * 8) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
+        for (int q = 0; q < 4; ++q) {
+          const auto& c = acc[a][b0 + b];
+          char* row = turn + r32 * (LPR * 16);
+          if constexpr (WORDS) {
+            typedef decltype(c[0] + c[0]) value_t;
+            typedef value_t value4 __attribute__((ext_vector_type(4)));
+            *(value4*)(row + ((b * 8 + q * 2 + half) ^ (r32 & (LPR - 1))) * 16) = value4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+          } else {
+            *(uint2*)(row + ((b * 4 + q) ^ (r32 & (LPR - 1))) * 16 + half * 8) =
+                make_uint2(pack2<OUT>(c[4 * q], c[4 * q + 1]), pack2<OUT>(c[4 * q + 2], c[4 * q + 3]));
+          }
         }
-      }
-    if constexpr (OUT != kElemF32) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const int ch = lane % LPR;
-      if (MI == 4 && NI == 4 && inside) {
+      const int c = wn + b0 * 32 + ch * PER;
 #pragma unroll
-        for (int k = 0; k < 32 * LPR / 64; ++k) {
-          const int rr = k * (64 / LPR) + lane / LPR;
-          const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
-          *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
-        }
-      } else {
+      for (int k = 0; k < 32 * LPR / 64; ++k) {
+        const int rr = k * (64 / LPR) + lane / LPR, r = wm + a * 32 + rr;
+        const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
+        char* to = p.pc + r * g.c_row + (int64_t)c * elem_bytes(OUT);
+        const bool there = (MI == 4 && NI == 4 && inside) || (r < p.m_edge && c < p.n_edge);
+        if constexpr (TY == kElemI8) {
+          const float as = __shfl(factors.rows[a], rr);
+          float f[4];
 #pragma unroll
-        for (int k = 0; k < 32 * LPR / 64; ++k) {
-          const int rr = k * (64 / LPR) + lane / LPR;
-          const gi32x4 v = *(const gi32x4*)(turn + rr * (LPR * 16) + (ch ^ (rr & (LPR - 1))) * 16);
-          if (wm + a * 32 + rr < p.m_edge && wn + ch * 8 < p.n_edge)
-            *(gi32x4*)(p.pc + (wm + a * 32 + rr) * g.c_row + (int64_t)(wn + ch * 8) * 2) = v;
+          for (int e = 0; e < 4; ++e) f[e] = (float)v[e] * as * factors.cols[b0 / 2][e];
+          if (there) {
+            if constexpr (OUT == kElemF32)
+              *(gf32x4*)to = gf32x4{f[0], f[1], f[2], f[3]};
+            else
+              *(uint2*)to = make_uint2(pack2<OUT>(f[0], f[1]), pack2<OUT>(f[2], f[3]));
+          }
+        } else if (there) {
+          *(gi32x4*)to = v;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
-  }
 }
 
 // The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
@@ -491,10 +505,12 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       tile.rb.init(ring, wn, lane);
       const int n = stages(p);
       tile.run(n, load_a, load_b, one_a, one_b);
+      Factors<TY == kElemI8, MI, NI> factors;
+      if (p.partial == nullptr && n > 0) factors.load(p, wm, wn, lane);
       stage_barrier();
       if (more) first_units(nxt);
       stores_behind = MI == 4 && NI == 4 && TY != kElemI8 && p.partial == nullptr && p.m_edge == kGT && p.n_edge == kGT;
-      write_tile<TY, OUT, MI, NI>(g, p, tile.acc, lds + 4 * kUnit + w * (kUnit / 4), wm, wn, w, lane, stores_behind);
+      write_tile<TY, OUT, MI, NI>(g, p, tile.acc, factors, lds + 4 * kUnit + w * (kUnit / 4), wm, wn, w, lane, stores_behind);
     };
     int mi, ni, wm, wn;
     tile_shape(p.m_edge, p.n_edge, AX, w, mi, ni, wm, wn);
@@ -610,9 +626,11 @@ __device__ __forceinline__ void do_short_pieces(const GroupedArgs& g, char* lds,
           if (st + 4 < n) load(st + 4, n);
         }
       }
+      Factors<TY == kElemI8, MI, NI> factors;
+      if (p.partial == nullptr) factors.load(p, 0, wn, lane);
       stage_barrier();
       if (more) first_stages(nxt);
-      write_tile<TY, OUT, MI, NI>(g, p, acc, lds + 3 * kShortStage + w * (kShortStage / 4), 0, wn, w, lane, false);
+      write_tile<TY, OUT, MI, NI>(g, p, acc, factors, lds + 3 * kShortStage + w * (kShortStage / 4), 0, wn, w, lane, false);
     };
     if (p.m_edge > 32)
       whole(Const<2>());
@@ -643,7 +661,7 @@ struct RowsWork {
     if (!all.find(BM, NT, pick_tile, tile, s)) return false;
     int rt, nt;
     band_tile(tile - s.base, (s.rows + BM - 1) / BM, NT, rt, nt);
-    const int m0 = rt * BM, n0 = nt * kGT, grp = max(s.group, 0);
+    const int m0 = rt * BM, n0 = nt * kGT, grp = s.group;
     const int64_t row = s.row0 + m0;
     p.pa = g.a + row * g.a_row;
     p.pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * EB : n0 * g.b_row);
@@ -652,7 +670,7 @@ struct RowsWork {
     p.bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
     p.m_edge = min(BM, s.rows - m0);
     p.n_edge = min(kGT, g.N - n0);
-    p.K = s.group < 0 ? 0 : g.K;
+    p.K = g.K;
     p.partial = nullptr;
     if (tile >= split.whole && split.cols) {
       const int skip = part * kGT / 2;
@@ -680,6 +698,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
   extern __shared__ __align__(16) char ring[];
   RowsWork<TY, OUT, BX, BM> work;
   work.all.init(g.off, g.G, g.R);
+  work.all.zero_others(g.c, g.c_row, g.N * elem_bytes(OUT));
   auto next = [&](int i, Piece& p) __attribute__((always_inline)) {
     return work.find(g, p, [&](RowsWork<TY, OUT, BX, BM>& w) {
       int tile;

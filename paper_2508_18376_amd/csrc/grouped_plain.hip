@@ -195,14 +195,15 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
     Segment s;
     Segments all;
     all.init(g.off, g.G, g.R);
+    all.zero_others(g.c, g.c_row, g.N * elem_bytes(TY == kElemI8 ? g.out_type : TY));
     if (!all.find(kPT, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
     int rt, nt;
     band_tile(piece - s.base, (s.rows + kPT - 1) / kPT, NT, rt, nt);
     m0 = rt * kPT;
     n0 = BX ? last_tile(nt, g.N) : nt * kPT;
     m_edge = min(kPT, s.rows - m0);
-    K = s.group < 0 ? 0 : g.K;
-    const int grp = max(s.group, 0);
+    K = g.K;
+    const int grp = s.group;
     pa = g.a + (int64_t)(s.row0 + m0) * g.a_row;
     pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * E::bytes : n0 * g.b_row);
     pc = g.c;
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int r = mw + i * 32 + r32;
-    const float as = TY == kElemI8 && K > 0 && r < m_edge ? g.a_scale[c_row0 + m0 + r] : 1.f;
+    const float as = TY == kElemI8 && r < m_edge ? g.a_scale[c_row0 + m0 + r] : 1.f;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           v[e] = acc[i][j].get(4 * q + e);
-          if (TY == kElemI8) v[e] = K > 0 && nw + c + e < n_edge ? v[e] * as * b_scale[n0 + nw + c + e] : 0.f;
+          if (TY == kElemI8) v[e] = nw + c + e < n_edge ? v[e] * as * b_scale[n0 + nw + c + e] : 0.f;
         }
         if (out == kElemF32) {
           *(pf32x4*)(turn + r32 * 272 + c * 4) = pf32x4{v[0], v[1], v[2], v[3]};

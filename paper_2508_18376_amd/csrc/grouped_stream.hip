@@ -229,7 +229,7 @@ __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, con
   for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[r][j] = acc_t{0, 0, 0, 0};
-  if (K > 0) stream_tile<TY, BX, NR, J, W, ONCE>(g, pa, pb, rows, n0, cols, K, acc);
+  stream_tile<TY, BX, NR, J, W, ONCE>(g, pa, pb, rows, n0, cols, K, acc);
   // A lane's sums: row lane % 16 of sixteen; along: columns 16 j + 4 q .. + 3 from acc[.][j]; across: columns J (4 q + v) + j from acc[.][j][v].
   typedef uint32_t word4 __attribute__((ext_vector_type(4)));
   constexpr int COLS = 16 * J, RF = row_floats(J);
@@ -261,7 +261,7 @@ __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, con
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) sum += (int)at[w * (16 * RF)];
-        out[p] = K > 0 && rr < rows && col + p < cols ? (float)sum * as[rr] * bs[col + p] : 0.f;
+        out[p] = rr < rows && col + p < cols ? (float)sum * as[rr] * bs[col + p] : 0.f;
       } else {
         out[p] = 0.f;
 #pragma unroll
@@ -292,17 +292,18 @@ __global__ __launch_bounds__(64 * W, J == 8 ? 2 : 4) void grouped_stream_kernel(
   Segment s;
   Segments all;
   all.init(g.off, g.G, g.R);
+  all.zero_others(g.c, g.c_row, g.N * (OUT == kElemF32 ? 4 : 2));
   if (!all.find(kStreamTile, NT, [](int n) { return piece_of(blockIdx.x, n); }, piece, s)) return;
   int rt, nt;
   band_tile(piece - s.base, (s.rows + kStreamTile - 1) / kStreamTile, NT, rt, nt);
-  const int m0 = rt * kStreamTile, n0 = nt * COLS, grp = max(s.group, 0);
+  const int m0 = rt * kStreamTile, n0 = nt * COLS, grp = s.group;
   const int64_t row = s.row0 + m0;
   const char* pa = g.a + row * g.a_row;
   const char* pb = g.b + grp * g.b_group + (BX ? (int64_t)n0 * E::bytes : n0 * g.b_row);
   char* pc = g.c + row * g.c_row + (int64_t)n0 * (OUT == kElemF32 ? 4 : 2);
   const float* as = TY == kElemI8 ? g.a_scale + row : nullptr;
   const float* bs = TY == kElemI8 ? g.b_scale + grp * g.bs_group + n0 : nullptr;
-  const int rows = min(kStreamTile, s.rows - m0), cols = min(COLS, g.N - n0), K = s.group < 0 ? 0 : g.K;
+  const int rows = min(kStreamTile, s.rows - m0), cols = min(COLS, g.N - n0), K = g.K;
   if (rows <= 16)
     stream_rows<TY, OUT, BX, 1, J, W, ONCE>(g, lds, pa, pb, pc, as, bs, rows, n0, cols, K);
   else

@@ -35,6 +35,8 @@ __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* 
   top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
   const float s = __uint_as_float(top) / 127.f;
   const bool zero = s == 0.f || top >= 0x7f800000u;
+  // (a factor below 2^-125 has no finite reciprocal, or one that has lost bits: its quotients are all computed)
+  const float inv = s < 0x1p-120f ? 0.f : 1.f / s;
 #pragma unroll N
   for (int j = 0; j < n; ++j) {
     const int c = i0 + j * kRowThreads * 8, k = NCH ? j : 0;
@@ -43,8 +45,11 @@ __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* 
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int t = zero ? 0 : (int)fminf(fmaxf(rintf(v[k][e] / s), -127.f), 127.f);
-      w[e >> 2] |= (uint32_t)(t & 0xff) << (8 * (e & 3));
+      float t = v[k][e] * inv;
+      // within 2^-13 of a half the product with the reciprocal (off by less than 127 * 2^-22) may lie on the other side: there the quotient decides
+      if (inv == 0.f || fabsf(fabsf(t - rintf(t)) - 0.5f) < 1.f / 8192) t = v[k][e] / s;
+      const int i = zero ? 0 : (int)fminf(fmaxf(rintf(t), -127.f), 127.f);
+      w[e >> 2] |= (uint32_t)(i & 0xff) << (8 * (e & 3));
     }
     *(uint2*)(q + r * q_row + c) = make_uint2(w[0], w[1]);  // (rows of q are whole chunks, zeros behind K)
   }

@@ -71,6 +71,23 @@ def test_ties_signs_and_largest_values():
     assert y.cpu().tolist() == [[127, 0, 2, 2, 0, -2, -2, -127], [-127, 126, 126, -126, -126, 0, -1, 64]]
 
 
+@pytest.mark.parametrize("scale", [1.0, 1e-30, 1e-37, 3e-41, 1e37])
+def test_every_rounding_is_the_quotients(scale):
+    """Values on and next to the halves of a row's steps, at scales down to subnormal ones: q is round(x / s) of the fp32 quotient."""
+    from paper_2508_18376_amd import moe_int8_matmul
+    gen = torch.Generator().manual_seed(8)
+    half = (torch.randint(-127, 127, (64, 1024), generator=gen) + 0.5) / 127
+    x = (half * (1 + torch.randint(-3, 4, half.shape, generator=gen) * 2.0 ** -24) * torch.rand(64, 1, generator=gen).add(0.5)).float()
+    x[:, 0] = x.abs().amax(1) * 1.004
+    x = x * scale
+    s = x.abs().amax(1) / 127
+    q = torch.where(s[:, None] > 0, torch.round(x / s[:, None]).clamp(-127, 127), torch.zeros_like(x))
+    w = torch.zeros(1, 1024, 1024, dtype=torch.int8)
+    w[0, torch.arange(1024), torch.arange(1024)] = 1
+    y = moe_int8_matmul(x.to(DEV), w.to(DEV), torch.ones(1, 1024, device=DEV)).cpu()
+    assert torch.equal(y, q * s[:, None])
+
+
 def test_largest_sums_are_exact():
     from paper_2508_18376_amd import moe_int8_matmul
     k = 1 << 17
