@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(BlockNormArgs a) {
 // varies inside the row, and d = dy + u / rms(y),
 //   sum of q dx = sum of q d - (sum of u y' / (d rms(y))) * sum of q y'
 // so one exchange between the wavefronts gives all three.  The next row's values are on their way while this one is worked on: without that and with
-// two exchanges 8192 rows of 4096 took 145 us, two thirds of it waiting.
+// two exchanges 8192 rows of 4096 took 145 us; now 84.
 // A last chunk that is not whole is the row's last 8 values: what it has in common with the chunk before it comes out the same in both, and only
 // counts once in the sums.
 template <int TY>
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(1024) void block_norm_columns_kernel(BlockNormArgs 
 }
 
 // Rows of the partial table: as many sets of threads as the card holds of the kernel, but at least four rows each, so that the table does not become
-// the larger part of what is written (1001 rows of 2047: 1001 sets 24 us, 256 sets 14).
+// the larger part of what is written (1001 rows of 2047, both launches: 1001 sets 21.5 us, 256 sets 19.3).
 inline int backward_threads(int D) { return D <= 512 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
 inline int partial_sets(int T, int D) {
   if (D > 8192) return T < 256 ? T : 256;

@@ -268,8 +268,10 @@ struct Piece {
 // the tiles beyond whole rounds of 256 are cut where that pays: into two halves of their columns, which take 0.6 of a tile's time each, or along the
 // contraction into `parts` pieces of work, whose sums go to a workspace as they are and which a second launch adds up in order.  A
 // stage of 128 bytes takes about 1.2 us, a partial tile's way out and back about 0.1 us of the whole card's bandwidth, the second launch 5 us:
-// the least sum of these decides.  (8192 rows on 8 experts, y = x W^T with 4096 columns and 14336 values to sum: 576 tiles, the last 64 in 4
-// parts, 936 -> 824 us; 65536 rows on 64 experts of 2048 x 1024: 1152 tiles, the last 128 in halves.)
+// the least sum of these decides.  (8192 rows on 8 experts, along the contraction: 14336 x 4096, y = x W 956 -> 872 us; 4096 x 14336, dy W^T
+// 964 -> 868.  Halves: 20000 rows of 1024 x 1024 61 -> 54, 2000 of 4096 x 4096 in 8 bits 66 -> 55, 5000 of 1024 x 4096 58 -> 52; over many ragged groups,
+// where tiles differ anyway, they come out within 1 % of whole tiles.)
+constexpr int kHalvesFrom = 96;  // rows of a tile on average; see split_of
 struct Split {
   int whole;  // tiles that are not cut
   int parts;  // of each of the others (1: none is)
@@ -283,7 +285,7 @@ __host__ __device__ inline Split split_of(int tiles, int stages, int rows, const
   Split s = {tiles, 1, 0};
   if (rest == 0 || 2 * rest > kWorkgroups) return s;
   int least = 12 * stages - 50;
-  if (rows > kGT / 2) {
+  if (rows > kHalvesFrom) {
     s = Split{tiles - rest, 2, 1};
     least = 36 * stages / 5 - 50;
   }
@@ -301,7 +303,7 @@ __host__ __device__ inline Split split_of(int tiles, int stages, int rows, const
 // cost has: sqrt(12 stages / tiles * 256 / rows).
 inline SplitRoom split_room(int64_t most_tiles, int stages, int rows) {
   if (stages < 9) return SplitRoom{0, 0};
-  const double share = rows < kGT ? rows < 1 ? 1. / kGT : (double)rows / kGT : 1., gain = (rows > kGT / 2 ? 7.2 : 12.) * stages - 50;
+  const double share = rows < kGT ? rows < 1 ? 1. / kGT : (double)rows / kGT : 1., gain = (rows > kHalvesFrom ? 7.2 : 12.) * stages - 50;
   int64_t rest = (int64_t)(gain * gain / (48. * stages * share)) + 1;
   if (rest > kWorkgroups / 2) rest = kWorkgroups / 2;
   if (rest > most_tiles) rest = most_tiles;
@@ -340,8 +342,8 @@ __device__ __forceinline__ void tile_shape(int m_edge, int n_edge, bool across, 
 }
 
 // The factors of an 8-bit tile: of row lane % 32 of each 32, and of the four columns that the lane stores of each 64.  They are loaded before the
-// next tile's first units: vector memory comes back in order, and behind those (and one by one, where they are used) they cost an 8-bit
-// product of 6007 x 1024 x 2048 half its time.
+// next tile's first units: vector memory comes back in order, behind those (and one by one, where they are used) the products of an 8-bit
+// call of 6007 x 1024 x 2048 took 34 us instead of 27.
 template <bool I8, int MI, int NI>
 struct Factors {
   float rows[I8 ? MI : 1], cols[I8 ? NI / 2 : 1][4];
@@ -433,7 +435,7 @@ __device__ __forceinline__ void write_tile(const GroupedArgs& g, const Piece& p,
 
 // The workgroup's pieces, one after the other.  piece(i, p): its i-th one, false if there is none.
 // While a tile's values leave through the fifth unit of the ring, the next tile's first four units are under way.
-template <int TY, int OUT, bool AX, bool BX, class Next>
+template <int TY, int OUT, bool AX, bool BX, int BM, class Next>
 __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&& piece) {
   constexpr int EB = GElem<TY>::bytes;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -514,12 +516,18 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
     };
     int mi, ni, wm, wn;
     tile_shape(p.m_edge, p.n_edge, AX, w, mi, ni, wm, wn);
-    if (mi == 4 && ni == 4) {
-      Tile<TY, AX, BX, 4, 4> t;
-      whole(t, wm, wn, Const<4>(), Const<4>());
-    } else if (mi == 4) {
-      Tile<TY, AX, BX, 4, 2> t;
-      whole(t, wm, wn, Const<4>(), Const<2>());
+    bool done = false;
+    if constexpr (BM == kGT) {
+      done = mi == 4;
+      if (mi == 4 && ni == 4) {
+        Tile<TY, AX, BX, 4, 4> t;
+        whole(t, wm, wn, Const<4>(), Const<4>());
+      } else if (mi == 4) {
+        Tile<TY, AX, BX, 4, 2> t;
+        whole(t, wm, wn, Const<4>(), Const<2>());
+      }
+    }
+    if (done) {
     } else if (ni == 4) {
       Tile<TY, AX, BX, 2, 4> t;
       whole(t, wm, wn, Const<2>(), Const<4>());
@@ -708,7 +716,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mfma_kernel(GroupedArgs g) {
   if constexpr (BM == kShortRows)
     do_short_pieces<TY, OUT, BX>(g, ring, next);
   else
-    do_pieces<TY, OUT, false, BX>(g, ring, next);
+    do_pieces<TY, OUT, false, BX, BM>(g, ring, next);
 }
 
 // dW = X^T dY.  The groups' rows differ; what is split is split for all of them alike.
@@ -747,7 +755,7 @@ __global__ __launch_bounds__(256, 1) void grouped_dw_mfma_kernel(GroupedArgs g, 
   extern __shared__ __align__(16) char ring[];
   Segments all;
   all.init(g.off, g.G, g.R);
-  do_pieces<TY, TY, true, true>(g, ring, [&](int i, Piece& p) {
+  do_pieces<TY, TY, true, true, kGT>(g, ring, [&](int i, Piece& p) {
     int tile, part;
     if (!work_of(split, tiles, blockIdx.x, i, tile, part)) return false;
     DwWork<TY>::find(g, all, split, tile, part, p);
@@ -818,9 +826,16 @@ hipError_t prepare(K kernel, PerDeviceOnce& once) {
 }
 
 inline int row_stages(const GroupedArgs& g, int type) { return (int)(((int64_t)g.K * elem_bytes(type) + 127) / 128); }
-// Up to 64 rows a group on average: tiles of 64 rows.
-inline bool short_tiles(const GroupedArgs& g) { return g.R <= 64 * (int64_t)g.G; }
 inline int64_t most_tiles(const GroupedArgs& g, int BM) { return row_tiles_bound(g.R, g.G, g.off != nullptr, BM) * ((g.N + kGT - 1) / kGT); }
+// Rows of a tile: 64 up to 64 rows a group on average (128 tokens on 8 experts of 4096 x 14336: 188 us with tiles of 256 rows, 169 with these); 128 where
+// tiles of 256 would keep little of the card busy and the sums are too short to be split far (dy W^T of 1319 rows, 3 groups of 1024 x 2048: 30 us with 256
+// rows, 25 with 128; 500 rows of 4096 x 4096 in 8 bits 41 and 34; y = x W of 1024 rows, 2 groups of 14336 x 4096: 134 and 230, so those keep 256; so do
+// 4096 rows, 3 groups of 1024 x 2048, 128 tiles: 33 and 37).
+inline int tile_rows(const GroupedArgs& g, int type) {
+  if (g.R <= 64 * (int64_t)g.G) return kShortRows;
+  const int64_t tiles = ((int64_t)g.R + kGT - 1) / kGT * ((g.N + kGT - 1) / kGT);
+  return tiles <= kWorkgroups * 3 / 8 && row_stages(g, type) <= 48 ? 128 : kGT;
+}
 inline SplitRoom rows_room(const GroupedArgs& g, int type, int BM) {
   const int64_t tiles = most_tiles(g, BM);
   return split_room(tiles, row_stages(g, type), (int)((int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1)));
@@ -843,7 +858,8 @@ hipError_t launch_tiles(GroupedArgs g, hipStream_t s) {
 }
 template <int TY, int OUT, bool BX>
 hipError_t launch_rows(const GroupedArgs& g, hipStream_t s) {
-  return short_tiles(g) ? launch_tiles<TY, OUT, BX, kShortRows>(g, s) : launch_tiles<TY, OUT, BX, kGT>(g, s);
+  const int rows = tile_rows(g, TY);
+  return rows == kShortRows ? launch_tiles<TY, OUT, BX, kShortRows>(g, s) : rows == 128 ? launch_tiles<TY, OUT, BX, 128>(g, s) : launch_tiles<TY, OUT, BX, kGT>(g, s);
 }
 
 template <int TY>
@@ -883,7 +899,7 @@ hipError_t launch_grouped_mfma(const GroupedArgs& g, int type, bool b_along, hip
 }
 
 size_t grouped_split_bytes(const GroupedArgs& g, int type) {
-  const int BM = short_tiles(g) ? kShortRows : kGT;
+  const int BM = tile_rows(g, type);
   return (size_t)(rows_room(g, type, BM).parts * (kPartialBytes / kGT * BM));
 }
 size_t grouped_dw_split_bytes(const GroupedArgs& g) {

@@ -10,36 +10,39 @@ namespace dsmoe {
 
 namespace {
 
-// One row a workgroup.  NCH chunks of 8 values a thread stay in registers between the maximum and the rounding; NCH == 0: the row is read
+// TPR threads a row (a wavefront or a workgroup).  NCH chunks of 8 values a thread stay in registers between the maximum and the rounding; NCH == 0: the row is read
 // twice.  The maximum is that of the bits without the sign, so a NaN or an infinity comes out on top: the row's factor is then not finite
 // and its values are set to zero, which makes its outputs NaN.  A row whose factor is zero has q = 0.
-template <int TY, int NCH>
-__global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* x, int64_t x_row, int K, int8_t* q, int64_t q_row, float* scale) {
+template <int TY, int TPR, int NCH>
+__global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* x, int64_t x_row, int R, int K, int8_t* q, int64_t q_row, float* scale) {
   __shared__ uint32_t lds[4];
   constexpr int N = NCH ? NCH : 1;
-  const int64_t r = blockIdx.x;
-  const int i0 = threadIdx.x * 8, n = NCH ? NCH : (int)((q_row + kRowThreads * 8 - 1) / (kRowThreads * 8));
+  const int64_t r = (int64_t)blockIdx.x * (kRowThreads / TPR) + threadIdx.x / TPR;
+  if (r >= R) return;  // (whole wavefronts)
+  const int i0 = threadIdx.x % TPR * 8, n = NCH ? NCH : (int)((q_row + TPR * 8 - 1) / (TPR * 8));
   float v[N][8];
   uint32_t top = 0;
 #pragma unroll N
   for (int j = 0; j < n; ++j) {
-    const int c = i0 + j * kRowThreads * 8, k = NCH ? j : 0;
+    const int c = i0 + j * TPR * 8, k = NCH ? j : 0;
     load8<TY>(x, r * x_row + c, K - c, v[k]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[k][e]) & 0x7fffffffu);
   }
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+  if (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+  }
   const float s = __uint_as_float(top) / 127.f;
   const bool zero = s == 0.f || top >= 0x7f800000u;
   // (a factor below 2^-125 has no finite reciprocal, or one that has lost bits: its quotients are all computed)
   const float inv = s < 0x1p-120f ? 0.f : 1.f / s;
 #pragma unroll N
   for (int j = 0; j < n; ++j) {
-    const int c = i0 + j * kRowThreads * 8, k = NCH ? j : 0;
+    const int c = i0 + j * TPR * 8, k = NCH ? j : 0;
     if (c >= q_row) continue;
     if (!NCH) load8<TY>(x, r * x_row + c, K - c, v[k]);
     uint32_t w[2] = {0, 0};
@@ -53,20 +56,31 @@ __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* 
     }
     *(uint2*)(q + r * q_row + c) = make_uint2(w[0], w[1]);  // (rows of q are whole chunks, zeros behind K)
   }
-  if (threadIdx.x == 0) scale[r] = s;
+  if (i0 == 0) scale[r] = s;
 }
 
+template <int TY, int TPR, int NCH>
+void launch_quantize(const Int8Args& a, int8_t* q, int64_t q_row, float* scale, hipStream_t s) {
+  const int rows = kRowThreads / TPR;
+  quantize_rows_kernel<TY, TPR, NCH><<<dim3((unsigned)((a.R + rows - 1) / rows)), dim3(kRowThreads), 0, s>>>(a.x, a.x_row, a.R, a.K, q, q_row, scale);
+}
+
+// Many short rows: a wavefront each, since half of a workgroup would have nothing (whole product, 1024 columns: 6007 rows of 1024 29 -> 27 us, 2101 of
+// 512 16.3 -> 14.3; rows of 2048 values 22 -> 24, so those keep a workgroup).
 template <int TY>
 hipError_t quantize(const Int8Args& a, int8_t* q, int64_t q_row, float* scale, hipStream_t s) {
-  const dim3 grid((unsigned)a.R), block(kRowThreads);
-  if (a.K <= 2048)
-    quantize_rows_kernel<TY, 1><<<grid, block, 0, s>>>(a.x, a.x_row, a.K, q, q_row, scale);
+  if (a.R >= 512 && a.K <= 512)
+    launch_quantize<TY, 64, 1>(a, q, q_row, scale, s);
+  else if (a.R >= 512 && a.K <= 1024)
+    launch_quantize<TY, 64, 2>(a, q, q_row, scale, s);
+  else if (a.K <= 2048)
+    launch_quantize<TY, kRowThreads, 1>(a, q, q_row, scale, s);
   else if (a.K <= 4096)
-    quantize_rows_kernel<TY, 2><<<grid, block, 0, s>>>(a.x, a.x_row, a.K, q, q_row, scale);
+    launch_quantize<TY, kRowThreads, 2>(a, q, q_row, scale, s);
   else if (a.K <= 16384)
-    quantize_rows_kernel<TY, 8><<<grid, block, 0, s>>>(a.x, a.x_row, a.K, q, q_row, scale);
+    launch_quantize<TY, kRowThreads, 8>(a, q, q_row, scale, s);
   else
-    quantize_rows_kernel<TY, 0><<<grid, block, 0, s>>>(a.x, a.x_row, a.K, q, q_row, scale);
+    launch_quantize<TY, kRowThreads, 0>(a, q, q_row, scale, s);
   return hipGetLastError();
 }
 
