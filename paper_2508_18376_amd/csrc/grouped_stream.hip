@@ -345,22 +345,29 @@ hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Which calls these kernels take (all times: this path against the other one, us).
+// Which calls these kernels take (all times: this path against the other one, us; rows are those of each group).
 //   16-bit types and 8-bit integers whose rows start on 16 bytes, against the tiles of grouped_mfma.hip, which read weights through LDS: up to 12 rows
-//     a group on average, 2 where 16-bit weights lie along the contraction.  y = x W on 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 37 / 57 / 68
-//     against 37 / 54 / 55, on 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 62 / 77 against 71 / 74 / 76, on 8 of 4096 x 14336 at 4 / 16 rows 133 / 164 against
-//     138 / 166; gradient of x on the first 32 / 53 / 57 against 38 / 53 / 54, on the last at 4 / 16 rows 178 / 210 against 146 / 190; 8 bits on the first
-//     23 / 32 / 41 against 24 / 33 / 35, on the last 83 / 105 against 94 / 113.
-//     Few pieces of long sums keep too few compute units busy, which split tiles do not: 16 rows of 14336 values, 4096 columns 66 against 38;
-//     of 4096 values, 4096 columns 16 against 19.5.
-//   Rows that start elsewhere, against grouped_plain.hip: up to 16 rows a group (8 along), and few tiles across: 256 rows, 1001 x 1409 in one group 12.6 against 19.8, 512
-//     rows 22 against 20.
-//   fp32, against grouped_plain.hip: up to 128 rows a group, or tiles that do not fill the card: 16 experts of 2048 x 1408 at 64 / 96 / 128 / 192
-//     rows 100 / 122 / 149 / 203 against 144 / 147 / 213 / 256; 64 / 256 / 512 rows of 4096 x 4096 in one group 52 / 100 / 187 against 276 / 283 / 282.
+//     a group on average, 2 where 16-bit weights lie along the contraction.  y = x W on 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 42 / 57 / 59
+//     against 41 / 54 / 56, on 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 59 / 65 against 72 / 72 / 75, on 8 of 4096 x 14336 at 4 / 12 / 16 rows
+//     157 / 161 / 163 against 162 / 165 / 166; gradient of x on the first at 1 / 2 / 12 rows 36 / 46 / 53 against 40 / 47 / 52, on the last at 2 / 12
+//     rows 181 / 198 against 169 / 186; 8 bits on the first at 1 / 4 / 12 / 16 rows 25 / 29 / 39 / 45 against 32 / 29 / 38 / 40, on the last 66 / 90 / 104 /
+//     115 against 79 / 107 / 112 / 117.
+//     Few pieces of long sums keep too few compute units busy, which split tiles do not: 12 rows of 14336 values, 4096 columns 70 against 36;
+//     of 4096 values, 4096 columns 15.5 against 22.
+//   Rows that start elsewhere, against grouped_plain.hip: across, up to 16 rows a group (33 groups of 1001 x 1409 at 8 / 16 / 24 rows 31 / 33 / 40 against
+//     39 / 38 / 38) or few tiles (256 rows of 1001 x 1409 in one group 12 against 20, 512 rows 23 against 20); along, 8 rows a group where the tiles
+//     would not fill the card (8 groups of 2047 x 4093 56 against 89; 33 of 1001 x 1409, 264 tiles, 62 against 53).
+//   fp32, against grouped_plain.hip: up to 64 rows a group (48 along), or few tiles: 16 experts of 2048 x 1408 at 32 / 64 / 96 rows 66 / 100 / 129 against
+//     147 / 145 / 148, along 74 / 106 / 150 against 106 / 107 / 106; 64 of 1024 x 1024 at 64 / 96 rows 133 / 191 against 149 / 151; 8 of 4096 x 4096 at
+//     32 / 64 / 96 rows 196 / 284 / 387 against 300 / 290 / 294, along 240 / 346 / 477 against 290 / 287 / 288; 64 / 256 / 512 rows of 4096 x 4096 in one
+//     group 52 / 97 / 180 against 277 / 284 / 286.
 bool grouped_stream_sizes(const GroupedArgs& g, int type, bool b_along, bool tiles_fit) {
   const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 127) / 128);
-  if (type == kElemF32) return g.R <= 128 * (int64_t)g.G || tiles < 400;
-  if (!tiles_fit) return g.R <= (b_along && type != kElemI8 ? 8 : 16) * (int64_t)g.G || (!b_along && tiles < 64);
+  if (type == kElemF32) return g.R <= (b_along ? 48 : 64) * (int64_t)g.G || tiles < 320;
+  if (!tiles_fit) {
+    if (b_along && type != kElemI8) return g.R <= 8 * (int64_t)g.G && tiles < 256;
+    return g.R <= 16 * (int64_t)g.G || (!b_along && tiles < 64);
+  }
   const bool few = g.R <= (b_along && type != kElemI8 ? 2 : 12) * (int64_t)g.G;
   const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
   return few && ((int64_t)g.K * elem_bytes(type) <= 16384 || (!b_along && pieces >= 128));
