@@ -31,6 +31,11 @@ NO_SCRATCH = {
     "gemm_mfma.hip": ("gemm1_mfma_kernel", "gemm2_mfma_kernel", "gemm1_stream_kernel", "gemm2_stream_kernel"),
     "gemm_full.hip": ("gemm1_full_kernel", "gemm2_full_kernel", "gemm1_wide_kernel", "gemm2_wide_kernel"),
 }
+# ... and among the operators beside the layer.
+OPERATORS_NO_SCRATCH = {
+    "grouped_mfma.hip": ("grouped_mfma_kernel", "grouped_dw_mfma_kernel"),
+    "grouped_stream.hip": ("grouped_stream_kernel",),
+}
 
 
 def _scratch_users(remarks: str, kernels) -> list:
@@ -56,13 +61,14 @@ def build(force: bool = True, verbose: bool = False) -> str:
     def cc(src: str) -> str:
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
         cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
-        if src in NO_SCRATCH:
+        watched = NO_SCRATCH.get(src) or OPERATORS_NO_SCRATCH.get(src)
+        if watched:
             cmd.append("-Rpass-analysis=kernel-resource-usage")
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("hipcc failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))
-        if src in NO_SCRATCH:
-            bad = _scratch_users(r.stderr, NO_SCRATCH[src])
+        if watched:
+            bad = _scratch_users(r.stderr, watched)
             if bad:
                 raise RuntimeError("%s: kernels that must not spill use scratch memory: %s" % (src, "; ".join(bad)))
         elif verbose and r.stderr.strip():
