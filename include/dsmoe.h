@@ -354,7 +354,7 @@ int moe_grouped_matmul_dw(const void* x, int64_t x_stride, const void* dy, int64
 size_t dsmoe_grouped_dw_workspace_bytes(int32_t rows, int32_t groups, int32_t k, int32_t n, int32_t dtype);
 
 /*
- * Products in 8-bit integers, with a scale for each token and each output channel: s = max|x[r]| / 127 in fp32, q = x[r] / s rounded to
+ * Products in 8-bit integers, with a scale for each token and each output channel: s = max|x[r]| times 1 / 127 in fp32, q = x[r] / s rounded to
  * the nearest integer (ties to even) and clamped to +-127, y[r][c] = s * w_scale[g][c] * sum over k of q w[g][c], the sum exact in int32.
  *   w device int8 [groups][n][k], a row for each output channel; w_scale device float [groups][n] (a group's next to each other);
  *   offsets as above, or NULL for one group of all rows (groups = 1).  k at most 2^17.

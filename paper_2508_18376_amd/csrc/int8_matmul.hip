@@ -1,6 +1,8 @@
 // Products in 8-bit integers: y = x W^T with W held as 8-bit integers and a factor for each output channel, and the rows of x brought to 8 bits
 // within the call, each with a factor of its own:
-//   s[r] = max |x[r]| / 127      q[r] = round(x[r] / s[r])      y[r][n] = s[r] * w_scale[n] * sum over k of q[r][k] w[n][k]
+//   s[r] = max |x[r]| / 127  (times the fp32 value of 1 / 127: what a tensor's division by 127 is in torch on the GPU, so that a program
+//                              that quantizes rows itself finds the same bits; within one unit of the last place of the quotient)
+//   q[r] = round(x[r] / s[r])      y[r][n] = s[r] * w_scale[n] * sum over k of q[r][k] w[n][k]
 // The sum is exact in int32 (k is at most 2^17: 127 * 127 * 2^17 < 2^31); s and the products around it are fp32.
 #include "int8_matmul.h"
 
@@ -36,7 +38,7 @@ __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const void* 
     __syncthreads();
     top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
   }
-  const float s = __uint_as_float(top) / 127.f;
+  const float s = __uint_as_float(top) * (1.f / 127.f);
   const bool zero = s == 0.f || top >= 0x7f800000u;
   // (a factor below 2^-125 has no finite reciprocal, or one that has lost bits: its quotients are all computed)
   const float inv = s < 0x1p-120f ? 0.f : 1.f / s;

@@ -180,7 +180,7 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
 
 
 def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
-    """y[r][c] = s[r] * w_scale[g][c] * sum over k of q[r][k] w[g][c][k], with s = max|x[r]| / 127 and q = round(x[r] / s) in 8 bits.
+    """y[r][c] = s[r] * w_scale[g][c] * sum over k of q[r][k] w[g][c][k], with s = max|x[r]| * (1 / 127) in fp32 and q = round(x[r] / s) in 8 bits.
 
     x [rows][k] bf16, f16 or f32; w int8 [groups][n][k]; w_scale float32 [groups][n]; offsets int32 [groups + 1] on the GPU, or None for
     one group of all rows.  y has x's type.  Weights whose rows start on 16 bytes are faster."""
