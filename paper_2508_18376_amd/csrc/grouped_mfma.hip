@@ -1,13 +1,14 @@
 // Products over groups of rows for 16-bit types and 8-bit integers whose rows start on 16 bytes: the fast path.
 //
 // A tile of C is up to 256 x 256, one workgroup of 4 wavefronts (one per SIMD), 2 x 2 of 128 x 128 each (4 x 4 matrix instructions of 32 x 32,
-// 256 accumulation registers).  The contraction goes 64 bytes (of A's or B's rows; 32 values of 16 bits) a stage, through a ring of four
-// LDS stages of 32 KiB that buffer loads fill without registers in between, three stages ahead of the one being multiplied.
+// 256 accumulation registers).  The contraction goes 128 bytes (of A's or B's rows; 64 values of 16 bits) a stage: shorter ones halve what the L2
+// delivers.  A stage is two units of 32 KiB, one of A and one of B, in a ring of five units that is all of a compute unit's LDS, and that buffer
+// loads fill without registers in between, as far ahead as it has room.
 //
 // An operand lies in LDS as it lies in memory, in one of two ways:
 //   along   a row's values follow each other along the contraction (x; W for the gradient of x; both operands in 8 bits):
-//           [256 rows][64 bytes], the four 16-byte chunks of a row rotated (swz_chunk); a fragment is one 16-byte read
-//   across  the contraction strides over memory rows (W in y = x W, both operands of the gradient of W): [32][256 values]; a fragment is
+//           [256 rows][128 bytes], the eight 16-byte chunks of a row rotated (swz_wide); a fragment is one 16-byte read
+//   across  the contraction strides over memory rows (W in y = x W, both operands of the gradient of W): [64][256 values]; a fragment is
 //           two transposing reads (ds_read_b64_tr_b16), in each of which sixteen lanes take sixteen columns of four rows.  The rows' 64-byte
 //           blocks are rotated by the row (exclusive or with row mod 4), so that the four rows of a read lie in different banks.
 // The order of the values inside a stage does not matter to a sum, as long as both operands have the same one: lane half h of substep s
@@ -853,6 +854,10 @@ hipError_t launch_tiles(GroupedArgs g, hipStream_t s) {
   grouped_mfma_kernel<TY, OUT, BX, BM><<<dim3((unsigned)(g.room.tiles == 0 && 2 * tiles < kWorkgroups ? 2 * tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g);
   e = hipGetLastError();
   if (e != hipSuccess || g.room.tiles == 0) return e;
+  if (g.off == nullptr) {  // the tiles are known here: without a cut along the contraction there is nothing to add up
+    const Split split = split_of((int)tiles, row_stages(g, TY), (int)((int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1)), g.room);
+    if (split.cols || split.whole == tiles) return e;
+  }
   grouped_join_kernel<TY, OUT, false, BX, BM><<<dim3(g.room.tiles, BM / 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});
   return hipGetLastError();
 }
