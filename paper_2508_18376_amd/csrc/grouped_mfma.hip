@@ -300,6 +300,11 @@ __host__ __device__ inline Split split_of(int tiles, int stages, int rows, const
   }
   return s;
 }
+// Rows of a tile on average, of g's R rows in `tiles` tiles of at most BM rows: rows of no group count among the R, but fill no tile.
+__host__ __device__ inline int mean_rows(const GroupedArgs& g, int64_t tiles, int BM) {
+  const int64_t rows = (int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1);
+  return (int)(rows < BM ? rows : BM);
+}
 // rows: at least that many a tile.  No more tiles than 2 sqrt(12 stages tiles rows / 256) < 7.2 or 12 stages - 50 allows, and not many more parts than the least
 // cost has: sqrt(12 stages / tiles * 256 / rows).
 inline SplitRoom split_room(int64_t most_tiles, int stages, int rows) {
@@ -344,12 +349,13 @@ __device__ __forceinline__ void tile_shape(int m_edge, int n_edge, bool across, 
 
 // The factors of an 8-bit tile: of row lane % 32 of each 32, and of the four columns that the lane stores of each 64.  They are loaded before the
 // next tile's first units: vector memory comes back in order, behind those (and one by one, where they are used) the products of an 8-bit
-// call of 6007 x 1024 x 2048 took 34 us instead of 27.
+// call of 6007 x 1024 x 2048 took 34 us instead of 27.  A piece without columns (the second half of a narrow tile) has none to load.
 template <bool I8, int MI, int NI>
 struct Factors {
   float rows[I8 ? MI : 1], cols[I8 ? NI / 2 : 1][4];
   __device__ __forceinline__ void load(const Piece& p, int wm, int wn, int lane) {
     if constexpr (I8) {
+      if (p.n_edge <= 0) return;
 #pragma unroll
       for (int a = 0; a < MI; ++a) rows[a] = p.as[min(wm + a * 32 + (lane & 31), p.m_edge - 1)];
 #pragma unroll
@@ -509,7 +515,7 @@ __device__ __forceinline__ void do_pieces(const GroupedArgs& g, char* lds, Next&
       const int n = stages(p);
       tile.run(n, load_a, load_b, one_a, one_b);
       Factors<TY == kElemI8, MI, NI> factors;
-      if (p.partial == nullptr && n > 0) factors.load(p, wm, wn, lane);
+      if (p.partial == nullptr) factors.load(p, wm, wn, lane);
       stage_barrier();
       if (more) first_units(nxt);
       stores_behind = MI == 4 && NI == 4 && TY != kElemI8 && p.partial == nullptr && p.m_edge == kGT && p.n_edge == kGT;
@@ -664,7 +670,7 @@ struct RowsWork {
     Segment s;
     auto pick_tile = [&](int n) {
       tiles = n;
-      split = split_of(n, (g.K + STAGE - 1) / STAGE, (int)((int64_t)g.R * NT / max(n, 1)), g.room);
+      split = split_of(n, (g.K + STAGE - 1) / STAGE, mean_rows(g, n, BM), g.room);
       return pick(*this);
     };
     if (!all.find(BM, NT, pick_tile, tile, s)) return false;
@@ -839,7 +845,7 @@ inline int tile_rows(const GroupedArgs& g, int type) {
 }
 inline SplitRoom rows_room(const GroupedArgs& g, int type, int BM) {
   const int64_t tiles = most_tiles(g, BM);
-  return split_room(tiles, row_stages(g, type), (int)((int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1)));
+  return split_room(tiles, row_stages(g, type), mean_rows(g, tiles, BM));
 }
 inline int dw_tiles(const GroupedArgs& g) { return g.G * ((g.M + kGT - 1) / kGT) * ((g.N + kGT - 1) / kGT); }
 inline int dw_stages(const GroupedArgs& g) { return (g.R / g.G + 63) / 64; }  // (groups differ: the mean decides)
@@ -855,7 +861,7 @@ hipError_t launch_tiles(GroupedArgs g, hipStream_t s) {
   e = hipGetLastError();
   if (e != hipSuccess || g.room.tiles == 0) return e;
   if (g.off == nullptr) {  // the tiles are known here: without a cut along the contraction there is nothing to add up
-    const Split split = split_of((int)tiles, row_stages(g, TY), (int)((int64_t)g.R * ((g.N + kGT - 1) / kGT) / (tiles > 0 ? tiles : 1)), g.room);
+    const Split split = split_of((int)tiles, row_stages(g, TY), mean_rows(g, tiles, BM), g.room);
     if (split.cols || split.whole == tiles) return e;
   }
   grouped_join_kernel<TY, OUT, false, BX, BM><<<dim3(g.room.tiles, BM / 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});

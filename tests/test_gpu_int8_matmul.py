@@ -145,3 +145,24 @@ def test_no_rows():
     from paper_2508_18376_amd import moe_int8_matmul
     y = moe_int8_matmul(torch.empty(0, 32, device=DEV), torch.ones(1, 8, 32, dtype=torch.int8, device=DEV), torch.ones(1, 8, device=DEV))
     assert y.shape == (0, 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n", [8, 128, 136, 384])
+def test_few_rows_in_a_buffer_of_many(n, dtype):
+    """Four groups of at most 64 rows in a buffer with room for 512: the rows of no group fill no tile, and what lies in front of the factors stays out."""
+    from paper_2508_18376_amd import moe_int8_matmul
+    counts, k = [40, 0, 64, 0, 1, 0, 33, 0], 136
+    R, off = 512, offsets_of(counts)
+    x, w, ws = make(R, 8, k, n, DTYPES[dtype], 11, 8)
+    wd = torch.empty(8, n, k + 8, dtype=torch.int8, device=DEV)[:, :, :k]
+    wd.copy_(w)
+    held = torch.full((8 * n + 64,), float("nan"), device=DEV)
+    wsd = held[32:32 + 8 * n].view(8, n)
+    wsd.copy_(ws)
+    print(n, dtype, flush=True)
+    y = moe_int8_matmul(x.to(DEV), wd, wsd, off.to(DEV))
+    torch.cuda.synchronize()
+    ref = reference(x, w, ws, off)
+    assert_within(y, ref, 4 * U32 * ref.abs(), "y")
+    assert (y[sum(counts):] == 0).all()
