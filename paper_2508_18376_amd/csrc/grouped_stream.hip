@@ -343,6 +343,16 @@ hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
   return once ? launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, true>(g, s) : launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, false>(g, s);
 }
 
+// Threads of the launch, a workgroup for each piece: few rows of very many columns reach 2^32, where a launch is silently cut short (64 groups of a row each
+// and 2^23 columns: 2^23 pieces of 512 threads).  The other paths take those calls: their launches are bounded by the checks at the C boundary.
+// aligned: the weights' rows start on 16 bytes (see launch_w).
+inline bool launch_holds(const GroupedArgs& g, int type, bool b_along, bool aligned) {
+  const int64_t row_tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile);
+  const bool wide = !b_along && type != kElemF32 && aligned;
+  const int64_t threads = wide ? row_tiles * ((g.N + 127) / 128) * 256 : row_tiles * ((g.N + 63) / 64) * 512;
+  return threads < (int64_t)1 << 32;
+}
+
 }  // namespace
 
 // Which calls these kernels take (all times: this path against the other one, us; rows are those of each group).
@@ -362,6 +372,7 @@ hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
 //     32 / 64 / 96 rows 196 / 284 / 387 against 300 / 290 / 294, along 240 / 346 / 477 against 290 / 287 / 288; 64 / 256 / 512 rows of 4096 x 4096 in one
 //     group 52 / 97 / 180 against 277 / 284 / 286.
 bool grouped_stream_sizes(const GroupedArgs& g, int type, bool b_along, bool tiles_fit) {
+  if (!launch_holds(g, type, b_along, tiles_fit)) return false;
   const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 127) / 128);
   if (type == kElemF32) return g.R <= (b_along ? 48 : 64) * (int64_t)g.G || tiles < 320;
   if (!tiles_fit) {

@@ -14,7 +14,8 @@ int& no_ctx_hip_error() {
 
 namespace {
 
-// a workgroup of 256 threads for a row or a tile, and a launch of 2^32 threads and more is silently cut short
+// At most a workgroup of 256 threads for a row or a tile, and a launch of 2^32 threads and more is silently cut short.  (The kernels for groups of few
+// rows launch more for the same call: their own rule leaves such calls to the others.)
 constexpr int64_t kMostWidth = 1 << 24, kMostRows = 1 << 23, kMostGroups = 1 << 16, kMostPieces = 1 << 23;
 
 inline int status(hipError_t e) {

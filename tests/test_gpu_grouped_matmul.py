@@ -214,3 +214,20 @@ def test_rows_beyond_four_gigabytes():
     assert_within(dw, ref, product_error(mag, 500), "dw")
     del big, xs
     torch.cuda.empty_cache()
+
+
+def test_more_columns_than_workgroups_for_each_piece_hold():
+    """fp32, 64 groups of a row each, 2^23 outputs a row, one weight for all groups: all of them are written, the last ones too."""
+    from paper_2508_18376_amd import moe_grouped_matmul
+    G, K, N = 64, 4, 1 << 23
+    gen = torch.Generator(device=DEV).manual_seed(60)
+    x, w = torch.randn(G, K, generator=gen, device=DEV), torch.randn(1, N, K, generator=gen, device=DEV)
+    out = torch.full((G, N), float("nan"), device=DEV)
+    moe_grouped_matmul(x, w.expand(G, N, K), torch.arange(G + 1, dtype=torch.int32, device=DEV), w_transposed=True, out=out)
+    torch.cuda.synchronize()
+    step = 1 << 20
+    for c in range(0, N, step):
+        wc = w[0, c:c + step].double().t().contiguous()
+        ref, mag = x.double() @ wc, x.double().abs() @ wc.abs()
+        err = product_error(mag, K)
+        assert bool(((out[:, c:c + step].double() - ref).abs() <= err + 2.0 ** -24 * (ref.abs() + err)).all()), c

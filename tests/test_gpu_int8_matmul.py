@@ -166,3 +166,23 @@ def test_few_rows_in_a_buffer_of_many(n, dtype):
     ref = reference(x, w, ws, off)
     assert_within(y, ref, 4 * U32 * ref.abs(), "y")
     assert (y[sum(counts):] == 0).all()
+
+
+def test_more_columns_than_workgroups_for_each_piece_hold():
+    """64 groups of a row each and 2^23 columns, one weight for all groups: all outputs are written, the last ones too."""
+    from paper_2508_18376_amd import moe_int8_matmul
+    G, k, n = 64, 16, 1 << 23
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    x = torch.randn(G, k, generator=gen, device=DEV).bfloat16()
+    w = torch.randint(-127, 128, (1, n, k), generator=gen, device=DEV, dtype=torch.int8)
+    ws = torch.rand(1, n, generator=gen, device=DEV)
+    out = torch.full((G, n), float("nan"), dtype=torch.bfloat16, device=DEV)
+    moe_int8_matmul(x, w.expand(G, n, k), ws.expand(G, n), torch.arange(G + 1, dtype=torch.int32, device=DEV), out=out)
+    torch.cuda.synchronize()
+    s = x.float().abs().amax(1) * INV127.to(DEV)
+    q = torch.round(x.float() / s[:, None]).double()
+    step = 1 << 20
+    for c in range(0, n, step):
+        ref = q @ w[0, c:c + step].double().t().contiguous() * ws[0, c:c + step].double() * s[:, None].double()
+        got = out[:, c:c + step].double()
+        assert bool(((got - ref).abs() <= 2.0 ** -8 * ref.abs() * (1 + 8 * U32) + 8 * U32 * ref.abs()).all()), c

@@ -192,3 +192,19 @@ def test_norm_pointers():
 def test_errors_without_a_context_are_kept():
     _lib.dsmoe_last_hip_error.restype = ctypes.c_int
     assert _lib.dsmoe_last_hip_error(None) == 0
+
+
+def test_calls_too_large_for_a_workgroup_for_each_piece_go_to_the_tiles():
+    """A launch of 2^32 threads is cut short, and the kernels for groups of few rows have 512 threads (across: 256) for 64 (128) columns of 32 rows.
+    Which kernels a call goes to shows in the workspace: they split nothing, the tiles do."""
+    def int8_split(rows, groups, k, n):
+        held = (rows * ((k + 127) // 128 * 128) + 255) // 256 * 256 + (rows * 4 + 255) // 256 * 256
+        return _lib.dsmoe_int8_workspace_bytes(rows, groups, k, n) - held
+
+    k = 2048
+    assert int8_split(64, 64, k, (1 << 23) - 64) == 0 and int8_split(64, 64, k, 1 << 23) > 0
+    assert int8_split(1 << 16, 1 << 16, k, 8192 - 64) == 0 and int8_split(1 << 16, 1 << 16, k, 8192) > 0
+    assert int8_split(64, 64, k, 1 << 24) > 0
+    bf16 = _lib.dsmoe_grouped_workspace_bytes
+    assert bf16(64, 64, 1 << 22, k, 1, 1) == 0 and bf16(64, 64, 1 << 23, k, 1, 1) > 0  # along
+    assert bf16(64, 64, k, 1 << 23, 0, 1) == 0  # across: half as many pieces, of half as many threads
