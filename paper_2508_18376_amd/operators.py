@@ -11,6 +11,7 @@ from .binding import DsmoeError, _lib, _raw_stream
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _EINVAL, _EHIP = -1, -4
+_INT32_MAX = (1 << 31) - 1
 GATE_NONE, GATE_TOKEN, GATE_CHANNEL, GATE_FULL = 0, 1, 2, 3
 
 
@@ -78,6 +79,11 @@ def _device_of(where, x, *others) -> int:
     return d
 
 
+def _too_large(where):
+    """Sizes go to the library in 32 bits, where larger ones would come out as others.  (The calls or the sizes together: one comparison.)"""
+    _refuse(where, "no dimension may pass 2^31 - 1")
+
+
 def _check_offsets(offsets, groups, where) -> None:
     if offsets.dtype is not torch.int32 or offsets.dim() != 1 or offsets.shape[0] != groups + 1 or not offsets.is_contiguous():
         _refuse(where, "offsets must be int32 [%d], contiguous" % (groups + 1))
@@ -100,6 +106,8 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
         _refuse(f, "x must have 2 dimensions and w 3")
     R, K = x.shape
     G, k, n = w.shape
+    if R | G | k | n > _INT32_MAX:
+        _too_large(f)
     N = n
     if w_transposed:
         N, k_of_x = k, n
@@ -147,6 +155,8 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
     R, k = x.shape
     rows, n = dy.shape
     G = offsets.shape[0] - 1
+    if R | G | k | n > _INT32_MAX:
+        _too_large(f)
     if rows != R:
         _refuse(f, "x and dy must have the same rows")
     dtype = _DTYPES.get(x.dtype)
@@ -189,6 +199,8 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
         _refuse(f, "x must have 2 dimensions and w 3")
     R, k = x.shape
     G, n, k_of_w = w.shape
+    if R | G | k | n > _INT32_MAX:
+        _too_large(f)
     if k != k_of_w:
         _refuse(f, "x must have rows of %d values" % k_of_w)
     dtype = _DTYPES.get(x.dtype)
@@ -234,6 +246,8 @@ def _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, 
     if len(shape) != 2 or shape[1] < 1 or branch.shape != shape:
         _refuse(f, "x and branch must be [tokens][d], of one shape")
     T, D = shape
+    if T | D > _INT32_MAX:
+        _too_large(f)
     if branch_weight.dim() != 1 or weight.dim() != 1 or branch_weight.shape[0] != D or weight.shape[0] != D:
         _refuse(f, "branch_weight and weight must be [%d]" % D)
     code = _DTYPES.get(dtype)

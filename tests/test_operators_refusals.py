@@ -208,3 +208,23 @@ def test_calls_too_large_for_a_workgroup_for_each_piece_go_to_the_tiles():
     bf16 = _lib.dsmoe_grouped_workspace_bytes
     assert bf16(64, 64, 1 << 22, k, 1, 1) == 0 and bf16(64, 64, 1 << 23, k, 1, 1) > 0  # along
     assert bf16(64, 64, k, 1 << 23, 0, 1) == 0  # across: half as many pieces, of half as many threads
+
+
+MANY = (1 << 32) + 5  # 5, if cut off to 32 bits
+SIZES = {
+    "rows": lambda: ds.moe_grouped_matmul(z(1, 8).expand(MANY, 8), z(2, 8, 6), off(3)),
+    "columns": lambda: ds.moe_grouped_matmul(z(4, 8), z(2, 8, 1).expand(2, 8, MANY), off(3)),
+    "dw: rows": lambda: ds.moe_grouped_matmul_dw(z(1, 8).expand(MANY, 8), z(1, 6).expand(MANY, 6), off(3)),
+    "dw: columns": lambda: ds.moe_grouped_matmul_dw(z(4, 8), z(4, 1).expand(4, MANY), off(3)),
+    "int8: rows": lambda: ds.moe_int8_matmul(z(1, 8).expand(MANY, 8), z(1, 6, 8, dtype=torch.int8), z(1, 6, dtype=torch.float32)),
+    "int8: columns": lambda: ds.moe_int8_matmul(z(4, 8), z(1, 1, 8, dtype=torch.int8).expand(1, MANY, 8), z(1, 1, dtype=torch.float32).expand(1, MANY)),
+    "norm: tokens": lambda: norm(x=z(1, 8).expand(MANY, 8), branch=z(1, 8).expand(MANY, 8)),
+    "norm: width": lambda: norm(x=z(1, 1).expand(1, MANY), branch=z(1, 1).expand(1, MANY), branch_weight=z(1).expand(MANY), weight=z(1).expand(MANY)),
+}
+
+
+@pytest.mark.parametrize("case", SIZES)
+def test_sizes_beyond_32_bits_are_refused(case):
+    with pytest.raises(ds.DsmoeError, match="2\\^31") as e:
+        SIZES[case]()
+    assert e.value.status == -1
