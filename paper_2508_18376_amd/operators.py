@@ -1,11 +1,16 @@
 """The operators beside the layer (include/dsmoe.h): products over groups of rows with their gradients, products in 8-bit integers, and the
 norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
-the call runs on (the current one, or `stream`).  A call that does not fit its tensors raises DsmoeError before anything is launched."""
+the call runs on (the current one, or `stream`).  A call that does not fit its tensors raises DsmoeError before anything is launched.
+
+Nothing is recorded for automatic differentiation: the gradients are operators of their own.  While gradients are being recorded, tensors that need them
+(or have a forward-mode tangent) are refused, because the result would look like a constant.  Call inside torch.no_grad(), or from the
+forward and backward of a torch.autograd.Function, where recording is off."""
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import DsmoeError, _lib, _raw_stream
 
@@ -80,8 +85,21 @@ def _device_of(where, x, *others) -> int:
 
 
 def _too_large(where):
-    """Sizes go to the library in 32 bits, where larger ones would come out as others.  (The calls or the sizes together: one comparison.)"""
+    """Sizes go to the library in 32 bits, where larger ones would come out as others.  (Or-ed together they pass the limit if one does.)"""
     _refuse(where, "no dimension may pass 2^31 - 1")
+
+
+def _check_unrecorded(where, *tensors) -> None:
+    """Refuses tensors whose gradients or tangents the call would have to pass on (see the module's docstring)."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                _refuse(where, "an input needs gradients, which this call does not record: call it inside torch.no_grad() or a torch.autograd.Function")
+    # (no level of forward-mode differentiation: no tangents; where torch does not say, each tensor is asked)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                _refuse(where, "an input has a forward-mode tangent, which this call does not pass on")
 
 
 def _check_offsets(offsets, groups, where) -> None:
@@ -125,6 +143,7 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
         _no_rows(f, "x")
     if w_value != 1 and n > 1:
         _no_rows(f, "w")
+    _check_unrecorded(f, x, w, out)
     device = _device_of(f, x, w, offsets)
     entered = _entered(device, stream)
     if entered is not None:
@@ -169,6 +188,7 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
         _no_rows(f, "x")
     if dy_value != 1 and n > 1:
         _no_rows(f, "dy")
+    _check_unrecorded(f, x, dy, out)
     device = _device_of(f, x, dy, offsets)
     entered = _entered(device, stream)
     if entered is not None:
@@ -221,6 +241,7 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
         _no_rows(f, "w")
     if s_value != 1 and n > 1:
         _no_rows(f, "w_scale")
+    _check_unrecorded(f, x, w_scale, out)
     device = _device_of(f, x, w, w_scale, offsets)
     entered = _entered(device, stream)
     if entered is not None:
@@ -284,6 +305,7 @@ def moe_block_norm(x, *, branch, branch_weight, weight, gate=None, scale=1.0, we
     (float32 [2][tokens]) for moe_block_norm_backward."""
     f = "moe_block_norm"
     args = _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, eps)
+    _check_unrecorded(f, x, branch, branch_weight, weight, gate)
     device = _device_of(f, x, branch, branch_weight, weight, gate)
     entered = _entered(device, stream)
     if entered is not None:
@@ -314,6 +336,7 @@ def moe_block_norm_backward(dy, dh, x, stats, *, branch, branch_weight, weight, 
     args.dh_stride, dh_value = dh.stride()
     if D > 1 and (dy_value != 1 or dh_value != 1):
         _no_rows(f, "dy and dh")
+    _check_unrecorded(f, x, dy, dh, stats, branch, branch_weight, weight, gate)
     device = _device_of(f, x, dy, dh, stats, branch, branch_weight, weight, gate)
     entered = _entered(device, stream)
     if entered is not None:

@@ -231,3 +231,34 @@ def test_more_columns_than_workgroups_for_each_piece_hold():
         ref, mag = x.double() @ wc, x.double().abs() @ wc.abs()
         err = product_error(mag, K)
         assert bool(((out[:, c:c + step].double() - ref).abs() <= err + 2.0 ** -24 * (ref.abs() + err)).all()), c
+
+
+def test_inside_an_autograd_function():
+    """Tensors that need gradients are refused where they are recorded, and the forward and backward of a torch.autograd.Function may call the operators."""
+    from paper_2508_18376_amd import DsmoeError, moe_grouped_matmul, moe_grouped_matmul_dw
+
+    class Product(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, offsets):
+            ctx.save_for_backward(x, w, offsets)
+            return moe_grouped_matmul(x, w, offsets)
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w, offsets = ctx.saved_tensors
+            return moe_grouped_matmul(dy, w, offsets, w_transposed=True), moe_grouped_matmul_dw(x, dy, offsets), None
+
+    counts = [9, 0, 30]
+    off = offsets_of(counts)
+    x, w, dy = (make(s, torch.float32, 70 + i) for i, s in enumerate([(39, 24), (3, 24, 40), (39, 40)]))
+    xd, wd = x.to(DEV).requires_grad_(), w.to(DEV).requires_grad_()
+    with pytest.raises(DsmoeError, match="needs gradients"):
+        moe_grouped_matmul(xd, wd, off.to(DEV))
+    y = Product.apply(xd, wd, off.to(DEV))
+    y.backward(dy.to(DEV))
+    ref, mag = grouped_reference(x, w, off)
+    assert_within(y, ref, product_error(mag, 24), "y")
+    ref, mag = grouped_reference(dy, w, off, transposed=True)
+    assert_within(xd.grad, ref, product_error(mag, 40), "dx")
+    ref, mag = grouped_dw_reference(x, dy, off)
+    assert_within(wd.grad, ref, product_error(mag, 30), "dw")

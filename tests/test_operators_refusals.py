@@ -228,3 +228,39 @@ def test_sizes_beyond_32_bits_are_refused(case):
     with pytest.raises(ds.DsmoeError, match="2\\^31") as e:
         SIZES[case]()
     assert e.value.status == -1
+
+
+def _calls():
+    """Each operator with its tensors by name, and which of them a gradient can go to."""
+    f32 = torch.float32
+    nm = dict(x=z(4, 8), branch=z(4, 8), branch_weight=z(8), weight=z(8), gate=z(4, 1))
+    return {
+        "moe_grouped_matmul": (lambda a: ds.moe_grouped_matmul(a["x"], a["w"], off(3), out=a["out"]), dict(x=z(4, 8), w=z(2, 8, 6), out=z(4, 6))),
+        "moe_grouped_matmul_dw": (lambda a: ds.moe_grouped_matmul_dw(a["x"], a["dy"], off(3), out=a["out"]), dict(x=z(4, 8), dy=z(4, 6), out=z(2, 8, 6))),
+        "moe_int8_matmul": (lambda a: ds.moe_int8_matmul(a["x"], z(1, 6, 8, dtype=torch.int8), a["w_scale"], out=a["out"]),
+                            dict(x=z(4, 8), w_scale=z(1, 6, dtype=f32), out=z(4, 6))),
+        "moe_block_norm": (lambda a: ds.moe_block_norm(a.pop("x"), **a), nm),
+        "moe_block_norm_backward": (lambda a: ds.moe_block_norm_backward(*[a.pop(n) for n in ("dy", "dh", "x", "stats")], **a),
+                                    dict(nm, dy=z(4, 8), dh=z(4, 8), stats=z(2, 4, dtype=f32))),
+    }
+
+
+@pytest.mark.parametrize("op,name", [(op, name) for op, (_, tensors) in _calls().items() for name in tensors])
+def test_nothing_is_cut_from_the_graph_in_silence(op, name):
+    """A tensor that needs gradients, or has a tangent, is refused while they are recorded.  (Where they are not, the next check refuses: no GPU here.)"""
+    def refusal(change):
+        call, tensors = _calls()[op]
+        tensors[name] = change(tensors[name])
+        with pytest.raises(ds.DsmoeError) as e:
+            call(tensors)
+        assert e.value.status == -1 and op in str(e.value)
+        return str(e.value)
+
+    assert "needs gradients" in refusal(lambda t: t.requires_grad_())
+    assert "needs gradients" in refusal(lambda t: t.requires_grad_() * 1)  # not a leaf
+    with torch.no_grad():
+        assert "on one GPU" in refusal(lambda t: t.requires_grad_())
+    assert "on one GPU" in refusal(lambda t: t)
+    with torch.autograd.forward_ad.dual_level():
+        assert "tangent" in refusal(lambda t: torch.autograd.forward_ad.make_dual(t, torch.ones_like(t)))
+        assert "on one GPU" in refusal(lambda t: t)
