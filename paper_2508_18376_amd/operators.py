@@ -67,9 +67,11 @@ def _no_rows(where, name):
     _refuse(where, "%s: the values of a row must be contiguous" % name)
 
 
-def _entered(device, stream):
+def _entered(where, device, stream):
     """The device, and where the call names a stream that stream, made current: allocations then belong to it.  None: they are."""
     if stream is not None:
+        if stream.device.index != device:
+            _refuse(where, "stream must be of the tensors' GPU")
         return torch.cuda.stream(stream)
     return None if device == _current_device() else torch.cuda.device(device)
 
@@ -145,7 +147,7 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
         _no_rows(f, "w")
     _check_unrecorded(f, x, w, out)
     device = _device_of(f, x, w, offsets)
-    entered = _entered(device, stream)
+    entered = _entered(f, device, stream)
     if entered is not None:
         with entered:
             return moe_grouped_matmul(x, w, offsets, w_transposed, out)
@@ -190,7 +192,7 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
         _no_rows(f, "dy")
     _check_unrecorded(f, x, dy, out)
     device = _device_of(f, x, dy, offsets)
-    entered = _entered(device, stream)
+    entered = _entered(f, device, stream)
     if entered is not None:
         with entered:
             return moe_grouped_matmul_dw(x, dy, offsets, out)
@@ -243,7 +245,7 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
         _no_rows(f, "w_scale")
     _check_unrecorded(f, x, w_scale, out)
     device = _device_of(f, x, w, w_scale, offsets)
-    entered = _entered(device, stream)
+    entered = _entered(f, device, stream)
     if entered is not None:
         with entered:
             return moe_int8_matmul(x, w, w_scale, offsets, out)
@@ -307,7 +309,7 @@ def moe_block_norm(x, *, branch, branch_weight, weight, gate=None, scale=1.0, we
     args = _norm_args(f, x, branch, branch_weight, gate, weight, scale, weight_offset, eps)
     _check_unrecorded(f, x, branch, branch_weight, weight, gate)
     device = _device_of(f, x, branch, branch_weight, weight, gate)
-    entered = _entered(device, stream)
+    entered = _entered(f, device, stream)
     if entered is not None:
         with entered:
             return moe_block_norm(x, branch=branch, branch_weight=branch_weight, weight=weight, gate=gate, scale=scale, weight_offset=weight_offset,
@@ -338,7 +340,7 @@ def moe_block_norm_backward(dy, dh, x, stats, *, branch, branch_weight, weight, 
         _no_rows(f, "dy and dh")
     _check_unrecorded(f, x, dy, dh, stats, branch, branch_weight, weight, gate)
     device = _device_of(f, x, dy, dh, stats, branch, branch_weight, weight, gate)
-    entered = _entered(device, stream)
+    entered = _entered(f, device, stream)
     if entered is not None:
         with entered:
             return moe_block_norm_backward(dy, dh, x, stats, branch=branch, branch_weight=branch_weight, weight=weight, gate=gate, scale=scale,

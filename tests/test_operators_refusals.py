@@ -264,3 +264,44 @@ def test_nothing_is_cut_from_the_graph_in_silence(op, name):
     with torch.autograd.forward_ad.dual_level():
         assert "tangent" in refusal(lambda t: torch.autograd.forward_ad.make_dual(t, torch.ones_like(t)))
         assert "on one GPU" in refusal(lambda t: t)
+
+
+class OnGpu0:
+    """A CPU tensor that says it lies on the first GPU: the checks up to the stream's read nothing of it."""
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
+
+
+class Stream1:
+    device = torch.device("cuda", 1)
+
+
+@pytest.mark.parametrize("op", ["moe_grouped_matmul", "moe_grouped_matmul_dw", "moe_int8_matmul", "moe_block_norm", "moe_block_norm_backward"])
+def test_streams_of_another_gpu_are_refused(op, monkeypatch):
+    """The call would run on the tensors' GPU, on a stream that the caller did not name."""
+    monkeypatch.setattr(ops, "_current_device", lambda: 0)
+
+    def refuse(*_):
+        raise AssertionError("the named stream is entered, though it is another GPU's")
+
+    monkeypatch.setattr(torch.cuda, "stream", refuse)
+    norms = {k: OnGpu0(v) for k, v in dict(branch=z(4, 8), branch_weight=z(8), weight=z(8)).items()}
+    x, o = OnGpu0(z(4, 8)), OnGpu0(off(3))
+    with pytest.raises(ds.DsmoeError, match="stream") as e:
+        if op == "moe_grouped_matmul":
+            ds.moe_grouped_matmul(x, OnGpu0(z(2, 8, 6)), o, stream=Stream1())
+        elif op == "moe_grouped_matmul_dw":
+            ds.moe_grouped_matmul_dw(x, OnGpu0(z(4, 6)), o, stream=Stream1())
+        elif op == "moe_int8_matmul":
+            ds.moe_int8_matmul(x, OnGpu0(z(1, 6, 8, dtype=torch.int8)), OnGpu0(z(1, 6, dtype=torch.float32)), stream=Stream1())
+        elif op == "moe_block_norm":
+            ds.moe_block_norm(x, stream=Stream1(), **norms)
+        else:
+            ds.moe_block_norm_backward(OnGpu0(z(4, 8)), OnGpu0(z(4, 8)), x, OnGpu0(z(2, 4, dtype=torch.float32)), stream=Stream1(), **norms)
+    assert e.value.status == -1 and op in str(e.value)
