@@ -116,6 +116,12 @@ def _check_out(out, shape, like, where) -> None:
         _no_rows(where, "out")
 
 
+def _written(out) -> None:
+    """The caller's `out` has other values now: a graph that kept the old ones for a gradient has to notice.  (Inference tensors are in no graph.)"""
+    if not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+
+
 def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None):
     """y[r] = x[r] W[g], or x[r] W[g]^T with w_transposed, for the rows offsets[g] .. offsets[g + 1] - 1 of each group g.
 
@@ -151,6 +157,7 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
     if entered is not None:
         with entered:
             return moe_grouped_matmul(x, w, offsets, w_transposed, out)
+    given = out
     if out is None:
         out, y_row = x.new_empty(R, N), N
     else:
@@ -163,6 +170,8 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
                                  out.data_ptr(), y_row, workspace.data_ptr() if size else None, _raw_stream(device))
     if rc:
         _failed(rc, f)
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -196,6 +205,7 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
     if entered is not None:
         with entered:
             return moe_grouped_matmul_dw(x, dy, offsets, out)
+    given = out
     if out is None:
         out, row, group = x.new_empty(G, k, n), n, k * n
     else:
@@ -208,6 +218,8 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
                                     workspace.data_ptr() if size else None, _raw_stream(device))
     if rc:
         _failed(rc, f)
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -249,6 +261,7 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
     if entered is not None:
         with entered:
             return moe_int8_matmul(x, w, w_scale, offsets, out)
+    given = out
     if out is None:
         out, y_row = x.new_empty(R, n), n
     else:
@@ -261,6 +274,8 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
                               workspace.data_ptr() if size else None, _raw_stream(device))
     if rc:
         _failed(rc, f)
+    if given is not None:
+        _written(given)
     return out
 
 

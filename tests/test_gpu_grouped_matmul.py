@@ -262,3 +262,23 @@ def test_inside_an_autograd_function():
     assert_within(xd.grad, ref, product_error(mag, 40), "dx")
     ref, mag = grouped_dw_reference(x, dy, off)
     assert_within(wd.grad, ref, product_error(mag, 30), "dw")
+
+
+def test_values_that_a_graph_kept_are_not_overwritten_in_silence():
+    """A buffer that a recorded product needs for its gradient, then written as `out`: the backward pass refuses, as after torch's own writes."""
+    from paper_2508_18376_amd import moe_grouped_matmul, moe_grouped_matmul_dw, moe_int8_matmul
+    off = offsets_of([4, 2]).to(DEV)
+    x, w, dy = torch.ones(6, 16, device=DEV), torch.ones(2, 16, 24, device=DEV), torch.ones(6, 24, device=DEV)
+    w8, ws = torch.ones(2, 24, 16, dtype=torch.int8, device=DEV), torch.ones(2, 24, device=DEV)
+    for shape, call in (((6, 24), lambda out: moe_grouped_matmul(x, w, off, out=out)), ((2, 16, 24), lambda out: moe_grouped_matmul_dw(x, dy, off, out=out)),
+                        ((6, 24), lambda out: moe_int8_matmul(x, w8, ws, off, out=out))):
+        leaf, out = torch.ones(shape, device=DEV, requires_grad=True), torch.zeros(shape, device=DEV)
+        loss = (leaf * out).sum()
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        with torch.inference_mode():
+            kept = torch.zeros(shape, device=DEV)
+            call(kept)
+        call(kept)
+        assert torch.equal(kept, out)
