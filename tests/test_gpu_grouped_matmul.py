@@ -282,3 +282,41 @@ def test_values_that_a_graph_kept_are_not_overwritten_in_silence():
             call(kept)
         call(kept)
         assert torch.equal(kept, out)
+
+
+# More pieces of work than workgroups (256), so that each takes several: counts, k, n.
+SEVERAL = {
+    "tiles_of_256": ([1300, 0, 900, 800], 136, 6000),  # 288 and more (y; dx has few)
+    "tiles_of_128": ([65 + i % 3 for i in range(40)], 264, 1800),  # 320; dW 640
+    "tiles_of_64_one_stage": ([13 + i * 7 % 52 for i in range(40)], 56, 2056),  # 360
+    "tiles_of_64_two_stages": ([13 + i * 7 % 52 for i in range(40)], 72, 2056),
+    "tiles_of_64_three_stages": ([13 + i * 7 % 52 for i in range(40)], 192, 2056),
+    "tiles_of_64_six_stages": ([13 + i * 7 % 52 for i in range(40)], 328, 2056),
+    "tiles_of_64_split": ([13 + i * 7 % 52 for i in range(33)], 1608, 2056),  # 297: the last 41 are cut along the contraction
+    "tiles_of_64_dx": ([13 + i * 7 % 52 for i in range(40)], 2056, 328),
+    "weights": ([100 + i for i in range(20)], 520, 1288),  # dW: 360, of 2 and 3 stages
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name", SEVERAL)
+def test_workgroups_that_take_several_tiles(name, dtype):
+    from paper_2508_18376_amd import moe_grouped_matmul, moe_grouped_matmul_dw
+    counts, k, n = SEVERAL[name]
+    G, R, off, dt = len(counts), sum(counts) + 9, offsets_of(counts, 2), DTYPES[dtype]
+    x, w, dy = make((R, k), dt, 80), make((G, k, n), dt, 81, 0.1), make((R, n), dt, 82)
+    xd, wd, dyd, offd = x.to(DEV), w.to(DEV), dy.to(DEV), off.to(DEV)
+    print(name, dtype, R, G, k, n, flush=True)
+    y, dx, dw = (moe_grouped_matmul(xd, wd, offd), moe_grouped_matmul(dyd, wd, offd, w_transposed=True), moe_grouped_matmul_dw(xd, dyd, offd))
+    torch.cuda.synchronize()
+    ref, mag = grouped_reference(x, w, off)
+    assert_within(y, ref, product_error(mag, k), "y")
+    ref, mag = grouped_reference(dy, w, off, transposed=True)
+    assert_within(dx, ref, product_error(mag, n), "dx")
+    ref, mag = grouped_dw_reference(x, dy, off)
+    assert_within(dw, ref, product_error(mag, max(counts)), "dw")
+    for t in (y, dx):
+        assert (t[:2] == 0).all() and (t[2 + sum(counts):] == 0).all()
+    for _ in range(3):
+        assert torch.equal(y, moe_grouped_matmul(xd, wd, offd)) and torch.equal(dx, moe_grouped_matmul(dyd, wd, offd, w_transposed=True))
+        assert torch.equal(dw, moe_grouped_matmul_dw(xd, dyd, offd))

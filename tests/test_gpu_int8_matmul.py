@@ -186,3 +186,43 @@ def test_more_columns_than_workgroups_for_each_piece_hold():
         ref = q @ w[0, c:c + step].double().t().contiguous() * ws[0, c:c + step].double() * s[:, None].double()
         got = out[:, c:c + step].double()
         assert bool(((got - ref).abs() <= 2.0 ** -8 * ref.abs() * (1 + 8 * U32) + 8 * U32 * ref.abs()).all()), c
+
+
+# More pieces of work than workgroups (256), so that each takes several: counts, k, n.  The factors differ by a factor of 1000 between groups and columns.
+SEVERAL = {
+    "tiles_of_256": ([1300, 0, 900, 800], 136, 6000),  # 288 and more
+    "tiles_of_256_long": ([1300, 0, 900, 800], 700, 6000),
+    "tiles_of_128": ([65 + i % 3 for i in range(40)], 264, 1800),  # 320
+    "tiles_of_64_one_stage": ([13 + i * 7 % 52 for i in range(40)], 100, 2056),  # 360
+    "tiles_of_64_two_stages": ([13 + i * 7 % 52 for i in range(40)], 136, 2056),
+    "tiles_of_64_three_stages": ([13 + i * 7 % 52 for i in range(40)], 384, 2056),
+    "tiles_of_64_six_stages": ([13 + i * 7 % 52 for i in range(40)], 700, 2056),
+    "tiles_of_64_split": ([13 + i * 7 % 52 for i in range(33)], 3300, 2056),  # 297: the last 41 are cut along the contraction
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("name", SEVERAL)
+def test_workgroups_that_take_several_tiles(name, dtype):
+    from paper_2508_18376_amd import moe_int8_matmul
+    counts, k, n = SEVERAL[name]
+    G, R, off, pad = len(counts), sum(counts) + 9, offsets_of(counts, 2), -k % 16
+    x, w, ws = make(R, G, k, n, DTYPES[dtype], 13, pad)
+    gen = torch.Generator().manual_seed(14)
+    ws = ws * torch.exp(torch.rand(G, n, generator=gen) * 6.9)
+    wd = torch.empty(G, n, k + pad, dtype=torch.int8, device=DEV)[:, :, :k]
+    wd.copy_(w)
+    print(name, dtype, R, G, k, n, flush=True)
+    xd, wsd, offd = x.to(DEV), ws.to(DEV), off.to(DEV)
+    y = moe_int8_matmul(xd, wd, wsd, offd)
+    torch.cuda.synchronize()
+    ref = reference(x, w, ws, off)
+    # f16 ends at 65504, and from half a step behind it on a value is an infinity of its sign (between the two: either)
+    beyond = ref.abs() > torch.finfo(x.dtype).max
+    far = ref.abs() > torch.finfo(x.dtype).max * (1 + 2.0 ** -12) * (1 + 8 * U32)
+    assert torch.equal(y.cpu()[far].double(), ref[far].sign() * float("inf"))
+    keep = ~beyond
+    assert_within(y.cpu()[keep], ref[keep], 4 * U32 * ref[keep].abs(), "y")
+    assert (y[:2] == 0).all() and (y[2 + sum(counts):] == 0).all()
+    for _ in range(3):
+        assert torch.equal(y, moe_int8_matmul(xd, wd, wsd, offd))
