@@ -320,3 +320,54 @@ def test_workgroups_that_take_several_tiles(name, dtype):
     for _ in range(3):
         assert torch.equal(y, moe_grouped_matmul(xd, wd, offd)) and torch.equal(dx, moe_grouped_matmul(dyd, wd, offd, w_transposed=True))
         assert torch.equal(dw, moe_grouped_matmul_dw(xd, dyd, offd))
+
+
+# More groups than a wavefront has lanes, on every kind of tile: counts, k, n.
+MANY = {
+    "tiles_of_64": ([(13 + i * 7 % 52) * (i % 11 != 3) + 2 for i in range(150)], 72, 264),
+    "tiles_of_64_full_groups": ([13 + i * 5 % 40 for i in range(512)], 40, 264),
+    "tiles_of_64_split": ([13 + i * 7 % 52 for i in range(65)], 1536, 136),  # y in 3 parts
+    "tiles_of_128": ([65 + i % 5 for i in range(150)], 136, 264),
+    "tiles_of_128_ragged": ([(i * 37 % 301) * (i % 7 != 2) + 60 for i in range(65)], 72, 264),
+    "tiles_of_256": ([65 + i % 9 for i in range(520)], 72, 264),
+    "weights_split": ([1000 + i % 50 for i in range(260)], 24, 40),  # dW of the last four in parts
+    "odd": ([17 + i % 30 for i in range(150)], 45, 77),
+    "odd_few": ([i % 3 for i in range(512)], 45, 77),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", MANY)
+def test_more_groups_than_lanes(name, dtype):
+    from paper_2508_18376_amd import moe_grouped_matmul, moe_grouped_matmul_dw
+    counts, k, n = MANY[name]
+    G, R, off, dt = len(counts), sum(counts) + 9, offsets_of(counts, 2), DTYPES[dtype]
+    x, w, dy = make((R, k), dt, 90), make((G, k, n), dt, 91, 0.1), make((R, n), dt, 92)
+    xd, wd, dyd, offd = x.to(DEV), w.to(DEV), dy.to(DEV), off.to(DEV)
+    print(name, dtype, R, G, k, n, flush=True)
+    y, dx, dw = (moe_grouped_matmul(xd, wd, offd), moe_grouped_matmul(dyd, wd, offd, w_transposed=True), moe_grouped_matmul_dw(xd, dyd, offd))
+    torch.cuda.synchronize()
+    ref, mag = grouped_reference(x, w, off)
+    assert_within(y, ref, product_error(mag, k), "y")
+    ref, mag = grouped_reference(dy, w, off, transposed=True)
+    assert_within(dx, ref, product_error(mag, n), "dx")
+    ref, mag = grouped_dw_reference(x, dy, off)
+    assert_within(dw, ref, product_error(mag, max(counts)), "dw")
+    for t in (y, dx):
+        assert (t[:2] == 0).all() and (t[2 + sum(counts):] == 0).all()
+
+
+@pytest.mark.parametrize("k,n", [(72, 40), (45, 77)])
+@pytest.mark.parametrize("rows", [400, 6000, 12000])
+def test_long_tables_out_of_order_stay_in_bounds(rows, k, n):
+    """150 groups whose bounds are any numbers around the rows."""
+    from paper_2508_18376_amd import moe_grouped_matmul, moe_grouped_matmul_dw
+    gen = torch.Generator().manual_seed(rows)
+    off = (torch.linspace(-0.1, 1.1, 151) * rows + torch.randn(151, generator=gen) * rows / 40).to(torch.int32)
+    x, w, dy = make((rows, k), torch.bfloat16, 93), make((150, k, n), torch.bfloat16, 94), make((rows, n), torch.bfloat16, 95)
+    y = moe_grouped_matmul(x.to(DEV), w.to(DEV), off.to(DEV))
+    ref, mag = grouped_reference(x, w, off)
+    assert_within(y, ref, product_error(mag, k), "y")
+    dw = moe_grouped_matmul_dw(x.to(DEV), dy.to(DEV), off.to(DEV))
+    ref, mag = grouped_dw_reference(x, dy, off)
+    assert_within(dw, ref, product_error(mag, rows), "dw")

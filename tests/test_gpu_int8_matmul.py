@@ -226,3 +226,29 @@ def test_workgroups_that_take_several_tiles(name, dtype):
     assert (y[:2] == 0).all() and (y[2 + sum(counts):] == 0).all()
     for _ in range(3):
         assert torch.equal(y, moe_int8_matmul(xd, wd, wsd, offd))
+
+
+MANY = {
+    "tiles_of_64": ([(13 + i * 7 % 52) * (i % 11 != 3) + 2 for i in range(150)], 200, 264),
+    "tiles_of_64_split": ([13 + i * 7 % 52 for i in range(65)], 3000, 136),
+    "tiles_of_128": ([65 + i % 5 for i in range(150)], 136, 264),
+    "tiles_of_256": ([65 + i % 9 for i in range(520)], 72, 264),
+    "few_rows": ([i % 3 for i in range(512)], 200, 77),
+    "odd": ([17 + i % 30 for i in range(150)], 45, 77),
+}
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_more_groups_than_lanes(name):
+    from paper_2508_18376_amd import moe_int8_matmul
+    counts, k, n = MANY[name]
+    G, R, off, pad = len(counts), sum(counts) + 9, offsets_of(counts, 2), -k % 16 if n % 8 == 0 else 0
+    x, w, ws = make(R, G, k, n, torch.bfloat16, 15, pad)
+    wd = torch.empty(G, n, k + pad, dtype=torch.int8, device=DEV)[:, :, :k]
+    wd.copy_(w)
+    print(name, R, G, k, n, flush=True)
+    y = moe_int8_matmul(x.to(DEV), wd, ws.to(DEV), off.to(DEV))
+    torch.cuda.synchronize()
+    ref = reference(x, w, ws, off)
+    assert_within(y, ref, 4 * U32 * ref.abs(), "y")
+    assert (y[:2] == 0).all() and (y[2 + sum(counts):] == 0).all()
