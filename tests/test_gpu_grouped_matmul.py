@@ -371,3 +371,37 @@ def test_long_tables_out_of_order_stay_in_bounds(rows, k, n):
     dw = moe_grouped_matmul_dw(x.to(DEV), dy.to(DEV), off.to(DEV))
     ref, mag = grouped_dw_reference(x, dy, off)
     assert_within(dw, ref, product_error(mag, rows), "dw")
+
+
+def test_tiles_of_rows_beyond_four_gigabytes():
+    """Rows exactly 4 MiB apart, the most that the tiles take, and more than 2^32 bytes of them: x, dy, outputs, and the weights' rows too."""
+    from paper_2508_18376_amd import moe_grouped_matmul, moe_grouped_matmul_dw
+    R, k, n, apart = 1100, 264, 328, 1 << 21
+    big = torch.empty(R * apart, dtype=torch.bfloat16, device=DEV).view(R, apart)
+    weights = torch.empty(2 * k * apart, dtype=torch.bfloat16, device=DEV).view(2, k, apart)
+    x, w, dy = make((R, k), torch.bfloat16, 52), make((2, k, n), torch.bfloat16, 53, 0.1), make((R, n), torch.bfloat16, 54)
+    xd, dyd, yd, dxd = (big[:, c:c + v] for c, v in ((0, k), (1024, n), (2048, n), (4096, k)))
+    xd.copy_(x)
+    dyd.copy_(dy)
+    wd, dwd = weights[:, :, :n], weights[:, :, 1024:1024 + n]
+    wd.copy_(w)
+    off = offsets_of([1000, 100])
+    moe_grouped_matmul(xd, wd, off.to(DEV), out=yd)
+    moe_grouped_matmul(dyd, wd, off.to(DEV), w_transposed=True, out=dxd)
+    moe_grouped_matmul_dw(xd, dyd, off.to(DEV), out=dwd)
+    torch.cuda.synchronize()
+    ref, mag = grouped_reference(x, w, off)
+    assert_within(yd, ref, product_error(mag, k), "y")
+    ref, mag = grouped_reference(dy, w, off, transposed=True)
+    assert_within(dxd, ref, product_error(mag, n), "dx")
+    ref, mag = grouped_dw_reference(x, dy, off)
+    assert_within(dwd, ref, product_error(mag, 1000), "dw")
+    # tiles of 64 rows: many groups of few rows, all weights the first group's
+    counts = [50 + i % 2 for i in range(20)]
+    off = offsets_of(counts)
+    moe_grouped_matmul(xd, wd[:1].expand(20, k, n), off.to(DEV), out=yd)
+    torch.cuda.synchronize()
+    ref, mag = grouped_reference(x, w[:1].expand(20, k, n), off)
+    assert_within(yd, ref, product_error(mag, k), "y")
+    del big, weights, xd, dyd, yd, dxd, wd, dwd
+    torch.cuda.empty_cache()
