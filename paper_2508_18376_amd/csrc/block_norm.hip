@@ -97,8 +97,9 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(BlockNormArgs a) {
 // The two sums that a row needs depend on each other, but the second is linear in the first: with q = b' (branch_weight + offset), times the gate where that
 // varies inside the row, and d = dy + u / rms(y),
 //   sum of q dx = sum of q d - (sum of u y' / (d rms(y))) * sum of q y'
-// so one exchange between the wavefronts gives all three.  The next row's values are on their way while this one is worked on: without that and with
-// two exchanges 8192 rows of 4096 took 145 us; now 84.
+// so one exchange between the wavefronts gives all three.  Where dh lies along y the difference cancels more than q dx does: the error of a gate's gradient is
+// then 1.1 - 1.2 times that of the sum as it stands (both in fp32 on the CPU, rms over 400 rows of 512 and of 4096; 1.0 otherwise).
+// The next row's values are on their way while this one is worked on: without that and with two exchanges 8192 rows of 4096 took 145 us; now 84.
 // A last chunk that is not whole is the row's last 8 values: what it has in common with the chunk before it comes out the same in both, and only
 // counts once in the sums.
 template <int TY>

@@ -1,4 +1,4 @@
-// Shared by the products over groups of rows (grouped.hip, int8_matmul.hip): arguments, and the groups' rows worked out on the device.
+// Shared by the products over groups of rows (grouped_mfma.hip, grouped_stream.hip, grouped_plain.hip, int8_matmul.hip): arguments, and the groups' rows worked out on the device.
 #pragma once
 #include "common.h"
 
@@ -149,7 +149,7 @@ struct Segments {
   }
 };
 
-// most row tiles of BM rows that R rows in G groups can give
+// Most row tiles of BM rows that R rows in G groups can give: a first row in each group, and a tile more for every BM further rows.
 inline int64_t row_tiles_bound(int64_t R, int64_t G, bool grouped, int BM) {
   if (!grouped) return (R + BM - 1) / BM;
   const int64_t groups = G < R ? G : R;
@@ -173,7 +173,7 @@ __device__ __forceinline__ void band_tile(int id, int row_tiles, int col_tiles, 
   rt = band * kBand + left - ct * h;
 }
 
-// (R - segments) / BM + segments tiles: a first row in each segment, and a tile more for every BM further rows at most
+// any type, alignment and stride
 hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
 hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s);
 // the fast path of 16-bit types and 8-bit integers, where the operands lie for it

@@ -355,7 +355,8 @@ inline bool launch_holds(const GroupedArgs& g, int type, bool b_along, bool alig
 
 }  // namespace
 
-// Which calls these kernels take (all times: this path against the other one, us; rows are those of each group).
+// Which calls these kernels take (all times: this path against the other one, us; rows are a group's on average, the groups ragged as routing makes them, and
+// the calls take three sets of inputs in turn).
 //   16-bit types and 8-bit integers whose rows start on 16 bytes, against the tiles of grouped_mfma.hip, which read weights through LDS: up to 12 rows
 //     a group on average, 2 where 16-bit weights lie along the contraction.  y = x W on 64 experts of 2048 x 1024 at 1 / 8 / 16 rows 42 / 57 / 59
 //     against 41 / 54 / 56, on 64 of 2048 x 1408 at 6 / 12 / 24 rows 57 / 59 / 65 against 72 / 72 / 75, on 8 of 4096 x 14336 at 4 / 12 / 16 rows

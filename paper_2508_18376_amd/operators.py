@@ -123,7 +123,8 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
     """y[r] = x[r] W[g], or x[r] W[g]^T with w_transposed, for the rows offsets[g] .. offsets[g + 1] - 1 of each group g.
 
     x [rows][k] ([rows][n] with w_transposed), w [groups][k][n], offsets int32 [groups + 1] on the GPU; bf16, f16 or f32.  Rows of no group
-    (before the first offset, from the last one on) come out zero.  Rows and weights may be strided, the values of a row are contiguous."""
+    (before the first offset, from the last one on) come out zero.  Rows and weights may be strided, the values of a row are contiguous.  out, if
+    given, is written and returned: it may be strided too, and must not overlap the inputs."""
     f = "moe_grouped_matmul"
     if x.dim() != 2 or w.dim() != 3:
         _refuse(f, "x must have 2 dimensions and w 3")
@@ -178,7 +179,8 @@ def moe_grouped_matmul(x, w, offsets, w_transposed=False, out=None, stream=None)
 def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
     """dw[g] = sum over the rows of group g of x[r]^T dy[r]: the weights' gradient of moe_grouped_matmul.
 
-    x [rows][k], dy [rows][n], offsets int32 [groups + 1] on the GPU; returns [groups][k][n], zeros for a group without rows."""
+    x [rows][k], dy [rows][n], offsets int32 [groups + 1] on the GPU; returns [groups][k][n], zeros for a group without rows.  out as in
+    moe_grouped_matmul."""
     f = "moe_grouped_matmul_dw"
     if x.dim() != 2 or dy.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 2:
         _refuse(f, "x and dy must have 2 dimensions, offsets 1")
@@ -230,7 +232,7 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
     """y[r][c] = s[r] * w_scale[g][c] * sum over k of q[r][k] w[g][c][k], with s = max|x[r]| * (1 / 127) in fp32 and q = round(x[r] / s) in 8 bits.
 
     x [rows][k] bf16, f16 or f32; w int8 [groups][n][k]; w_scale float32 [groups][n]; offsets int32 [groups + 1] on the GPU, or None for
-    one group of all rows.  y has x's type.  Weights whose rows start on 16 bytes are faster."""
+    one group of all rows.  y has x's type.  Weights whose rows start on 16 bytes are faster.  out as in moe_grouped_matmul."""
     f = "moe_int8_matmul"
     if x.dim() != 2 or w.dim() != 3:
         _refuse(f, "x must have 2 dimensions and w 3")
