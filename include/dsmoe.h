@@ -392,6 +392,32 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
                             const void* branch_weight, const void* gate, const void* weight, const float* stats, void* dx, void* dbranch,
                             void* dbranch_weight, void* dgate, void* dweight, void* workspace, void* stream);
 
+/*
+ * The gated half of a block of experts (Eq. 4 up to W2) over groups of rows, both projections, the activation and the product in one:
+ *   a = x W1[g]   b = x W3[g]   h = f(a) * b        x [rows][k], W1, W3 [groups][k][n], h [rows][n]; a and b are not rounded
+ *   activation DSMOE_SILU: f(a) = a / (1 + exp(-a)) (Swish); DSMOE_GELU_TANH: f(a) = a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2
+ * offsets as above, or NULL for one group of all rows (groups = 1).  W1 and W3 have the same strides.  Rows of no group: zeros in h.
+ *   saved device float [2][rows][n], or NULL: a and b as they were summed, which the backward pass takes; 16 bytes aligned are faster.  Rows of no
+ *   group are not written.
+ *   workspace as for moe_grouped_matmul, dsmoe_gated_workspace_bytes(args) bytes or NULL.
+ * Backward: from dh [rows][n] (h_stride is then dh's) dx = da W1[g]^T + db W3[g]^T, dw1[g] = sum over the group's rows of x[r]^T da[r] and dw3[g]
+ * likewise of db, with da = dh * b * f'(a) and db = dh * f(a), each rounded to dtype once, as are the results.  dx [rows][k] (rows of no group:
+ * zeros) and dw1, dw3 [groups][k][n] (a group without rows: zeros) are written without gaps.
+ *   workspace device, dsmoe_gated_backward_workspace_bytes(args) bytes, 256-byte aligned (needed if there are rows).
+ * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 rows x 64 columns of h, or 128 x 128 of dx and the weights, in all.
+ */
+enum { DSMOE_SILU = 0, DSMOE_GELU_TANH = 1 };
+typedef struct {
+  int32_t rows, groups, k, n, dtype, activation;
+  int64_t x_stride, w_group_stride, w_row_stride, h_stride;
+} dsmoe_gated_args;
+size_t dsmoe_gated_workspace_bytes(const dsmoe_gated_args* args);
+int moe_gated_matmul(const dsmoe_gated_args* args, const void* x, const void* w1, const void* w3, const int32_t* offsets, void* h, float* saved,
+                     void* workspace, void* stream);
+size_t dsmoe_gated_backward_workspace_bytes(const dsmoe_gated_args* args);
+int moe_gated_matmul_backward(const dsmoe_gated_args* args, const void* dh, const void* x, const void* w1, const void* w3, const float* saved,
+                              const int32_t* offsets, void* dx, void* dw1, void* dw3, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,6 +40,8 @@ _BINDING_NAMES = (
 _OPERATOR_NAMES = (
     "moe_grouped_matmul",
     "moe_grouped_matmul_dw",
+    "moe_gated_matmul",
+    "moe_gated_matmul_backward",
     "moe_int8_matmul",
     "moe_block_norm",
     "moe_block_norm_backward",

@@ -1,4 +1,5 @@
-// Shared by the products over groups of rows (grouped_mfma.hip, grouped_stream.hip, grouped_plain.hip, int8_matmul.hip): arguments, and the groups' rows worked out on the device.
+// Shared by the products over groups of rows (grouped_tiles.h, grouped_streams.h, grouped_plain.h and what launches them; int8_matmul.hip): arguments, and the groups'
+// rows worked out on the device.
 #pragma once
 #include "common.h"
 
@@ -9,6 +10,13 @@ inline __host__ __device__ int elem_bytes(int t) { return t == kElemF32 ? 4 : t 
 
 struct SplitRoom {
   int32_t tiles, parts;  // tiles that may be split, and parts of all of them
+};
+
+// What a launch over rows computes (see gated.hip for the last two).
+enum GroupedMode : int32_t {
+  kOneProduct,   // C_g = A_g B_g
+  kGatedPair,    // C_g = f(A_g B_g) * (A_g B2_g)
+  kSumOfTwo,     // C_g = A_g B_g + A2_g B2_g
 };
 
 // One launch of products C_g = A_g B_g.  Rows are the caller's rows (tokens); a group owns rows [off[g], off[g+1]).
@@ -25,9 +33,30 @@ struct GroupedArgs {
   const float* b_scale;
   int64_t bs_group;  // ... in values
   int32_t out_type;
+  const char *a2, *b2;  // kSumOfTwo, kGatedPair: the second operands, strides as the first ones'
+  float* sums;          // kGatedPair: where both products go as they are, [2][R][N], or nullptr
+  int32_t act;          // kGatedPair: the activation f
   char* partial;  // workspace for tiles whose contraction is split (grouped_workspace_bytes), or nullptr
   SplitRoom room;
 };
+
+// The activations are f(a) = a sigmoid(z(a)): z = a (Swish), or 2 sqrt(2 / pi) (a + 0.044715 a^3), which makes it a (1 + tanh(z / 2)) / 2 (GELU by tanh)
+// without that sum's cancellation.  Beyond +-100 the sigmoid of GELU's z is 0 or 1, and a^3 must not overflow there.
+constexpr float kGeluSlope = 1.5957691216057308f, kGeluCube = 0.044715f;
+__device__ __forceinline__ float activation_exponent(int act, float a) {
+  if (act == DSMOE_SILU) return a;
+  const float b = fminf(fmaxf(a, -100.f), 100.f);
+  return kGeluSlope * (b + kGeluCube * b * b * b);
+}
+__device__ __forceinline__ float activation(int act, float a) { return a / (1.f + expf(-activation_exponent(act, a))); }
+// f(a) and f'(a) = s + a s (1 - s) z'(a)
+__device__ __forceinline__ void activation_slope(int act, float a, float& f, float& slope) {
+  const float s = 1.f / (1.f + expf(-activation_exponent(act, a)));
+  const float b = fminf(fmaxf(a, -100.f), 100.f);
+  const float z = act == DSMOE_SILU ? 1.f : kGeluSlope * (1.f + 3.f * kGeluCube * b * b);
+  f = a * s;
+  slope = s + a * s * (1.f - s) * z;
+}
 
 // Inclusive scans over the 64 lanes (DPP: shifts inside the rows of sixteen, then the last lane of a row to the next ones).
 // Identity 0: sums, and maxima of values that are not negative.
@@ -173,6 +202,7 @@ __device__ __forceinline__ void band_tile(int id, int row_tiles, int col_tiles, 
   rt = band * kBand + left - ct * h;
 }
 
+// (of the launches below, those without a mode are of kOneProduct)
 // any type, alignment and stride
 hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hipStream_t s);
 hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s);

@@ -1,5 +1,6 @@
 // C ABI of the operators beside the layer (see include/dsmoe.h): argument checks and launches.
 #include "block_norm.h"
+#include "gated.h"
 #include "grouped.h"
 #include "int8_matmul.h"
 
@@ -69,6 +70,35 @@ BlockNormArgs norm_args(const dsmoe_block_norm_args* a, const void* x, const voi
   n.offset = a->weight_offset;
   n.eps = a->eps;
   return n;
+}
+
+bool gated_args_ok(const dsmoe_gated_args* a) {
+  return a && sizes_ok(a->rows, a->groups, a->k, a->n) && float_type(a->dtype) && (a->activation == DSMOE_SILU || a->activation == DSMOE_GELU_TANH) &&
+         in_stride(a->x_stride) && in_stride(a->w_group_stride) && in_stride(a->w_row_stride) &&
+         row_tiles_bound(a->rows, a->groups, true, 128) * tiles(a->n, 64) <= kMostPieces;
+}
+bool gated_backward_args_ok(const dsmoe_gated_args* a) {
+  return gated_args_ok(a) && in_stride(a->h_stride) && row_tiles_bound(a->rows, a->groups, true, 128) * tiles(a->k, 128) <= kMostPieces &&
+         tiles(a->k, 128) * tiles(a->n, 128) <= kMostPieces / a->groups;
+}
+GatedArgs gated_args(const dsmoe_gated_args* a, const void* x, const void* w1, const void* w3, const int32_t* offsets, void* workspace) {
+  GatedArgs g = {};
+  g.x = x;
+  g.w1 = w1;
+  g.w3 = w3;
+  g.offsets = offsets;
+  g.x_row = a->x_stride;
+  g.w_row = a->w_row_stride;
+  g.w_group = a->w_group_stride;
+  g.h_row = a->h_stride;
+  g.R = a->rows;
+  g.G = a->groups;
+  g.K = a->k;
+  g.N = a->n;
+  g.type = a->dtype;
+  g.act = a->activation;
+  g.workspace = (char*)workspace;
+  return g;
 }
 
 }  // namespace
@@ -216,6 +246,42 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
   n.dweight = dweight;
   n.partial = (float*)workspace;
   return status(launch_block_norm_backward(n, (hipStream_t)stream));
+}
+
+size_t dsmoe_gated_workspace_bytes(const dsmoe_gated_args* args) {
+  return gated_args_ok(args) ? gated_workspace_bytes(gated_args(args, nullptr, nullptr, nullptr, nullptr, nullptr)) : 0;
+}
+
+int moe_gated_matmul(const dsmoe_gated_args* args, const void* x, const void* w1, const void* w3, const int32_t* offsets, void* h, float* saved,
+                     void* workspace, void* stream) {
+  if (!gated_args_ok(args) || !out_stride(args->h_stride, args->n) || (!offsets && args->groups != 1) || ((uintptr_t)workspace & 255) != 0) return DSMOE_EINVAL;
+  if (args->rows == 0) return DSMOE_OK;
+  if (!x || !w1 || !w3 || !h || ((uintptr_t)saved & 3) != 0) return DSMOE_EINVAL;
+  for (const void* p : {x, w1, w3, (const void*)h})
+    if (!aligned_to(p, args->dtype)) return DSMOE_EINVAL;
+  GatedArgs g = gated_args(args, x, w1, w3, offsets, workspace);
+  g.h = h;
+  g.saved = saved;
+  return status(launch_gated(g, (hipStream_t)stream));
+}
+
+size_t dsmoe_gated_backward_workspace_bytes(const dsmoe_gated_args* args) {
+  return gated_backward_args_ok(args) ? gated_backward_workspace_bytes(gated_args(args, nullptr, nullptr, nullptr, nullptr, nullptr)) : 0;
+}
+
+int moe_gated_matmul_backward(const dsmoe_gated_args* args, const void* dh, const void* x, const void* w1, const void* w3, const float* saved,
+                              const int32_t* offsets, void* dx, void* dw1, void* dw3, void* workspace, void* stream) {
+  if (!gated_backward_args_ok(args) || (!offsets && args->groups != 1) || ((uintptr_t)workspace & 255) != 0 || ((uintptr_t)saved & 3) != 0) return DSMOE_EINVAL;
+  if (!dw1 || !dw3 || (args->rows > 0 && (!dh || !x || !w1 || !w3 || !saved || !dx || !workspace))) return DSMOE_EINVAL;
+  for (const void* p : {dh, x, w1, w3, (const void*)dx, (const void*)dw1, (const void*)dw3})
+    if (!aligned_to(p, args->dtype)) return DSMOE_EINVAL;
+  GatedArgs g = gated_args(args, x, w1, w3, offsets, workspace);
+  g.dh = dh;
+  g.saved = const_cast<float*>(saved);
+  g.dx = dx;
+  g.dw1 = dw1;
+  g.dw3 = dw3;
+  return status(launch_gated_backward(g, (hipStream_t)stream));
 }
 
 }  // extern "C"

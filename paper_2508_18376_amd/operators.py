@@ -1,5 +1,5 @@
-"""The operators beside the layer (include/dsmoe.h): products over groups of rows with their gradients, products in 8-bit integers, and the
-norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
+"""The operators beside the layer (include/dsmoe.h): products over groups of rows with their gradients, the gated half of a block with its
+gradients, products in 8-bit integers, and the norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
 the call runs on (the current one, or `stream`).  A call that does not fit its tensors raises DsmoeError before anything is launched.
 
 Nothing is recorded for automatic differentiation: the gradients are operators of their own.  While gradients are being recorded, tensors that need them
@@ -27,6 +27,14 @@ class _BlockNormArgs(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("x_stride", "branch_stride", "gate_stride", "dy_stride", "dh_stride")])
 
 
+class _GatedArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "groups", "k", "n", "dtype", "activation")]
+                + [(n, ctypes.c_int64) for n in ("x_stride", "w_group_stride", "w_row_stride", "h_stride")])
+
+
+ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+
+
 def _declare(L):
     vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
     args = ctypes.POINTER(_BlockNormArgs)
@@ -39,9 +47,15 @@ def _declare(L):
     L.moe_block_norm.argtypes = [args] + [vp] * 9
     L.dsmoe_block_norm_workspace_bytes.argtypes = [args]
     L.moe_block_norm_backward.argtypes = [args] + [vp] * 15
-    for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes):
+    gated = ctypes.POINTER(_GatedArgs)
+    L.dsmoe_gated_workspace_bytes.argtypes = L.dsmoe_gated_backward_workspace_bytes.argtypes = [gated]
+    L.moe_gated_matmul.argtypes = [gated] + [vp] * 8
+    L.moe_gated_matmul_backward.argtypes = [gated] + [vp] * 11
+    for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes,
+              L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes):
         f.restype = ctypes.c_size_t
-    for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward):
+    for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward, L.moe_gated_matmul,
+              L.moe_gated_matmul_backward):
         f.restype = ctypes.c_int
 
 
@@ -226,6 +240,110 @@ def moe_grouped_matmul_dw(x, dy, offsets, out=None, stream=None):
     if given is not None:
         _written(given)
     return out
+
+
+def _gated_args(f, x, w1, w3, offsets, activation):
+    if x.dim() != 2 or w1.dim() != 3 or w1.shape != w3.shape:
+        _refuse(f, "x must have 2 dimensions, w1 and w3 3 and one shape")
+    R, k = x.shape
+    G, k_of_w, n = w1.shape
+    if R | G | k | n > _INT32_MAX:
+        _too_large(f)
+    if k != k_of_w:
+        _refuse(f, "x must have rows of %d values" % k_of_w)
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or w1.dtype is not x.dtype or w3.dtype is not x.dtype:
+        _refuse(f, "x, w1 and w3 must be of one type, bfloat16, float16 or float32")
+    if offsets is not None:
+        if offsets.dtype is not _INT32 or offsets.dim() != 1 or offsets.shape[0] != G + 1 or not offsets.is_contiguous():
+            _bad_offsets(f, G)
+    elif G != 1:
+        _refuse(f, "several groups need offsets")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        _refuse(f, "activation must be one of %s" % ", ".join(ACTIVATIONS))
+    x_row, x_value = x.stride()
+    w_group, w_row, w_value = w1.stride()
+    w3_group, w3_row, w3_value = w3.stride()
+    if x_value != 1 and k > 1:
+        _no_rows(f, "x")
+    if n > 1 and (w_value != 1 or w3_value != 1):
+        _no_rows(f, "w1 and w3")
+    if w_group != w3_group and G > 1 or w_row != w3_row and k > 1:
+        _refuse(f, "w1 and w3 must have the same strides")
+    return _GatedArgs(R, G, k, n, dtype, act, x_row, w_group, w_row, n)
+
+
+def moe_gated_matmul(x, w1, w3, offsets=None, activation="silu", want_saved=False, out=None, stream=None):
+    """h[r] = f(x[r] W1[g]) * (x[r] W3[g]) for the rows offsets[g] .. offsets[g + 1] - 1 of each group g: both projections of a block of experts, the
+    activation and the product.
+
+    x [rows][k], w1, w3 [groups][k][n] with the same strides, offsets int32 [groups + 1] on the GPU, or None for one group of all rows; bf16, f16 or
+    f32; rows of no group come out zero.  activation "silu" (a sigmoid(a)) or "gelu_tanh".  want_saved: (h, saved) with both products as they were
+    summed, float32 [2][rows][n], for moe_gated_matmul_backward (rows of no group are left as they were allocated).  out as in moe_grouped_matmul."""
+    f = "moe_gated_matmul"
+    args = _gated_args(f, x, w1, w3, offsets, activation)
+    if (_grad_enabled() and (x.requires_grad or w1.requires_grad or w3.requires_grad or out is not None and out.requires_grad)
+            or _forward_mode._current_level >= 0):
+        _check_unrecorded(f, x, w1, w3, out)
+    device = x.get_device()
+    if device < 0 or w1.get_device() != device or w3.get_device() != device or offsets is not None and offsets.get_device() != device:
+        _not_one_gpu(f)
+    if stream is not None or device != _current_device():
+        with _entered(f, device, stream):
+            return moe_gated_matmul(x, w1, w3, offsets, activation, want_saved, out)
+    R, n = args.rows, args.n
+    given = out
+    if out is None:
+        out = x.new_empty(R, n)
+    else:
+        _check_out(out, (R, n), x, f)
+        if R > 1:
+            args.h_stride = out.stride(0)
+    saved = torch.empty((2, R, n), dtype=torch.float32, device=x.device) if want_saved else None
+    size = _lib.dsmoe_gated_workspace_bytes(args)
+    workspace = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    rc = _lib.moe_gated_matmul(args, x.data_ptr(), w1.data_ptr(), w3.data_ptr(), None if offsets is None else offsets.data_ptr(), out.data_ptr(),
+                               saved.data_ptr() if want_saved else None, workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    if given is not None:
+        _written(given)
+    return (out, saved) if want_saved else out
+
+
+def moe_gated_matmul_backward(dh, x, w1, w3, saved, offsets=None, activation="silu", stream=None):
+    """Gradients of moe_gated_matmul from that of h: a dict of dx, dw1 and dw3.  The other arguments are those of the forward call, saved what it
+    returned with want_saved.  Rows of no group get a dx of zeros, groups without rows gradients of zeros."""
+    f = "moe_gated_matmul_backward"
+    args = _gated_args(f, x, w1, w3, offsets, activation)
+    R, n = args.rows, args.n
+    if dh.shape != (R, n) or dh.dtype is not x.dtype:
+        _refuse(f, "dh must be [%d][%d], of x's type" % (R, n))
+    if saved.shape != (2, R, n) or saved.dtype is not torch.float32 or not saved.is_contiguous():
+        _refuse(f, "saved must be float32 [2][%d][%d], contiguous" % (R, n))
+    args.h_stride, dh_value = dh.stride()
+    if dh_value != 1 and n > 1:
+        _no_rows(f, "dh")
+    if (_grad_enabled() and (x.requires_grad or w1.requires_grad or w3.requires_grad or dh.requires_grad or saved.requires_grad)
+            or _forward_mode._current_level >= 0):
+        _check_unrecorded(f, x, w1, w3, dh, saved)
+    device = x.get_device()
+    if (device < 0 or w1.get_device() != device or w3.get_device() != device or dh.get_device() != device or saved.get_device() != device
+            or offsets is not None and offsets.get_device() != device):
+        _not_one_gpu(f)
+    if stream is not None or device != _current_device():
+        with _entered(f, device, stream):
+            return moe_gated_matmul_backward(dh, x, w1, w3, saved, offsets, activation)
+    dx, dw1, dw3 = x.new_empty(R, args.k), x.new_empty(w1.shape), x.new_empty(w1.shape)
+    size = _lib.dsmoe_gated_backward_workspace_bytes(args)
+    workspace = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    rc = _lib.moe_gated_matmul_backward(args, dh.data_ptr(), x.data_ptr(), w1.data_ptr(), w3.data_ptr(), saved.data_ptr(),
+                                        None if offsets is None else offsets.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(),
+                                        workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    return {"dx": dx, "dw1": dw1, "dw3": dw3}
 
 
 def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
