@@ -393,6 +393,27 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
                             void* dbranch_weight, void* dgate, void* dweight, void* workspace, void* stream);
 
 /*
+ * Products with weights in 4 bits, a scale and if wanted a zero point for each block of `block` weights of an output channel:
+ *   y[r][c] = sum over k of x[r][k] (q[g][c][k] - z[g][c][j]) s[g][c][j]      j = k / block
+ * w device uint8 [groups][n][(k + 1) / 2], a row for each output channel: q of an even k in the low half of a byte, of an odd one in the high half
+ * (the last high half of an odd k is not used).  w_scale [groups][n][(k + block - 1) / block], dtype's or float: scale_dtype says which; w_zero device
+ * uint8, shaped like it, or NULL: 8 everywhere.  block: a power of two from 32 on.  offsets as above, or NULL for one group of all rows
+ * (groups = 1).  Rows of w on 16 bytes are faster.  Rows of no group: zeros.
+ *   In 16-bit types calls of many rows round each weight (q - z) s to dtype once (f16: after a power of two for each output channel has brought
+ *   it into range); sums are in 32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
+ * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
+ */
+typedef struct {
+  int32_t rows, groups, k, n, block, dtype, scale_dtype;
+  int32_t pad; /* 0 */
+  int64_t x_stride, y_stride;
+  int64_t w_group_stride, w_row_stride; /* in bytes */
+  int64_t scale_group_stride, scale_row_stride, zero_group_stride, zero_row_stride;
+} dsmoe_int4_args;
+int moe_int4_matmul(const dsmoe_int4_args* args, const void* x, const uint8_t* w, const void* w_scale, const uint8_t* w_zero,
+                    const int32_t* offsets, void* y, void* stream);
+
+/*
  * The gated half of a block of experts (Eq. 4 up to W2) over groups of rows, both projections, the activation and the product in one:
  *   a = x W1[g]   b = x W3[g]   h = f(a) * b        x [rows][k], W1, W3 [groups][k][n], h [rows][n]; a and b are not rounded
  *   activation DSMOE_SILU: f(a) = a / (1 + exp(-a)) (Swish); DSMOE_GELU_TANH: f(a) = a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2

@@ -43,6 +43,7 @@ _OPERATOR_NAMES = (
     "moe_gated_matmul",
     "moe_gated_matmul_backward",
     "moe_int8_matmul",
+    "moe_int4_matmul",
     "moe_block_norm",
     "moe_block_norm_backward",
 )

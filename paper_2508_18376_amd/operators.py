@@ -1,5 +1,5 @@
 """The operators beside the layer (include/dsmoe.h): products over groups of rows with their gradients, the gated half of a block with its
-gradients, products in 8-bit integers, and the norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
+gradients, products with weights in 8-bit integers and in 4 bits, and the norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
 the call runs on (the current one, or `stream`).  A call that does not fit its tensors raises DsmoeError before anything is launched.
 
 Nothing is recorded for automatic differentiation: the gradients are operators of their own.  While gradients are being recorded, tensors that need them
@@ -32,6 +32,12 @@ class _GatedArgs(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("x_stride", "w_group_stride", "w_row_stride", "h_stride")])
 
 
+class _Int4Args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "groups", "k", "n", "block", "dtype", "scale_dtype", "pad")]
+                + [(n, ctypes.c_int64) for n in ("x_stride", "y_stride", "w_group_stride", "w_row_stride", "scale_group_stride", "scale_row_stride",
+                                                 "zero_group_stride", "zero_row_stride")])
+
+
 ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
 
 
@@ -51,11 +57,12 @@ def _declare(L):
     L.dsmoe_gated_workspace_bytes.argtypes = L.dsmoe_gated_backward_workspace_bytes.argtypes = [gated]
     L.moe_gated_matmul.argtypes = [gated] + [vp] * 8
     L.moe_gated_matmul_backward.argtypes = [gated] + [vp] * 11
+    L.moe_int4_matmul.argtypes = [ctypes.POINTER(_Int4Args)] + [vp] * 7
     for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes,
               L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes):
         f.restype = ctypes.c_size_t
     for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward, L.moe_gated_matmul,
-              L.moe_gated_matmul_backward):
+              L.moe_gated_matmul_backward, L.moe_int4_matmul):
         f.restype = ctypes.c_int
 
 
@@ -398,6 +405,78 @@ def moe_int8_matmul(x, w, w_scale, offsets=None, out=None, stream=None):
     rc = _lib.moe_int8_matmul(x.data_ptr(), x_row, w.data_ptr(), w_group, w_row, w_scale.data_ptr(), s_group,
                               None if offsets is None else offsets.data_ptr(), R, G, k, n, dtype, out.data_ptr(), y_row,
                               workspace.data_ptr() if size else None, _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    if given is not None:
+        _written(given)
+    return out
+
+
+def moe_int4_matmul(x, w, w_scale, w_zero=None, offsets=None, block=128, out=None, stream=None):
+    """y[r][c] = sum over k of x[r][k] (q[g][c][k] - z[g][c][k // block]) s[g][c][k // block]: products with weights in 4 bits, a scale (and a zero point) for
+    each block of an output channel's weights.
+
+    x [rows][k] bf16, f16 or f32; w uint8 [groups][n][(k + 1) // 2], the weight of an even k in a byte's low half, of an odd one in its high half;
+    w_scale [groups][n][ceil(k / block)] of x's type or float32; w_zero uint8 of that shape, or None for 8 everywhere; block a power of two
+    from 32 on; offsets int32 [groups + 1] on the GPU, or None for one group of all rows.  y has x's type.  Weights whose rows start on
+    16 bytes are faster.  out as in moe_grouped_matmul."""
+    f = "moe_int4_matmul"
+    if x.dim() != 2 or w.dim() != 3:
+        _refuse(f, "x must have 2 dimensions and w 3")
+    R, k = x.shape
+    G, n, row_bytes = w.shape
+    if R | G | k | n > _INT32_MAX:
+        _too_large(f)
+    if row_bytes != (k + 1) // 2:
+        _refuse(f, "w must have rows of %d bytes, for the %d values of x's" % ((k + 1) // 2, k))
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None or w.dtype is not torch.uint8:
+        _refuse(f, "x must be bfloat16, float16 or float32 and w uint8")
+    if type(block) is not int or not 32 <= block <= 1 << 30 or block & block - 1:
+        _refuse(f, "block must be a power of two from 32 on")
+    blocks = -(-k // block)
+    if w_scale.dtype is not torch.float32 and w_scale.dtype is not x.dtype or w_scale.shape != (G, n, blocks):
+        _refuse(f, "w_scale must be [%d][%d][%d] of x's type or float32" % (G, n, blocks))
+    z_group = z_row = 0
+    if w_zero is not None:
+        if w_zero.dtype is not torch.uint8 or w_zero.shape != (G, n, blocks):
+            _refuse(f, "w_zero must be uint8 [%d][%d][%d]" % (G, n, blocks))
+        z_group, z_row, z_value = w_zero.stride()
+        if z_value != 1 and blocks > 1:
+            _no_rows(f, "w_zero")
+    if offsets is not None:
+        if offsets.dtype is not _INT32 or offsets.dim() != 1 or offsets.shape[0] != G + 1 or not offsets.is_contiguous():
+            _bad_offsets(f, G)
+    elif G != 1:
+        _refuse(f, "several groups need offsets")
+    x_row, x_value = x.stride()
+    w_group, w_row, w_value = w.stride()
+    s_group, s_row, s_value = w_scale.stride()
+    if x_value != 1 and k > 1:
+        _no_rows(f, "x")
+    if w_value != 1 and row_bytes > 1:
+        _no_rows(f, "w")
+    if s_value != 1 and blocks > 1:
+        _no_rows(f, "w_scale")
+    if (_grad_enabled() and (x.requires_grad or w_scale.requires_grad or out is not None and out.requires_grad)
+            or _forward_mode._current_level >= 0):
+        _check_unrecorded(f, x, w_scale, out)
+    device = x.get_device()
+    if (device < 0 or w.get_device() != device or w_scale.get_device() != device or w_zero is not None and w_zero.get_device() != device
+            or offsets is not None and offsets.get_device() != device):
+        _not_one_gpu(f)
+    if stream is not None or device != _current_device():
+        with _entered(f, device, stream):
+            return moe_int4_matmul(x, w, w_scale, w_zero, offsets, block, out)
+    given = out
+    if out is None:
+        out, y_row = x.new_empty(R, n), n
+    else:
+        _check_out(out, (R, n), x, f)
+        y_row = out.stride(0) if R > 1 else n
+    args = _Int4Args(R, G, k, n, block, dtype, _DTYPES[w_scale.dtype], 0, x_row, y_row, w_group, w_row, s_group, s_row, z_group, z_row)
+    rc = _lib.moe_int4_matmul(args, x.data_ptr(), w.data_ptr(), w_scale.data_ptr(), None if w_zero is None else w_zero.data_ptr(),
+                              None if offsets is None else offsets.data_ptr(), out.data_ptr(), _raw_stream(device))
     if rc:
         _failed(rc, f)
     if given is not None:
