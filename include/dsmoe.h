@@ -439,6 +439,27 @@ size_t dsmoe_gated_backward_workspace_bytes(const dsmoe_gated_args* args);
 int moe_gated_matmul_backward(const dsmoe_gated_args* args, const void* dh, const void* x, const void* w1, const void* w3, const float* saved,
                               const int32_t* offsets, void* dx, void* dw1, void* dw3, void* workspace, void* stream);
 
+/*
+ * The norm over all gradients together, and clipping by it:
+ *   norm = sqrt(sum over all values of grad^2)      out = grad * min(1, max_norm / (norm + eps)), rounded to dtype once
+ * Squares and sums are in 64 bits, norm device float.  An infinity or NaN among the gradients shows in norm (infinity: finite values become zero,
+ * infinite ones NaN; NaN: everything becomes NaN).
+ *   grads HOST array of `count` tensors: rows of `width` values next to each other, grad_stride (out_stride) values from row to row; a
+ *   tensor without gaps is one row.  out may be grad itself, with the same strides; apart from that outputs must overlap neither each
+ *   other nor gradients.  The array is read before the call returns.
+ *   workspace device, dsmoe_clip_workspace_bytes() bytes, 256-byte aligned.
+ * count 1 .. 2^20, rows 0 .. 2^31 - 1, width 0 .. 2^40 (with several rows 2^31 - 1), at most 2^44 values in a tensor; dtype is the tensor's.
+ */
+typedef struct {
+  const void* grad;
+  void* out; /* moe_grad_norm: not looked at */
+  int64_t rows, width, grad_stride, out_stride;
+  int32_t dtype, pad; /* pad 0 */
+} dsmoe_grad;
+size_t dsmoe_clip_workspace_bytes(void);
+int moe_grad_norm(const dsmoe_grad* grads, int32_t count, float* norm, void* workspace, void* stream);
+int moe_clip_grads(const dsmoe_grad* grads, int32_t count, float max_norm, float eps, float* norm, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

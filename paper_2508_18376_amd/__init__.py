@@ -46,6 +46,8 @@ _OPERATOR_NAMES = (
     "moe_int4_matmul",
     "moe_block_norm",
     "moe_block_norm_backward",
+    "moe_grad_norm",
+    "moe_clip_grads",
 )
 __all__ = list(_BINDING_NAMES + _OPERATOR_NAMES)
 

@@ -1,5 +1,6 @@
 // C ABI of the operators beside the layer (see include/dsmoe.h): argument checks and launches.
 #include "block_norm.h"
+#include "clip_grads.h"
 #include "gated.h"
 #include "grouped.h"
 #include "int4_matmul.h"
@@ -71,6 +72,19 @@ BlockNormArgs norm_args(const dsmoe_block_norm_args* a, const void* x, const voi
   n.offset = a->weight_offset;
   n.eps = a->eps;
   return n;
+}
+
+bool grads_ok(const dsmoe_grad* grads, int32_t count, bool written, const float* norm, const void* workspace) {
+  if (!grads || count < 1 || count > 1 << 20 || !norm || ((uintptr_t)norm & 3) != 0 || !workspace || ((uintptr_t)workspace & 255) != 0) return false;
+  for (int32_t i = 0; i < count; ++i) {
+    const dsmoe_grad& g = grads[i];
+    if (!float_type(g.dtype) || g.rows < 0 || g.rows > INT32_MAX || g.width < 0 || g.width > (g.rows > 1 ? (int64_t)INT32_MAX : (int64_t)1 << 40)) return false;
+    if (g.rows == 0 || g.width == 0) continue;
+    if (g.rows > ((int64_t)1 << 44) / g.width || !g.grad || !aligned_to(g.grad, g.dtype) || (g.rows > 1 && !in_stride(g.grad_stride))) return false;
+    if (written && (!g.out || !aligned_to(g.out, g.dtype) || (g.rows > 1 && !out_stride(g.out_stride, g.width)))) return false;
+    if (written && g.out == g.grad && g.rows > 1 && g.out_stride != g.grad_stride) return false;
+  }
+  return true;
 }
 
 bool gated_args_ok(const dsmoe_gated_args* a) {
@@ -323,6 +337,18 @@ int moe_gated_matmul_backward(const dsmoe_gated_args* args, const void* dh, cons
   g.dw1 = dw1;
   g.dw3 = dw3;
   return status(launch_gated_backward(g, (hipStream_t)stream));
+}
+
+size_t dsmoe_clip_workspace_bytes(void) { return clip_grads_bytes(); }
+
+int moe_grad_norm(const dsmoe_grad* grads, int32_t count, float* norm, void* workspace, void* stream) {
+  if (!grads_ok(grads, count, false, norm, workspace)) return DSMOE_EINVAL;
+  return status(launch_clip_grads(grads, count, false, 0.f, 0.f, norm, (double*)workspace, (hipStream_t)stream));
+}
+
+int moe_clip_grads(const dsmoe_grad* grads, int32_t count, float max_norm, float eps, float* norm, void* workspace, void* stream) {
+  if (!grads_ok(grads, count, true, norm, workspace) || !(max_norm >= 0.f) || !(eps >= 0.f)) return DSMOE_EINVAL;
+  return status(launch_clip_grads(grads, count, true, max_norm, eps, norm, (double*)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 """The operators beside the layer (include/dsmoe.h): products over groups of rows with their gradients, the gated half of a block with its
-gradients, products with weights in 8-bit integers and in 4 bits, and the norms around a block.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
+gradients, products with weights in 8-bit integers and in 4 bits, the norms around a block,
+and the norm over all gradients with clipping.  Same names as the C ABI, on torch tensors on the GPU; outputs and workspaces are torch allocations on the stream that
 the call runs on (the current one, or `stream`).  A call that does not fit its tensors raises DsmoeError before anything is launched.
 
 Nothing is recorded for automatic differentiation: the gradients are operators of their own.  While gradients are being recorded, tensors that need them
@@ -38,6 +39,11 @@ class _Int4Args(ctypes.Structure):
                                                  "zero_group_stride", "zero_row_stride")])
 
 
+class _Grad(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("grad", "out")] + [(n, ctypes.c_int64) for n in ("rows", "width", "grad_stride", "out_stride")]
+                + [(n, ctypes.c_int32) for n in ("dtype", "pad")])
+
+
 ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
 
 
@@ -57,12 +63,15 @@ def _declare(L):
     L.dsmoe_gated_workspace_bytes.argtypes = L.dsmoe_gated_backward_workspace_bytes.argtypes = [gated]
     L.moe_gated_matmul.argtypes = [gated] + [vp] * 8
     L.moe_gated_matmul_backward.argtypes = [gated] + [vp] * 11
+    L.moe_grad_norm.argtypes = [ctypes.POINTER(_Grad), i32, vp, vp, vp]
+    L.moe_clip_grads.argtypes = [ctypes.POINTER(_Grad), i32, ctypes.c_float, ctypes.c_float, vp, vp, vp]
+    L.dsmoe_clip_workspace_bytes.argtypes = []
     L.moe_int4_matmul.argtypes = [ctypes.POINTER(_Int4Args)] + [vp] * 7
     for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes,
-              L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes):
+              L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes, L.dsmoe_clip_workspace_bytes):
         f.restype = ctypes.c_size_t
     for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward, L.moe_gated_matmul,
-              L.moe_gated_matmul_backward, L.moe_int4_matmul):
+              L.moe_gated_matmul_backward, L.moe_int4_matmul, L.moe_grad_norm, L.moe_clip_grads):
         f.restype = ctypes.c_int
 
 
@@ -585,3 +594,105 @@ def moe_block_norm_backward(dy, dh, x, stats, *, branch, branch_weight, weight, 
     if rc:
         _failed(rc, f)
     return out
+
+
+def _rows_of(f, name, t, out):
+    """(rows, width, stride, stride of out): what the library takes a tensor as, and another one that is written value for value."""
+    if t.is_contiguous() and out.is_contiguous():
+        return 1, t.numel(), 0, 0
+    dims = sorted(((s, o, n) for n, s, o in zip(t.shape, t.stride(), out.stride()) if n > 1), reverse=True)
+    merged = []
+    for s, o, n in dims:  # (s, o: strides; an outer dimension that goes on where the inner one ends is one with it)
+        if merged and merged[-1][0] == s * n and merged[-1][1] == o * n:
+            merged[-1] = (s, o, merged[-1][2] * n)
+        else:
+            merged.append((s, o, n))
+    if not merged:
+        return 1, t.numel(), 0, 0
+    if len(merged) > 2 or merged[-1][:2] != (1, 1):
+        _refuse(f, "%s: gradients must be dense, or rows of values next to each other" % name)
+    if len(merged) == 1:
+        return 1, merged[0][2], 0, 0
+    (s, o, rows), (_, _, width) = merged
+    if o < width:
+        _refuse(f, "%s: rows that are written must not overlap" % name)
+    return rows, width, s, o
+
+
+def _grads(f, grads, out):
+    """The library's array of the tensors, and their GPU."""
+    if not isinstance(grads, (list, tuple)) or not grads:
+        _refuse(f, "grads must be a list of tensors, of at least one")
+    if len(grads) > 1 << 20:
+        _refuse(f, "at most 2^20 gradients")
+    if out is not grads:
+        if not isinstance(out, (list, tuple)) or len(out) != len(grads):
+            _refuse(f, "out must be a list of as many tensors as grads")
+    array = (_Grad * len(grads))()
+    device, elsewhere = grads[0].get_device(), False
+    for i, (e, t, o) in enumerate(zip(array, grads, out)):
+        dtype = _DTYPES.get(t.dtype)
+        if dtype is None:
+            _refuse(f, "gradients must be bfloat16, float16 or float32")
+        if o is not t and (o.shape != t.shape or o.dtype is not t.dtype):
+            _refuse(f, "out[%d] must have its gradient's shape and type" % i)
+        if _grad_enabled() and (t.requires_grad or o.requires_grad) or _forward_mode._current_level >= 0:
+            _check_unrecorded(f, t, o)
+        e.rows, e.width, e.grad_stride, e.out_stride = _rows_of(f, "grads[%d]" % i, t, o)
+        if t.get_device() != device or o.get_device() != device:
+            elsewhere = True
+        e.grad, e.out, e.dtype = t.data_ptr(), o.data_ptr(), dtype
+    if device < 0 or elsewhere:
+        _not_one_gpu(f)
+    return array, device
+
+
+def moe_grad_norm(grads, stream=None):
+    """The norm over all gradients together, sqrt(sum of all squares), as a float32 tensor without dimensions; squares and sums are in 64 bits.
+
+    grads: a list of tensors on one GPU, bf16, f16 or f32 in any mixture, each dense or rows of values next to each other."""
+    f = "moe_grad_norm"
+    array, device = _grads(f, grads, grads)
+    if stream is not None or device != _current_device():
+        with _entered(f, device, stream):
+            return moe_grad_norm(grads)
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+    workspace = torch.empty(_lib.dsmoe_clip_workspace_bytes(), dtype=torch.uint8, device=norm.device)
+    rc = _lib.moe_grad_norm(array, len(grads), norm.data_ptr(), workspace.data_ptr(), _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    return norm
+
+
+def moe_clip_grads(grads, max_norm, eps=1e-6, out=None, stream=None):
+    """(clipped, norm): each gradient times min(1, max_norm / (norm + eps)), with the norm of moe_grad_norm.
+
+    out: the tensors that are written and returned, of the gradients' shapes and types; `grads` itself to clip in place; None for new ones.  They must
+    overlap neither each other nor (but for its own) a gradient.  Nothing waits for the GPU: an infinity or NaN shows in norm."""
+    f = "moe_clip_grads"
+    if not max_norm >= 0 or not eps >= 0:
+        _refuse(f, "max_norm and eps must not be negative")
+    given = out
+    if out is None:
+        if not isinstance(grads, (list, tuple)):
+            _refuse(f, "grads must be a list of tensors, of at least one")
+        out = []  # filled below, on the stream that the call runs on
+    else:
+        if isinstance(out, (list, tuple)) and len({t.data_ptr() for t in out if t.numel()}) != sum(1 for t in out if t.numel()):
+            _refuse(f, "out must not hold a tensor twice")
+    array, device = _grads(f, grads, grads if given is None else out)
+    if stream is not None or device != _current_device():
+        with _entered(f, device, stream):
+            return moe_clip_grads(grads, max_norm, eps, given)
+    if given is None:
+        out = [torch.empty_like(t) for t in grads]
+        array, _ = _grads(f, grads, out)
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+    workspace = torch.empty(_lib.dsmoe_clip_workspace_bytes(), dtype=torch.uint8, device=norm.device)
+    rc = _lib.moe_clip_grads(array, len(grads), max_norm, eps, norm.data_ptr(), workspace.data_ptr(), _raw_stream(device))
+    if rc:
+        _failed(rc, f)
+    if given is not None:
+        for t in given:
+            _written(t)
+    return out, norm
