@@ -20,6 +20,8 @@ struct Int4Args {
 };
 
 hipError_t launch_int4_plain(const Int4Args& a, hipStream_t s);
+bool int4_stream_fits(const Int4Args& a);
+hipError_t launch_int4_stream(const Int4Args& a, hipStream_t s);
 hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s);
 
 __device__ __forceinline__ float int4_scale(const Int4Args& a, int64_t i) { return elem_to_f32(a.scale + i * elem_bytes(a.scale_type), a.scale_type); }

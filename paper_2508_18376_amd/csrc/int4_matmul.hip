@@ -3,6 +3,8 @@
 
 namespace dsmoe {
 
-hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s) { return launch_int4_plain(a, s); }
+hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s) {
+  return int4_stream_fits(a) ? launch_int4_stream(a, s) : launch_int4_plain(a, s);
+}
 
 }  // namespace dsmoe
