@@ -400,7 +400,8 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
  * uint8, shaped like it, or NULL: 8 everywhere.  block: a power of two from 32 on.  offsets as above, or NULL for one group of all rows
  * (groups = 1).  Rows of w on 16 bytes are faster.  Rows of no group: zeros.
  *   In 16-bit types calls of many rows round each weight (q - z) s to dtype once (f16: after a power of two for each output channel has brought
- *   it into range); sums are in 32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
+ * *   it into range); sums are in 32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
+ *   workspace as for moe_grouped_matmul, dsmoe_int4_workspace_bytes(args) bytes or NULL.
  * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
  */
 typedef struct {
@@ -410,8 +411,9 @@ typedef struct {
   int64_t w_group_stride, w_row_stride; /* in bytes */
   int64_t scale_group_stride, scale_row_stride, zero_group_stride, zero_row_stride;
 } dsmoe_int4_args;
+size_t dsmoe_int4_workspace_bytes(const dsmoe_int4_args* args);
 int moe_int4_matmul(const dsmoe_int4_args* args, const void* x, const uint8_t* w, const void* w_scale, const uint8_t* w_zero,
-                    const int32_t* offsets, void* y, void* stream);
+                    const int32_t* offsets, void* y, void* workspace, void* stream);
 
 /*
  * The gated half of a block of experts (Eq. 4 up to W2) over groups of rows, both projections, the activation and the product in one:

@@ -17,11 +17,17 @@ struct Int4Args {
   int64_t s_row, s_group, z_row, z_group;         // in values (s: of scale_type)
   int32_t R, G, N, K, type, scale_type, shift;    // a block has 2^shift values
   int32_t blocks;
+  int32_t parts;  // of the contraction (int4_short.hip), whose sums go to the workspace
+  char* partial;  // workspace, or nullptr: none is split
 };
 
 hipError_t launch_int4_plain(const Int4Args& a, hipStream_t s);
 bool int4_stream_fits(const Int4Args& a);
 hipError_t launch_int4_stream(const Int4Args& a, hipStream_t s);
+bool int4_short_fits(const Int4Args& a);
+size_t int4_short_bytes(const Int4Args& a);  // what a's pointers and strides are does not matter
+hipError_t launch_int4_short(Int4Args a, hipStream_t s);
+size_t int4_workspace_bytes(const Int4Args& a);
 hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s);
 
 __device__ __forceinline__ float int4_scale(const Int4Args& a, int64_t i) { return elem_to_f32(a.scale + i * elem_bytes(a.scale_type), a.scale_type); }

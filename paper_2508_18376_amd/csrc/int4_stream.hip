@@ -1,27 +1,16 @@
-// Products with weights in 4 bits for groups of few rows, where the weights' stream is what counts: they go straight into registers, 16-bit x.
+// Products with weights in 4 bits for few rows and few output channels, any alignment, 16-bit x: the weights go straight into registers, and the contraction is
+// dealt out among the wavefronts of a workgroup, so that all of the weights are under way at once.
 //
-// A workgroup takes 64 output channels for up to 32 rows of a group.  Its wavefronts deal the contraction out among themselves in steps of 128 values and add
-// their sums up through LDS at the end.  Products are 16 x 16 matrix instructions of 32 contraction values with x as the first operand, so that a lane
-// has one output channel, whose scale and zero point it loads itself.
-//
-// A step is spans of SPAN = 128, 64 or 32 values that lie in one block each.  Lane 16 q + i has channel i of sixteen, and of a span its q-th quarter, so that
-// its 4-bit weights are one load (16, 8 or 4 bytes).  Eight weights are a word; with p = its 4-bit numbers j and j + 4 in the two halves, moved to the top of
-// the mantissa, (1 + q[j] / 16, 1 + q[j + 4] / 16) is one shift and one and-or of all of p: half an instruction a weight.  The rest is linear:
-//   sum of x (q - z) s = 16 s sum of x (1 + q / 16) - (16 + z) s sum of x
-// with the sum of x from the same matrix instructions against ones.  The terms are up to some seven times larger than x (q - z) / 16, which costs three bits of
-// the sums' 24.  x is brought to the order of the weights' pairs by four byte permutations for eight values.
+// A workgroup takes 64 output channels for up to 32 rows of a group.  Its wavefronts take steps of 128 values of the contraction in turn and add their sums up
+// through LDS at the end.  A step is spans of SPAN = 128, 64 or 32 values that lie in one block each: lane 16 q + i has channel i of sixteen, and of a span its
+// q-th quarter, so that its weights of a span are one load (16, 8 or 4 bytes).
 #include <type_traits>
 
-#include "int4_matmul.h"
+#include "int4_widen.h"
 
 namespace dsmoe {
 
 namespace {
-
-typedef __bf16 qbf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 qf16x8 __attribute__((ext_vector_type(8)));
-typedef int qi32x4 __attribute__((ext_vector_type(4)));
-typedef float qf32x4 __attribute__((ext_vector_type(4)));
 
 struct Yes {
   static constexpr bool value = true;
@@ -31,37 +20,6 @@ struct No {
 };
 
 constexpr int kCols4 = 64, kJ4 = kCols4 / 16, kRowFloats4 = kCols4 + 4;
-
-template <int TY>
-struct Unit {
-  static constexpr uint32_t one = TY == kElemBF16 ? 0x3f803f80u : 0x3c003c00u, mask = TY == kElemBF16 ? 0x00780078u : 0x03c003c0u;
-  static constexpr int up = TY == kElemBF16 ? 3 : 6;  // where the mantissa's top four bits are
-};
-
-template <int TY>
-__device__ __forceinline__ void mac4(qf32x4& c, const qi32x4& a, const qi32x4& b) {
-  if constexpr (TY == kElemBF16)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qbf16x8, a), __builtin_bit_cast(qbf16x8, b), c, 0, 0, 0);
-  else
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(qf16x8, a), __builtin_bit_cast(qf16x8, b), c, 0, 0, 0);
-}
-
-// eight weights as 1 + q / 16, in pairs (j, j + 4)
-template <int TY>
-__device__ __forceinline__ qi32x4 widened(uint32_t w) {
-  qi32x4 v;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int by = 4 * j - Unit<TY>::up;
-    v[j] = (int)(((by < 0 ? w << -by : w >> by) & Unit<TY>::mask) | Unit<TY>::one);
-  }
-  return v;
-}
-// eight values of x in the same order
-__device__ __forceinline__ qi32x4 paired(const uint32_t* x) {
-  return qi32x4{(int)__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), (int)__builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
-                (int)__builtin_amdgcn_perm(x[3], x[1], 0x05040100u), (int)__builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
-}
 
 // Loads go through buffers: a base in scalar registers, an offset of 32 bits in each lane and a scalar one.  (From pointers the compiler keeps a 64-bit
 // address in each lane for each load of the loop, which leaves no registers for the loads.)  An offset from kBeyond on is out of bounds: it loads zero.
@@ -201,7 +159,7 @@ __global__ __launch_bounds__(64 * W, 2) void int4_stream_kernel(Int4Args a) {
         qi32x4 x[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-          x[r] = paired(t.x[r][p][m]);
+          x[r] = paired(qi32x4{(int)t.x[r][p][m][0], (int)t.x[r][p][m][1], (int)t.x[r][p][m][2], (int)t.x[r][p][m][3]});
           mac4<TY>(sum[r], x[r], ones);
         }
 #pragma unroll
@@ -213,9 +171,8 @@ __global__ __launch_bounds__(64 * W, 2) void int4_stream_kernel(Int4Args a) {
       }
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const float s = S32 ? __uint_as_float(t.s[j][p]) : TY == kElemBF16 ? __uint_as_float(p & 1 ? t.s[j][p / 2] & 0xffff0000u : t.s[j][p / 2] << 16)
-                                                                       : (float)__builtin_bit_cast(_Float16, (uint16_t)(t.s[j][p / 2] >> (16 * (p & 1))));
-        const float z = 1.f + (float)((t.z[j] | no_zeros) >> (8 * p) & 0xff) * (1.f / 16);
+        const float s = scale_of<TY, S32>(S32 ? t.s[j][p] : t.s[j][p / 2] >> (16 * (p & 1)) & 0xffff);
+        const float z = zero_of((t.z[j] | no_zeros) >> (8 * p) & 0xff);
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll

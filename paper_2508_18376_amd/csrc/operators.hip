@@ -87,6 +87,32 @@ bool grads_ok(const dsmoe_grad* grads, int32_t count, bool written, const float*
   return true;
 }
 
+bool int4_args_ok(const dsmoe_int4_args* a) {
+  return a && sizes_ok(a->rows, a->groups, a->k, a->n) && float_type(a->dtype) && (a->scale_dtype == a->dtype || a->scale_dtype == DSMOE_F32) &&
+         a->block >= 32 && (a->block & (a->block - 1)) == 0 && row_tiles_bound(a->rows, a->groups, true, 128) * tiles(a->n, 128) <= kMostPieces;
+}
+Int4Args int4_args(const dsmoe_int4_args* a) {
+  const int64_t e = elem_bytes(a->dtype);
+  Int4Args g = {};
+  g.x_row = a->x_stride * e;
+  g.y_row = a->y_stride * e;
+  g.w_row = a->w_row_stride;
+  g.w_group = a->w_group_stride;
+  g.s_row = a->scale_row_stride;
+  g.s_group = a->scale_group_stride;
+  g.z_row = a->zero_row_stride;
+  g.z_group = a->zero_group_stride;
+  g.R = a->rows;
+  g.G = a->groups;
+  g.N = a->n;
+  g.K = a->k;
+  g.type = a->dtype;
+  g.scale_type = a->scale_dtype;
+  g.shift = __builtin_ctz((unsigned)a->block);
+  g.blocks = (int32_t)tiles(a->k, a->block);
+  return g;
+}
+
 bool gated_args_ok(const dsmoe_gated_args* a) {
   return a && sizes_ok(a->rows, a->groups, a->k, a->n) && float_type(a->dtype) && (a->activation == DSMOE_SILU || a->activation == DSMOE_GELU_TANH) &&
          in_stride(a->x_stride) && in_stride(a->w_group_stride) && in_stride(a->w_row_stride) &&
@@ -218,43 +244,32 @@ int moe_int8_matmul(const void* x, int64_t x_stride, const int8_t* w, int64_t w_
   return status(launch_int8_matmul(a, (hipStream_t)stream));
 }
 
+size_t dsmoe_int4_workspace_bytes(const dsmoe_int4_args* args) {
+  static const int32_t some = 0;
+  if (!int4_args_ok(args)) return 0;
+  Int4Args g = int4_args(args);
+  g.off = &some;
+  return int4_workspace_bytes(g);
+}
+
 int moe_int4_matmul(const dsmoe_int4_args* args, const void* x, const uint8_t* w, const void* w_scale, const uint8_t* w_zero,
-                    const int32_t* offsets, void* y, void* stream) {
+                    const int32_t* offsets, void* y, void* workspace, void* stream) {
   const dsmoe_int4_args* a = args;
-  if (!a || !sizes_ok(a->rows, a->groups, a->k, a->n) || !float_type(a->dtype) || (a->scale_dtype != a->dtype && a->scale_dtype != DSMOE_F32) ||
-      a->block < 32 || (a->block & (a->block - 1)) != 0 || (!offsets && a->groups != 1))
-    return DSMOE_EINVAL;
+  if (!int4_args_ok(a) || (!offsets && a->groups != 1) || ((uintptr_t)workspace & 255) != 0) return DSMOE_EINVAL;
   if (!in_stride(a->x_stride) || !out_stride(a->y_stride, a->n)) return DSMOE_EINVAL;
   for (const int64_t s : {a->w_group_stride, a->w_row_stride, a->scale_group_stride, a->scale_row_stride})
     if (!in_stride(s)) return DSMOE_EINVAL;
   if (w_zero && (!in_stride(a->zero_group_stride) || !in_stride(a->zero_row_stride))) return DSMOE_EINVAL;
   if (a->rows == 0) return DSMOE_OK;
   if (!x || !w || !w_scale || !y || !aligned_to(x, a->dtype) || !aligned_to(y, a->dtype) || !aligned_to(w_scale, a->scale_dtype)) return DSMOE_EINVAL;
-  if (row_tiles_bound(a->rows, a->groups, offsets != nullptr, 128) * tiles(a->n, 128) > kMostPieces) return DSMOE_EINVAL;
-  const int64_t e = elem_bytes(a->dtype);
-  Int4Args g = {};
+  Int4Args g = int4_args(a);
   g.x = (const char*)x;
   g.w = w;
   g.scale = (const char*)w_scale;
   g.zero = w_zero;
   g.off = offsets;
   g.y = (char*)y;
-  g.x_row = a->x_stride * e;
-  g.y_row = a->y_stride * e;
-  g.w_row = a->w_row_stride;
-  g.w_group = a->w_group_stride;
-  g.s_row = a->scale_row_stride;
-  g.s_group = a->scale_group_stride;
-  g.z_row = a->zero_row_stride;
-  g.z_group = a->zero_group_stride;
-  g.R = a->rows;
-  g.G = a->groups;
-  g.N = a->n;
-  g.K = a->k;
-  g.type = a->dtype;
-  g.scale_type = a->scale_dtype;
-  g.shift = __builtin_ctz((unsigned)a->block);
-  g.blocks = (int32_t)tiles(a->k, a->block);
+  g.partial = (char*)workspace;
   return status(launch_int4_matmul(g, (hipStream_t)stream));
 }
 

@@ -66,9 +66,10 @@ def _declare(L):
     L.moe_grad_norm.argtypes = [ctypes.POINTER(_Grad), i32, vp, vp, vp]
     L.moe_clip_grads.argtypes = [ctypes.POINTER(_Grad), i32, ctypes.c_float, ctypes.c_float, vp, vp, vp]
     L.dsmoe_clip_workspace_bytes.argtypes = []
-    L.moe_int4_matmul.argtypes = [ctypes.POINTER(_Int4Args)] + [vp] * 7
+    L.dsmoe_int4_workspace_bytes.argtypes = [ctypes.POINTER(_Int4Args)]
+    L.moe_int4_matmul.argtypes = [ctypes.POINTER(_Int4Args)] + [vp] * 8
     for f in (L.dsmoe_grouped_workspace_bytes, L.dsmoe_grouped_dw_workspace_bytes, L.dsmoe_int8_workspace_bytes, L.dsmoe_block_norm_workspace_bytes,
-              L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes, L.dsmoe_clip_workspace_bytes):
+              L.dsmoe_gated_workspace_bytes, L.dsmoe_gated_backward_workspace_bytes, L.dsmoe_clip_workspace_bytes, L.dsmoe_int4_workspace_bytes):
         f.restype = ctypes.c_size_t
     for f in (L.moe_grouped_matmul, L.moe_grouped_matmul_dw, L.moe_int8_matmul, L.moe_block_norm, L.moe_block_norm_backward, L.moe_gated_matmul,
               L.moe_gated_matmul_backward, L.moe_int4_matmul, L.moe_grad_norm, L.moe_clip_grads):
@@ -484,8 +485,11 @@ def moe_int4_matmul(x, w, w_scale, w_zero=None, offsets=None, block=128, out=Non
         _check_out(out, (R, n), x, f)
         y_row = out.stride(0) if R > 1 else n
     args = _Int4Args(R, G, k, n, block, dtype, _DTYPES[w_scale.dtype], 0, x_row, y_row, w_group, w_row, s_group, s_row, z_group, z_row)
+    size = _lib.dsmoe_int4_workspace_bytes(args)
+    workspace = w.new_empty(size) if size else None
     rc = _lib.moe_int4_matmul(args, x.data_ptr(), w.data_ptr(), w_scale.data_ptr(), None if w_zero is None else w_zero.data_ptr(),
-                              None if offsets is None else offsets.data_ptr(), out.data_ptr(), _raw_stream(device))
+                              None if offsets is None else offsets.data_ptr(), out.data_ptr(), workspace.data_ptr() if size else None,
+                              _raw_stream(device))
     if rc:
         _failed(rc, f)
     if given is not None:

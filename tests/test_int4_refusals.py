@@ -95,7 +95,7 @@ ARGS = dict(rows=10, groups=2, k=64, n=32, block=32, dtype=1, scale_dtype=1, pad
                                 dict(zero_group_stride=-1), dict(zero_row_stride=-1), dict(rows=(1 << 23) + 1), dict(groups=1 << 17), dict(k=(1 << 24) + 1),
                                 dict(rows=1 << 23, n=1 << 24, y_stride=1 << 24)], ids=str)
 def test_boundary(kw):
-    assert _lib.moe_int4_matmul(ops._Int4Args(**dict(ARGS, **kw)), P, P, P, P, P, P, None) == -1
+    assert _lib.moe_int4_matmul(ops._Int4Args(**dict(ARGS, **kw)), P, P, P, P, P, P, None, None) == -1
 
 
 def test_pointers():
@@ -103,12 +103,22 @@ def test_pointers():
     for i in (0, 1, 2, 4, 5):  # (the zero points may be missing)
         p = list(good)
         p[i] = None
-        assert _lib.moe_int4_matmul(a, *p, None) == -1, i
+        assert _lib.moe_int4_matmul(a, *p, None, None) == -1, i
     for i in (0, 2, 5):
         p = list(good)
         p[i] = P + 1
-        assert _lib.moe_int4_matmul(a, *p, None) == -1, i
-    assert _lib.moe_int4_matmul(None, *good, None) == -1
+        assert _lib.moe_int4_matmul(a, *p, None, None) == -1, i
+    assert _lib.moe_int4_matmul(None, *good, None, None) == -1 and _lib.moe_int4_matmul(a, *good, P + 128, None) == -1
+
+
+def test_workspace_sizes():
+    """Few tiles of long sums are split; many, short sums, many rows and fp32 are not."""
+    def size(**kw):
+        return _lib.dsmoe_int4_workspace_bytes(ops._Int4Args(**dict(ARGS, **kw)))
+
+    assert size(rows=1, groups=1, k=4096, n=4096) > 0 and size(rows=1, groups=1, k=256, n=4096) == 0 and size(rows=64, groups=8, k=4096, n=1 << 17) == 0
+    assert size(rows=1, groups=1, k=4096, n=4096, dtype=0, scale_dtype=0) == 0 and size(rows=-1) == 0 and size(block=48) == 0
+    assert _lib.dsmoe_int4_workspace_bytes(None) == 0
 
 
 class OnGpu0:
