@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libdsmoe.so")
 SOURCES = ["api.hip", "route_plan.hip", "pack.hip", "gemm_full.hip", "gemm_mfma.hip", "importance.hip", "thresholds.hip", "router.hip", "transform.hip",
            "operators.hip", "grouped_plain.hip", "grouped_mfma.hip", "grouped_stream.hip", "int8_matmul.hip", "block_norm.hip",
            "gated.hip", "gated_pair.hip", "gated_sum.hip", "int4_matmul.hip", "int4_plain.hip", "int4_stream.hip",
-           "int4_short.hip", "clip_grads.hip"]
+           "int4_short.hip", "int4_tiles.hip", "clip_grads.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -39,6 +39,7 @@ OPERATORS_NO_SCRATCH = {
     "grouped_stream.hip": ("grouped_stream_kernel",),
     "gated_pair.hip": ("grouped_mfma_kernel", "grouped_stream_kernel"),
     "int4_stream.hip": ("int4_stream_kernel",),
+    "int4_tiles.hip": ("int4_tiles_kernel",),
     "int4_short.hip": ("int4_short_kernel",),
     "gated_sum.hip": ("grouped_mfma_kernel", "grouped_stream_kernel"),
 }

@@ -17,6 +17,7 @@ enum GroupedMode : int32_t {
   kOneProduct,   // C_g = A_g B_g
   kGatedPair,    // C_g = f(A_g B_g) * (A_g B2_g)
   kSumOfTwo,     // C_g = A_g B_g + A2_g B2_g
+  kFourBits,     // one product, B in 4 bits along the contraction (see int4_tiles.hip)
 };
 
 // One launch of products C_g = A_g B_g.  Rows are the caller's rows (tokens); a group owns rows [off[g], off[g+1]).

@@ -285,7 +285,8 @@ struct Piece {
   const char *pa, *pb;   // first row (column) of the tile in A and B
   const char *pa2, *pb2; // ... in the second operands.  A sum of two: where their stretch begins, if the piece comes to it
   int until;             // a sum of two: stages until the contraction goes over to the second operands, or ends
-  int row, column;       // a gated pair: of the tile in C
+  int row, column;       // a gated pair, 4 bits: of the tile in C
+  int group, first;      // 4 bits: the group, and where its stretch of the contraction begins
   char* pc;              // first value of the tile in C
   const float *as, *bs;  // 8-bit: factors from the tile's first row and column on
   int m_edge, n_edge;    // rows and columns of the tile that exist
@@ -850,6 +851,11 @@ struct RowsWork {
       p.row = (int)row;
       p.column = n0;
     }
+    if (MODE == kFourBits) {
+      p.group = grp;
+      p.column = n0;
+      p.first = 0;
+    }
     if (MODE == kSumOfTwo) {
       p.pa2 = g.a2 + row * g.a_row;
       p.pb2 = g.b2 + (p.pb - g.b);
@@ -864,8 +870,8 @@ struct RowsWork {
         p.pb += BX ? (int64_t)skip * EB : skip * g.b_row;
         p.pc += (int64_t)skip * elem_bytes(OUT);
         if (TY == kElemI8) p.bs += skip;
-        if (MODE != kOneProduct) p.pb2 += BX ? (int64_t)skip * EB : skip * g.b_row;
-        if (MODE == kGatedPair) p.column += skip;
+        if (MODE == kGatedPair || MODE == kSumOfTwo) p.pb2 += BX ? (int64_t)skip * EB : skip * g.b_row;
+        if (MODE == kGatedPair || MODE == kFourBits) p.column += skip;
       }
     } else if (tile >= split.whole) {
       p.partial = g.partial + ((tile - split.whole) * split.parts + part) * (kPartialBytes / kGT * BM);
@@ -881,7 +887,8 @@ struct RowsWork {
         p.until = (along >= p.until ? stages : p.until) - along;
       }
       p.pa += (int64_t)first * EB;
-      p.pb += BX ? first * g.b_row : (int64_t)first * EB;
+      p.pb += BX ? first * g.b_row : MODE == kFourBits ? first / 2 : (int64_t)first * EB;
+      if (MODE == kFourBits) p.first = first;
       if (MODE == kGatedPair) p.pb2 += first * g.b_row;
     }
     return true;

@@ -27,6 +27,9 @@ hipError_t launch_int4_stream(const Int4Args& a, hipStream_t s);
 bool int4_short_fits(const Int4Args& a);
 size_t int4_short_bytes(const Int4Args& a);  // what a's pointers and strides are does not matter
 hipError_t launch_int4_short(Int4Args a, hipStream_t s);
+bool int4_tiles_fit(const Int4Args& a);
+size_t int4_tiles_bytes(const Int4Args& a);  // what a's pointers and strides are does not matter
+hipError_t launch_int4_tiles(const Int4Args& a, hipStream_t s);
 size_t int4_workspace_bytes(const Int4Args& a);
 hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s);
 

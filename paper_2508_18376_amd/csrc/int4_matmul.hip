@@ -10,10 +10,11 @@ bool short_sizes(const Int4Args& a) { return a.type != kElemF32 && a.R <= 64 * (
 
 }  // namespace
 
-size_t int4_workspace_bytes(const Int4Args& a) { return short_sizes(a) ? int4_short_bytes(a) : 0; }
+size_t int4_workspace_bytes(const Int4Args& a) { return a.type == kElemF32 || a.R == 0 ? 0 : short_sizes(a) ? int4_short_bytes(a) : int4_tiles_bytes(a); }
 
 hipError_t launch_int4_matmul(const Int4Args& a, hipStream_t s) {
   if (short_sizes(a) && int4_short_fits(a)) return launch_int4_short(a, s);
+  if (!short_sizes(a) && int4_tiles_fit(a)) return launch_int4_tiles(a, s);
   return int4_stream_fits(a) ? launch_int4_stream(a, s) : launch_int4_plain(a, s);
 }
 

@@ -1,0 +1,396 @@
+// Products with weights in 4 bits for groups of many rows (16-bit x, rows on 16 bytes): the tiles of grouped_tiles.h, whose weights are widened between the matrix
+// instructions.
+//
+// A stage is 64 values of the contraction; x comes to LDS as in grouped_tiles.h.  Of the weights a thread loads 16 bytes (32 values, all in one block) of two
+// output channels into registers, and writes them to LDS as (q - z) s, rounded to x's type: 23 vector instructions for eight values, and 64 values a thread
+// and stage against 64 matrix instructions, which leave room for seven each.  Two units of LDS hold x, three the widened weights:
+//   stage s - 3, last quarter   the weights of stage s are loaded
+//   stage s - 2, last quarter   the first quarter of them is widened; x of stage s is loaded
+//   stage s - 1                 the others are widened
+// Everything that is under way at a stage's barrier was issued a stage before.
+//
+// The rounding of a weight is of the size of the result's own; the sums of half as many rows would have room beside them for the exact way of the
+// tiles of few rows (int4_widen.h), at twice the weights' traffic and vector instructions.
+#include "grouped_tiles.h"
+#include "int4_matmul.h"
+
+namespace dsmoe {
+
+namespace {
+
+// Weights of a thread for one stage, as loaded.
+struct Raw {
+  uint32_t q[8];
+  float s[2], z[2];
+};
+
+// The weights' way from memory to LDS: channels t / 2 and 128 + t / 2 of the tile, half t % 2 of the stage.
+// S32: scales in fp32.
+template <int TY, bool S32>
+struct Widen {
+  static constexpr int EB = S32 ? 4 : 2;
+  uint32_t w_off[2], s_off[2], z_off[2], to[4];
+  int exponent[2], no_zeros;
+  const char *pw, *ps, *pz;  // the tile's first channel at the piece's first stage; of the scales and zero points, the first block
+  int extent, cols;
+
+  __device__ __forceinline__ void lanes(const Int4Args& a, uint32_t ring, int tid) {
+    const int c = tid >> 1, h = tid & 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = ring + c * 128 + swz_wide(c, h * 4 + j) * 16;
+    no_zeros = a.zero ? 0 : 8;
+  }
+  // cols: channels that exist (the last one again behind them)
+  __device__ __forceinline__ void tile(const Int4Args& a, const Piece& p, int tid) {
+    cols = max(p.n_edge, 1);
+    const int64_t ch = p.column;
+    pw = (const char*)p.pb;
+    ps = a.scale + (p.group * a.s_group + ch * a.s_row) * EB;
+    pz = (const char*)a.zero + p.group * a.z_group + ch * a.z_row;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t c = min(i * 128 + (tid >> 1), cols - 1);
+      w_off[i] = c * (uint32_t)a.w_row + (tid & 1) * 16;
+      s_off[i] = c * (uint32_t)a.s_row * EB;
+      z_off[i] = a.zero ? c * (uint32_t)a.z_row : kOutOfBounds;
+    }
+    if (TY == kElemF16) {  // (two threads a channel)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t top = 0;
+        for (int j = tid & 1; j < a.blocks; j += 2)
+          top = max(top, __float_as_uint(elem_to_f32(ps + s_off[i] + (int64_t)j * EB, S32 ? kElemF32 : TY)) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        exponent[i] = int4_exponent(top);
+      }
+    }
+  }
+  // stage st of the piece
+  __device__ __forceinline__ void load(const Int4Args& a, const Piece& p, int st, Raw& r, int tid) const {
+    const int k0 = p.first + st * 64, left = min(a.K - k0, 64);
+    const __amdgpu_buffer_rsrc_t bw = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pw + st * 32), 0, (int)((cols - 1) * a.w_row + left / 2), 0x00020000);
+    const int block = min((k0 + (tid & 1) * 32) >> a.shift, a.blocks - 1);
+    const __amdgpu_buffer_rsrc_t bs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(ps), 0, (int)(kOutOfBounds - 1), 0x00020000);
+    const __amdgpu_buffer_rsrc_t bz = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pz), 0, (int)(kOutOfBounds - 1), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const auto v = __builtin_amdgcn_raw_buffer_load_b128(bw, (int)w_off[i], 0, 0);
+      __builtin_memcpy(r.q + 4 * i, &v, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      r.s[i] = __uint_as_float(S32 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(bs, (int)(s_off[i] + block * EB), 0, 0)
+                                   : (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(bs, (int)(s_off[i] + block * EB), 0, 0));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r.z[i] = __uint_as_float((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(bz, (int)(z_off[i] + block), 0, 0));
+  }
+  // scales and zero points from their bits: (q - z) s = q s + z, z = -z s
+  __device__ __forceinline__ void ready(Raw& r) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t bits = __float_as_uint(r.s[i]);
+      float s = r.s[i];
+      if (!S32 && TY == kElemBF16) s = __uint_as_float(bits << 16);
+      if (!S32 && TY == kElemF16) s = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+      if (TY == kElemF16) s = ldexpf(s, -exponent[i]);
+      r.s[i] = s;
+      r.z[i] = -(float)(__float_as_uint(r.z[i]) | no_zeros) * s;
+    }
+  }
+  // eight of a thread's weights, to the unit at `unit`
+  __device__ __forceinline__ void put(const Raw& r, int k, uint32_t unit) const {
+    const uint32_t lo = r.q[k] & 0x0f0f0f0fu, hi = r.q[k] >> 4 & 0x0f0f0f0fu;
+    const float s = r.s[k >> 2], z = r.z[k >> 2];
+    gi32x4 out;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      out[d] = (int)pack2<TY>(fmaf((float)(lo >> (8 * d) & 0xff), s, z), fmaf((float)(hi >> (8 * d) & 0xff), s, z));
+    *(__attribute__((address_space(3))) gi32x4*)(uintptr_t)(to[k & 3] + unit + (k >> 2) * (128 * 128)) = out;
+  }
+};
+
+// Half precision: sums times their channel's power of two.  factor: of the tile's channels, in LDS.
+template <int MI, int NI>
+__device__ __forceinline__ void write_scaled(const GroupedArgs& g, const Piece& p, const gf32x16 (&acc)[MI][NI], const float* factor, char* turn, int wm, int wn,
+                                             int w, int lane) {
+  const int r32 = lane & 31, half = lane >> 5;
+  if (p.partial != nullptr) {  // as write_tile
+    char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
+#pragma unroll
+    for (int a = 0; a < MI; ++a)
+#pragma unroll
+      for (int b = 0; b < NI; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const gf32x4 f = *(const gf32x4*)(factor + wn + b * 32 + 8 * q + 4 * half);
+          const gf32x16& c = acc[a][b];
+          *(gf32x4*)(to + ((a * NI + b) * 4 + q) * 1024) = gf32x4{c[4 * q] * f[0], c[4 * q + 1] * f[1], c[4 * q + 2] * f[2], c[4 * q + 3] * f[3]};
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    return;
+  }
+  constexpr int LPR = 16;  // 64 columns of 32 bits a row
+#pragma unroll
+  for (int a = 0; a < MI; ++a)
+#pragma unroll
+    for (int b0 = 0; b0 < NI; b0 += 2) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const gf32x16& c = acc[a][b0 + b];
+          *(gf32x4*)(turn + r32 * 256 + ((b * 8 + q * 2 + half) ^ (r32 & 15)) * 16) = gf32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const int ch = lane % LPR, c = wn + b0 * 32 + ch * 4;
+      const gf32x4 f = *(const gf32x4*)(factor + c);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int rr = k * 4 + lane / LPR, r = wm + a * 32 + rr;
+        const gf32x4 v = *(const gf32x4*)(turn + rr * 256 + (ch ^ (rr & 15)) * 16);
+        if (r < p.m_edge && c < p.n_edge) *(uint2*)(p.pc + r * g.c_row + (int64_t)c * 2) = make_uint2(pack2<kElemF16>(v[0] * f[0], v[1] * f[1]), pack2<kElemF16>(v[2] * f[2], v[3] * f[3]));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+}
+
+constexpr uint32_t kWideB = 2 * kUnit;  // the widened weights' three units; x has the two before them
+
+template <int TY, int BM, bool S32, class Next>
+__device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4Args& a, char* lds, Next&& piece) {
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t ring = lds_address(lds), mine = ring + (uint32_t)w * 1024;
+  Feed<false> fa;
+  Widen<TY, S32> fb;
+  fa.lanes(g.a_row, tid);
+  uint32_t beyond = 0, tail = 0;
+  gi32x4 rs;
+  auto stages = [&](const Piece& p) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane((p.K + 63) / 64); };
+  auto load_a = [&](bool last) __attribute__((always_inline)) {
+    rs = fa.next(last);
+    tail = last ? beyond : 0;
+  };
+  auto one_a = [&](int q, uint32_t place) __attribute__((always_inline)) { load_to_lds(rs, mine + place, q * 4096, fa.voff[q] | tail); };
+  Raw r0, cur, nxt;  // weights of the first stage, the ones that are being widened, and the next ones
+  // x of a piece's first two stages
+  auto first_loads = [&](const Piece& p) __attribute__((always_inline)) {
+    const int kb = ((p.K * 2 + 127) & 127) + 1, n = stages(p);
+    fa.tile(p.pa, g.a_row, p.m_edge, kb);
+    beyond = swz_wide(tid >> 3, tid & 7) * 16 >= kb ? kOutOfBounds : 0;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      if (st >= n) continue;
+      load_a(st == n - 1);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) one_a(q, st * kUnit);
+    }
+  };
+  Piece p, after;
+  int i = 0;
+  bool more = piece(i, p);
+  if (!more) return;
+  first_loads(p);
+  while (more) {
+    more = piece(++i, after);
+    const int n = stages(p);
+    int t = tid;  // (an opaque copy: what follows from it is worked out for this tile, and not kept in registers across the others)
+    asm volatile("" : "+v"(t));
+    // (the weights' first loads wait for the last tile to be written: with them under way before that, its values do not fit the registers)
+    fb.lanes(a, ring + kWideB, t);
+    fb.tile(a, p, t);
+    if (n > 0) fb.load(a, p, 0, r0, t);
+    if (n > 1) fb.load(a, p, 1, cur, t);
+    if (n > 2) fb.load(a, p, 2, nxt, t);
+    if (n > 0) {
+      fb.ready(r0);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) fb.put(r0, k, 0);
+    }
+    if (n > 1) {
+      fb.ready(cur);
+      fb.put(cur, 0, kUnit);
+      fb.put(cur, 1, kUnit);
+    }
+    wait_loads<0>();
+    stage_barrier();
+    auto whole = [&](auto& tile, int wm, int wn, auto MI_, auto NI_) __attribute__((always_inline)) {
+      constexpr int MI = decltype(MI_)::value, NI = decltype(NI_)::value;
+      typedef Tile<TY, false, false, MI, NI> T;
+      int lane = tid & 63;
+      asm volatile("" : "+v"(lane));
+      tile.ra.init(ring, wm, lane);
+      tile.rb.init(ring + kWideB, wn, lane);
+#pragma unroll
+      for (int x = 0; x < MI; ++x)
+#pragma unroll
+        for (int y = 0; y < NI; ++y)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) tile.acc[x][y][v] = 0;
+      typename T::Frags f0, f1;
+      if (n > 0) {
+#pragma unroll
+        for (int k = 0; k < T::READS; ++k) tile.read_k(f0, k, 0, 0, 0);
+      }
+      uint32_t ua = 0, ub = 0;  // of stage st
+      auto turn3 = [](uint32_t u) { return u == 2 * kUnit ? 0 : u + kUnit; };
+      // behind: stages behind this one, 3 for that many and more (each kind its own code: accumulators that come from two sides are copied)
+      auto stage = [&](int st, auto behind) __attribute__((always_inline)) {
+        constexpr int BEHIND = decltype(behind)::value;
+        const uint32_t na = ua ^ kUnit, nb = turn3(ub), nnb = turn3(nb);
+        auto widen = [&](int k) __attribute__((always_inline)) {
+          if (BEHIND >= 1) fb.put(cur, k, nb);
+        };
+        tile.template substep<2>(f0, f1, true, 1, ua, ub, [&](int q) { widen(2 + q); });
+        tile.template substep<2>(f1, f0, true, 2, ua, ub, [&](int q) { widen(4 + q); });
+        tile.template substep<2>(f0, f1, true, 3, ua, ub, [&](int q) { widen(6 + q); });
+        if (BEHIND >= 1) {
+          wait_loads<0>();
+          stage_barrier();
+        }
+        if constexpr (BEHIND >= 2) {
+          cur = nxt;
+          fb.ready(cur);
+          if (BEHIND >= 3) fb.load(a, p, st + 3, nxt, t);
+          load_a(st + 3 == n);
+          tile.template substep<kLoads + 2>(f1, f0, true, 0, na, nb, [&](int q) {
+            if (q < kLoads)
+              one_a(q, ua);
+            else
+              fb.put(cur, q - kLoads, nnb);
+          });
+        } else {
+          tile.template substep<0>(f1, f0, BEHIND >= 1, 0, na, nb, [](int) {});
+        }
+        ua = na;
+        ub = nb;
+      };
+      int st = 0;
+      for (; st + 3 < n; ++st) stage(st, Const<3>());
+      for (; st + 2 < n; ++st) stage(st, Const<2>());
+      for (; st + 1 < n; ++st) stage(st, Const<1>());
+      for (; st < n; ++st) stage(st, Const<0>());
+      float* factor = (float*)(lds + kWideB);  // (the first unit: nobody reads it any more)
+      stage_barrier();
+      if (TY == kElemF16) {
+        if ((t & 1) == 0) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) factor[x * 128 + (t >> 1)] = ldexpf(1.f, fb.exponent[x]);
+        }
+        stage_barrier();
+      }
+      if (more) first_loads(after);
+      char* turn = lds + kWideB + 2 * kUnit + w * (kUnit / 4);
+      if constexpr (TY == kElemF16) {
+        write_scaled<MI, NI>(g, p, tile.acc, factor, turn, wm, wn, w, lane);
+        if (more) stage_barrier();  // (the factors are read)
+      } else {
+        write_tile<TY, TY, kOneProduct, MI, NI>(g, p, tile.acc, Factors<false, MI, NI>(), turn, wm, wn, w, lane, false);
+      }
+    };
+    int mi, ni, wm, wn;
+    tile_shape(p.m_edge, p.n_edge, false, false, w, mi, ni, wm, wn);
+    bool done = false;
+    if constexpr (BM == kGT) {
+      done = mi == 4;
+      if (mi == 4 && ni == 4) {
+        Tile<TY, false, false, 4, 4> t;
+        whole(t, wm, wn, Const<4>(), Const<4>());
+      } else if (mi == 4) {
+        Tile<TY, false, false, 4, 2> t;
+        whole(t, wm, wn, Const<4>(), Const<2>());
+      }
+    }
+    if (done) {
+    } else if (ni == 4) {
+      Tile<TY, false, false, 2, 4> t;
+      whole(t, wm, wn, Const<2>(), Const<4>());
+    } else if (mi == 2) {
+      Tile<TY, false, false, 2, 2> t;
+      whole(t, wm, wn, Const<2>(), Const<2>());
+    } else {
+      Tile<TY, false, false, 1, 2> t;
+      whole(t, wm, wn, Const<1>(), Const<2>());
+    }
+    p = after;
+  }
+}
+
+template <int TY, int BM, bool S32>
+__global__ __launch_bounds__(256, 1) void int4_tiles_kernel(GroupedArgs g, Int4Args a) {
+  extern __shared__ __align__(16) char ring[];
+  typedef RowsWork<TY, TY, false, BM, kFourBits> Work;
+  Work work;
+  work.all.init(g.off, g.G, g.R);
+  work.all.zero_others(g.c, g.c_row, g.N * 2);
+  do_int4_pieces<TY, BM, S32>(g, a, ring, [&](int i, Piece& p) __attribute__((always_inline)) {
+    return work.find(g, p, [&](Work& w) {
+      int tile;
+      return work_of(w.split, w.tiles, blockIdx.x, i, tile, w.part) ? tile : w.tiles;
+    });
+  });
+}
+
+GroupedArgs grouped_args(const Int4Args& a) {
+  GroupedArgs g = {};
+  g.a = a.x;
+  g.b = (const char*)a.w;
+  g.c = a.y;
+  g.off = a.off;
+  g.a_row = a.x_row;
+  g.b_row = a.w_row;
+  g.b_group = a.w_group;
+  g.c_row = a.y_row;
+  g.R = a.R;
+  g.G = a.G;
+  g.N = a.N;
+  g.K = a.K;
+  g.partial = a.partial;
+  return g;
+}
+inline int rows_of_tiles(const GroupedArgs& g) {
+  const int rows = tile_rows(g, kElemBF16);
+  return rows == kShortRows ? 128 : rows;
+}
+
+template <int TY, int BM, bool S32>
+hipError_t launch(GroupedArgs g, const Int4Args& a, hipStream_t s) {
+  static PerDeviceOnce once;
+  hipError_t e = prepare(int4_tiles_kernel<TY, BM, S32>, once);
+  if (e != hipSuccess) return e;
+  const int64_t tiles = most_tiles(g, BM);
+  if (g.partial != nullptr) g.room = rows_room(g, TY, BM);
+  int4_tiles_kernel<TY, BM, S32><<<dim3((unsigned)(g.room.tiles == 0 && 2 * tiles < kWorkgroups ? 2 * tiles : kWorkgroups)), dim3(256), kRingBytes, s>>>(g, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || g.room.tiles == 0) return e;
+  if (g.off == nullptr) {
+    const Split split = split_of((int)tiles, row_stages(g, TY), mean_rows(g, tiles, BM), g.room);
+    if (split.cols || split.whole == tiles) return e;
+  }
+  grouped_join_kernel<TY, TY, false, false, BM, kFourBits><<<dim3(g.room.tiles, BM / 16), dim3(256), 0, s>>>(g, 0, Split{0, 1, 0});
+  return hipGetLastError();
+}
+template <int TY>
+hipError_t launch_type(const Int4Args& a, hipStream_t s) {
+  const GroupedArgs g = grouped_args(a);
+  if (a.scale_type == kElemF32) return rows_of_tiles(g) == 128 ? launch<TY, 128, true>(g, a, s) : launch<TY, kGT, true>(g, a, s);
+  return rows_of_tiles(g) == 128 ? launch<TY, 128, false>(g, a, s) : launch<TY, kGT, false>(g, a, s);
+}
+
+}  // namespace
+
+bool int4_tiles_fit(const Int4Args& a) {
+  const int64_t most = (int64_t)1 << 22;
+  if (a.type == kElemF32 || a.K % 8 != 0 || a.N % 8 != 0) return false;
+  if ((((uintptr_t)a.w | a.w_row | a.w_group) & 15) != 0 || a.w_row > most || a.s_row * 4 > most || (a.zero && a.z_row > most)) return false;
+  return rows_fit(a.x, a.x_row, a.K * 2ll) && rows_fit(a.y, a.y_row, a.N * 2ll);
+}
+size_t int4_tiles_bytes(const Int4Args& a) {
+  const GroupedArgs g = grouped_args(a);
+  const int BM = rows_of_tiles(g);
+  return (size_t)(rows_room(g, kElemBF16, BM).parts * (kPartialBytes / kGT * BM));
+}
+hipError_t launch_int4_tiles(const Int4Args& a, hipStream_t s) { return a.type == kElemBF16 ? launch_type<kElemBF16>(a, s) : launch_type<kElemF16>(a, s); }
+
+}  // namespace dsmoe
