@@ -3,14 +3,18 @@
 //
 // A stage is 64 values of the contraction; x comes to LDS as in grouped_tiles.h.  Of the weights a thread loads 16 bytes (32 values, all in one block) of two
 // output channels into registers, and writes them to LDS as (q - z) s, rounded to x's type: 23 vector instructions for eight values, and 64 values a thread
-// and stage against 64 matrix instructions, which leave room for seven each.  Two units of LDS hold x, three the widened weights:
+// and stage against 64 matrix instructions, which leave room for seven each.  Two units of LDS hold x, two the widened weights:
 //   stage s - 3, last quarter   the weights of stage s are loaded
 //   stage s - 2, last quarter   the first quarter of them is widened; x of stage s is loaded
 //   stage s - 1                 the others are widened
 // Everything that is under way at a stage's barrier was issued a stage before.
 //
-// The rounding of a weight is of the size of the result's own; the sums of half as many rows would have room beside them for the exact way of the
-// tiles of few rows (int4_widen.h), at twice the weights' traffic and vector instructions.
+// Scales and zero points come by themselves, eight blocks of a channel at a time, to a table of sixteen blocks in the rest of LDS: a thread that loaded its
+// channels' for every stage looked up more lines of them than of weights and x together (a compute unit looks up one a clock), and the loads that the
+// matrix instructions wait for queued behind.
+//
+// The rounding of a weight is of the size of the result's own.  The exact way of the tiles of few rows (int4_widen.h) needs a second set of sums, so tiles of half
+// as many rows, at twice the weights' traffic and vector instructions.
 #include "grouped_tiles.h"
 #include "int4_matmul.h"
 
@@ -18,94 +22,149 @@ namespace dsmoe {
 
 namespace {
 
-// Weights of a thread for one stage, as loaded.
+constexpr int kTableBlocks = 8;  // of a half of the table
+// Where they lie in LDS: two units of x, two of the widened weights, the table (or what a tile turns around in).
+constexpr uint32_t kWideB = 2 * kUnit, kTable = 4 * kUnit;
+static_assert(kTable + 2 * kTableBlocks * kGT * 8 <= kRingBytes, "the table fits the last unit");
+
+// Weights of a thread for one stage, as loaded, and their scales: (q - z) s = q s + zs.
 struct Raw {
   uint32_t q[8];
-  float s[2], z[2];
+  float s[2], zs[2];
 };
 
-// The weights' way from memory to LDS: channels t / 2 and 128 + t / 2 of the tile, half t % 2 of the stage.
+// The weights' way from memory to LDS: channels t / 2 and 128 + t / 2 of the tile, half t % 2 of the stage; of the table, channel t.
 // S32: scales in fp32.
 template <int TY, bool S32>
 struct Widen {
-  static constexpr int EB = S32 ? 4 : 2;
-  uint32_t w_off[2], s_off[2], z_off[2], to[4];
-  int exponent[2], no_zeros;
+  static constexpr int EB = S32 ? 4 : 2, SW = kTableBlocks * EB / 4;  // words of a channel's scales in half of the table
+  uint32_t w_off[2], to[4], table, s_off, z_off;
+  uint32_t ts[SW], tz[2];  // channel t's scales and zero points on their way to the table
+  int exponent, no_zeros, cols, shift, blocks;
   const char *pw, *ps, *pz;  // the tile's first channel at the piece's first stage; of the scales and zero points, the first block
-  int extent, cols;
+  bool zeros;
 
-  __device__ __forceinline__ void lanes(const Int4Args& a, uint32_t ring, int tid) {
-    const int c = tid >> 1, h = tid & 1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) to[j] = ring + c * 128 + swz_wide(c, h * 4 + j) * 16;
-    no_zeros = a.zero ? 0 : 8;
-  }
   // cols: channels that exist (the last one again behind them)
-  __device__ __forceinline__ void tile(const Int4Args& a, const Piece& p, int tid) {
+  __device__ __forceinline__ void tile(const Int4Args& a, const Piece& p, uint32_t ring, int t) {
+    const int c = t >> 1, h = t & 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = ring + kWideB + c * 128 + swz_wide(c, h * 4 + j) * 16;
+    table = ring + kTable;
+    zeros = a.zero != nullptr;
+    no_zeros = zeros ? 0 : 8;
+    shift = a.shift;
+    blocks = a.blocks;
     cols = max(p.n_edge, 1);
     const int64_t ch = p.column;
     pw = (const char*)p.pb;
     ps = a.scale + (p.group * a.s_group + ch * a.s_row) * EB;
     pz = (const char*)a.zero + p.group * a.z_group + ch * a.z_row;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t c = min(i * 128 + (tid >> 1), cols - 1);
-      w_off[i] = c * (uint32_t)a.w_row + (tid & 1) * 16;
-      s_off[i] = c * (uint32_t)a.s_row * EB;
-      z_off[i] = a.zero ? c * (uint32_t)a.z_row : kOutOfBounds;
-    }
-    if (TY == kElemF16) {  // (two threads a channel)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t top = 0;
-        for (int j = tid & 1; j < a.blocks; j += 2)
-          top = max(top, __float_as_uint(elem_to_f32(ps + s_off[i] + (int64_t)j * EB, S32 ? kElemF32 : TY)) & 0x7fffffffu);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-        exponent[i] = int4_exponent(top);
-      }
+    for (int i = 0; i < 2; ++i) w_off[i] = (uint32_t)min(i * 128 + c, cols - 1) * (uint32_t)a.w_row + h * 16;
+    const uint32_t mine = min(t, cols - 1);
+    s_off = mine * (uint32_t)a.s_row * EB;
+    z_off = zeros ? mine * (uint32_t)a.z_row : kOutOfBounds;
+    exponent = 0;
+    if (TY == kElemF16) {
+      uint32_t top = 0;
+      for (int j = 0; j < blocks; ++j) top = max(top, __float_as_uint(elem_to_f32(ps + s_off + (int64_t)j * EB, S32 ? kElemF32 : TY)) & 0x7fffffffu);
+      exponent = int4_exponent(top);
     }
   }
-  // stage st of the piece
-  __device__ __forceinline__ void load(const Int4Args& a, const Piece& p, int st, Raw& r, int tid) const {
-    const int k0 = p.first + st * 64, left = min(a.K - k0, 64);
-    const __amdgpu_buffer_rsrc_t bw = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pw + st * 32), 0, (int)((cols - 1) * a.w_row + left / 2), 0x00020000);
-    const int block = min((k0 + (tid & 1) * 32) >> a.shift, a.blocks - 1);
-    const __amdgpu_buffer_rsrc_t bs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(ps), 0, (int)(kOutOfBounds - 1), 0x00020000);
-    const __amdgpu_buffer_rsrc_t bz = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pz), 0, (int)(kOutOfBounds - 1), 0x00020000);
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* p, int64_t extent) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, (int)extent, 0x00020000);
+  }
+  // the weights of stage st of the piece
+  __device__ __forceinline__ void load(const Int4Args& a, const Piece& p, int st, Raw& r) const {
+    const int left = min(a.K - p.first - st * 64, 64);
+    const __amdgpu_buffer_rsrc_t bw = buffer(pw + st * 32, (cols - 1) * a.w_row + left / 2);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const auto v = __builtin_amdgcn_raw_buffer_load_b128(bw, (int)w_off[i], 0, 0);
       __builtin_memcpy(r.q + 4 * i, &v, 16);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      r.s[i] = __uint_as_float(S32 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(bs, (int)(s_off[i] + block * EB), 0, 0)
-                                   : (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(bs, (int)(s_off[i] + block * EB), 0, 0));
-#pragma unroll
-    for (int i = 0; i < 2; ++i) r.z[i] = __uint_as_float((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(bz, (int)(z_off[i] + block), 0, 0));
   }
-  // scales and zero points from their bits: (q - z) s = q s + z, z = -z s
-  __device__ __forceinline__ void ready(Raw& r) const {
+  // blocks 8 m .. 8 m + 7 of channel t, the last one again behind it: as they lie in memory where all of them exist
+  __device__ __forceinline__ void load_table(int m) {
+    const __amdgpu_buffer_rsrc_t bs = buffer(ps, (int64_t)kOutOfBounds - 1), bz = buffer(pz, (int64_t)kOutOfBounds - 1);
+    const int b0 = m * kTableBlocks;
+    if (b0 + kTableBlocks <= blocks) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t bits = __float_as_uint(r.s[i]);
-      float s = r.s[i];
-      if (!S32 && TY == kElemBF16) s = __uint_as_float(bits << 16);
-      if (!S32 && TY == kElemF16) s = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-      if (TY == kElemF16) s = ldexpf(s, -exponent[i]);
-      r.s[i] = s;
-      r.z[i] = -(float)(__float_as_uint(r.z[i]) | no_zeros) * s;
+      for (int i = 0; i < SW; i += 4) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(bs, (int)(s_off + b0 * EB + 4 * i), 0, 0);
+        __builtin_memcpy(ts + i, &v, 16);
+      }
+      const auto v = __builtin_amdgcn_raw_buffer_load_b64(bz, (int)(z_off + b0), 0, 0);
+      __builtin_memcpy(tz, &v, 8);
+      return;
+    }
+    tz[0] = tz[1] = 0;
+#pragma unroll
+    for (int i = 0; i < kTableBlocks; ++i) {
+      const int b = min(b0 + i, blocks - 1);
+      if (S32) {
+        ts[i % SW] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(bs, (int)(s_off + b * EB), 0, 0);
+      } else {
+        const uint32_t v = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(bs, (int)(s_off + b * EB), 0, 0);
+        ts[i / 2 % SW] = i & 1 ? ts[i / 2 % SW] | v << 16 : v;
+      }
+      tz[i >> 2] |= (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(bz, (int)(z_off + b), 0, 0) << (8 * (i & 3));
     }
   }
-  // eight of a thread's weights, to the unit at `unit`
-  __device__ __forceinline__ void put(const Raw& r, int k, uint32_t unit) const {
-    const uint32_t lo = r.q[k] & 0x0f0f0f0fu, hi = r.q[k] >> 4 & 0x0f0f0f0fu;
-    const float s = r.s[k >> 2], z = r.z[k >> 2];
-    gi32x4 out;
+  // ... to the table's half, as s and -z s
+  __device__ __forceinline__ void put_table(int m, int t) const {
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-      out[d] = (int)pack2<TY>(fmaf((float)(lo >> (8 * d) & 0xff), s, z), fmaf((float)(hi >> (8 * d) & 0xff), s, z));
-    *(__attribute__((address_space(3))) gi32x4*)(uintptr_t)(to[k & 3] + unit + (k >> 2) * (128 * 128)) = out;
+    for (int i = 0; i < kTableBlocks; ++i) {
+      const uint32_t bits = S32 ? ts[i % SW] : ts[i / 2 % SW] >> (16 * (i & 1)) & 0xffff;
+      float s = S32 ? __uint_as_float(bits) : TY == kElemBF16 ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+      if (TY == kElemF16) s = ldexpf(s, -exponent);
+      typedef float f2 __attribute__((ext_vector_type(2)));
+      const f2 v = {s, -(float)((tz[i >> 2] >> (8 * (i & 3)) & 0xff) | no_zeros) * s};
+      *(__attribute__((address_space(3))) f2*)(uintptr_t)(table + (((m & 1) * kTableBlocks + i) * kGT + t) * 8) = v;
+    }
+  }
+  // the scales of stage st's weights, from the table
+  __device__ __forceinline__ void ready(const Piece& p, int st, Raw& r, int t) const {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const int block = min((p.first + st * 64 + (t & 1) * 32) >> shift, blocks - 1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f2 v = *(__attribute__((address_space(3))) const f2*)(uintptr_t)(table + ((block & (2 * kTableBlocks - 1)) * kGT + i * 128 + (t >> 1)) * 8);
+      r.s[i] = v[0];
+      r.zs[i] = v[1];
+    }
+  }
+  // Eight of a thread's weights, to the unit at `unit`, in eight slices: what is done between two matrix instructions must not take longer than one of them
+  // (whole at a time, 4096 rows of 4096 x 14336 took 640 us, with the matrix cores busy for 39 % of it).
+  struct Eight {
+    uint32_t lo, hi;
+    float u, v;
+    gi32x4 out;
+  };
+  __device__ __forceinline__ void slice(const Raw& r, Eight& e, int k, int i, uint32_t unit) const {
+    const float s = r.s[k >> 2], z = r.zs[k >> 2];
+    auto bytes = [&](int d) __attribute__((always_inline)) {
+      e.u = (float)(e.lo >> (8 * d) & 0xff);
+      e.v = (float)(e.hi >> (8 * d) & 0xff);
+    };
+    auto scaled = [&](int d) __attribute__((always_inline)) { e.out[d] = (int)pack2<TY>(fmaf(e.u, s, z), fmaf(e.v, s, z)); };
+    if (i == 0) {
+      e.lo = r.q[k] & 0x0f0f0f0fu;
+      e.hi = r.q[k] >> 4 & 0x0f0f0f0fu;
+      asm("" : "+v"(e.lo), "+v"(e.hi));  // (or the compiler would rather cut each number out by itself)
+    }
+    if (i == 1 || i == 4) bytes(i == 1 ? 0 : 2);
+    if (i == 2 || i == 5) scaled(i == 2 ? 0 : 2);
+    if (i == 3 || i == 6) {
+      bytes(i == 3 ? 1 : 3);
+      scaled(i == 3 ? 1 : 3);
+    }
+    if (i == 7) *(__attribute__((address_space(3))) gi32x4*)(uintptr_t)(to[k & 3] + unit + (k >> 2) * (128 * 128)) = e.out;
+  }
+  __device__ __forceinline__ void put(const Raw& r, int k, uint32_t unit) const {
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) slice(r, e, k, i, unit);
   }
 };
 
@@ -156,8 +215,6 @@ __device__ __forceinline__ void write_scaled(const GroupedArgs& g, const Piece& 
     }
 }
 
-constexpr uint32_t kWideB = 2 * kUnit;  // the widened weights' three units; x has the two before them
-
 template <int TY, int BM, bool S32, class Next>
 __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4Args& a, char* lds, Next&& piece) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -198,18 +255,31 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
     int t = tid;  // (an opaque copy: what follows from it is worked out for this tile, and not kept in registers across the others)
     asm volatile("" : "+v"(t));
     // (the weights' first loads wait for the last tile to be written: with them under way before that, its values do not fit the registers)
-    fb.lanes(a, ring + kWideB, t);
-    fb.tile(a, p, t);
-    if (n > 0) fb.load(a, p, 0, r0, t);
-    if (n > 1) fb.load(a, p, 1, cur, t);
-    if (n > 2) fb.load(a, p, 2, nxt, t);
+    fb.tile(a, p, ring, t);
+    if (n > 0) fb.load(a, p, 0, r0);
+    if (n > 1) fb.load(a, p, 1, cur);
+    if (n > 2) fb.load(a, p, 2, nxt);
+    // of eight blocks after eight, which half of the table the weights of the k-th value of the piece take
+    auto eights = [&](int k) { return (p.first + k) >> (a.shift + 3); };
+    if (i > 1) stage_barrier();  // (every wavefront has turned its values of the last tile around)
     if (n > 0) {
-      fb.ready(r0);
+      const int m = eights(0);
+      fb.load_table(m);
+      fb.put_table(m, t);
+      if ((m + 1) * kTableBlocks < a.blocks) {
+        fb.load_table(m + 1);
+        fb.put_table(m + 1, t);
+      }
+    }
+    stage_barrier();
+    int coming = -1;  // blocks that are on their way to the table
+    if (n > 0) {
+      fb.ready(p, 0, r0, t);
 #pragma unroll
       for (int k = 0; k < 8; ++k) fb.put(r0, k, 0);
     }
     if (n > 1) {
-      fb.ready(cur);
+      fb.ready(p, 1, cur, t);
       fb.put(cur, 0, kUnit);
       fb.put(cur, 1, kUnit);
     }
@@ -234,31 +304,38 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
         for (int k = 0; k < T::READS; ++k) tile.read_k(f0, k, 0, 0, 0);
       }
       uint32_t ua = 0, ub = 0;  // of stage st
-      auto turn3 = [](uint32_t u) { return u == 2 * kUnit ? 0 : u + kUnit; };
       // behind: stages behind this one, 3 for that many and more (each kind its own code: accumulators that come from two sides are copied)
       auto stage = [&](int st, auto behind) __attribute__((always_inline)) {
         constexpr int BEHIND = decltype(behind)::value;
-        const uint32_t na = ua ^ kUnit, nb = turn3(ub), nnb = turn3(nb);
-        auto widen = [&](int k) __attribute__((always_inline)) {
-          if (BEHIND >= 1) fb.put(cur, k, nb);
-        };
-        tile.template substep<2>(f0, f1, true, 1, ua, ub, [&](int q) { widen(2 + q); });
-        tile.template substep<2>(f1, f0, true, 2, ua, ub, [&](int q) { widen(4 + q); });
-        tile.template substep<2>(f0, f1, true, 3, ua, ub, [&](int q) { widen(6 + q); });
+        const uint32_t na = ua ^ kUnit, nb = ub ^ kUnit;  // of the next stage; the ones of the stage behind that take this one's places
+        // the q-th of 16 slices of the eights k and k + 1
+        typename Widen<TY, S32>::Eight e;
+        auto widen = [&](int k, int q, uint32_t unit) __attribute__((always_inline)) { fb.slice(cur, e, k + q / 8, q & 7, unit); };
+        tile.template substep<BEHIND >= 1 ? 16 : 0>(f0, f1, true, 1, ua, ub, [&](int q) { widen(2, q, nb); });
+        tile.template substep<BEHIND >= 1 ? 16 : 0>(f1, f0, true, 2, ua, ub, [&](int q) { widen(4, q, nb); });
+        tile.template substep<BEHIND >= 1 ? 16 : 0>(f0, f1, true, 3, ua, ub, [&](int q) { widen(6, q, nb); });
         if (BEHIND >= 1) {
           wait_loads<0>();
           stage_barrier();
         }
         if constexpr (BEHIND >= 2) {
           cur = nxt;
-          fb.ready(cur);
-          if (BEHIND >= 3) fb.load(a, p, st + 3, nxt, t);
+          fb.ready(p, st + 2, cur, t);
+          // A half of the table is free once the weights of the other one's first stage have been taken from it, and its new values, which are here at the
+          // next barrier, are read after the one behind that at the earliest: eight blocks are four stages at least.
+          if (coming >= 0) {
+            fb.put_table(coming, t);
+            coming = -1;
+          }
+          if (const int m = eights((st + 2) * 64); m != eights((st + 1) * 64) && (m + 1) * kTableBlocks < a.blocks) {
+            coming = m + 1;
+            fb.load_table(coming);
+          }
+          if (BEHIND >= 3) fb.load(a, p, st + 3, nxt);
           load_a(st + 3 == n);
-          tile.template substep<kLoads + 2>(f1, f0, true, 0, na, nb, [&](int q) {
-            if (q < kLoads)
-              one_a(q, ua);
-            else
-              fb.put(cur, q - kLoads, nnb);
+          tile.template substep<16>(f1, f0, true, 0, na, nb, [&](int q) {
+            if (q % 2 == 0) one_a(q / 2, ua);
+            widen(0, q, ub);
           });
         } else {
           tile.template substep<0>(f1, f0, BEHIND >= 1, 0, na, nb, [](int) {});
@@ -274,14 +351,11 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
       float* factor = (float*)(lds + kWideB);  // (the first unit: nobody reads it any more)
       stage_barrier();
       if (TY == kElemF16) {
-        if ((t & 1) == 0) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) factor[x * 128 + (t >> 1)] = ldexpf(1.f, fb.exponent[x]);
-        }
+        factor[t] = ldexpf(1.f, fb.exponent);
         stage_barrier();
       }
       if (more) first_loads(after);
-      char* turn = lds + kWideB + 2 * kUnit + w * (kUnit / 4);
+      char* turn = lds + kTable + w * (kUnit / 4);
       if constexpr (TY == kElemF16) {
         write_scaled<MI, NI>(g, p, tile.acc, factor, turn, wm, wn, w, lane);
         if (more) stage_barrier();  // (the factors are read)
