@@ -49,10 +49,15 @@ __device__ __forceinline__ float activation_exponent(int act, float a) {
   const float b = fminf(fmaxf(a, -100.f), 100.f);
   return kGeluSlope * (b + kGeluCube * b * b * b);
 }
-__device__ __forceinline__ float activation(int act, float a) { return a / (1.f + expf(-activation_exponent(act, a))); }
+// By the hardware's exp2 and reciprocal, a unit of the last place off each: with expf and a division a tile of 256 x 128 spent 6 of its 38 us here (8192 tokens
+// on 64 experts of 2048 x 1024, forward).  An argument of exp is off by |z| units of its last place either way.
+__device__ __forceinline__ float activation_sigmoid(int act, float a) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * activation_exponent(act, a)));
+}
+__device__ __forceinline__ float activation(int act, float a) { return a * activation_sigmoid(act, a); }
 // f(a) and f'(a) = s + a s (1 - s) z'(a)
 __device__ __forceinline__ void activation_slope(int act, float a, float& f, float& slope) {
-  const float s = 1.f / (1.f + expf(-activation_exponent(act, a)));
+  const float s = activation_sigmoid(act, a);
   const float b = fminf(fmaxf(a, -100.f), 100.f);
   const float z = act == DSMOE_SILU ? 1.f : kGeluSlope * (1.f + 3.f * kGeluCube * b * b);
   f = a * s;

@@ -220,11 +220,11 @@ __device__ __forceinline__ void stream_tile(const GroupedArgs& g, const char* pa
   }
 }
 
-// MODE: a gated pair deals its two weights out to the two halves of the wavefronts; a sum of two takes them one after the other.
+// MODE: a gated pair and a sum of two deal their two products out to the two halves of the wavefronts.
 template <int TY, int OUT, bool BX, int NR, int J, int W, bool ONCE, int MODE>
 __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, const char* pa, const char* pb, char* pc, const float* as,
                                             const float* bs, int64_t row0, int rows, int n0, int cols, int K) {
-  constexpr int WP = MODE == kGatedPair ? W / 2 : W;  // wavefronts of a product
+  constexpr int WP = MODE == kOneProduct ? W : W / 2;  // wavefronts of a product
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
   typedef typename SAcc<TY>::type acc_t;
   acc_t acc[NR][J];
@@ -232,9 +232,8 @@ __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, con
   for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[r][j] = acc_t{0, 0, 0, 0};
-  const int wv = __builtin_amdgcn_readfirstlane(wave), other = MODE == kGatedPair ? wv / WP : 0;
-  stream_tile<TY, BX, NR, J, WP, ONCE>(g, pa, other ? g.b2 + (pb - g.b) : pb, rows, n0, cols, K, wv - other * WP, acc);
-  if constexpr (MODE == kSumOfTwo) stream_tile<TY, BX, NR, J, WP, ONCE>(g, g.a2 + (pa - g.a), g.b2 + (pb - g.b), rows, n0, cols, K, wv, acc);
+  const int wv = __builtin_amdgcn_readfirstlane(wave), other = MODE == kOneProduct ? 0 : wv / WP;
+  stream_tile<TY, BX, NR, J, WP, ONCE>(g, MODE == kSumOfTwo && other ? g.a2 + (pa - g.a) : pa, other ? g.b2 + (pb - g.b) : pb, rows, n0, cols, K, wv - other * WP, acc);
   // A lane's sums: row lane % 16 of sixteen; along: columns 16 j + 4 q .. + 3 from acc[.][j]; across: columns J (4 q + v) + j from acc[.][j][v].
   typedef uint32_t word4 __attribute__((ext_vector_type(4)));
   constexpr int COLS = 16 * J, RF = row_floats(J);
@@ -270,7 +269,7 @@ __device__ __forceinline__ void stream_rows(const GroupedArgs& g, char* lds, con
       } else {
         out[p] = 0.f;
 #pragma unroll
-        for (int w = 0; w < WP; ++w) out[p] += __uint_as_float(at[w * (16 * RF)]);
+        for (int w = 0; w < (MODE == kGatedPair ? WP : W); ++w) out[p] += __uint_as_float(at[w * (16 * RF)]);
         if constexpr (MODE == kGatedPair) {
           float up = 0.f;
 #pragma unroll

@@ -168,24 +168,28 @@ struct Widen {
   }
 };
 
-// Half precision: sums times their channel's power of two.  factor: of the tile's channels, in LDS.
-template <int MI, int NI>
-__device__ __forceinline__ void write_scaled(const GroupedArgs& g, const Piece& p, const gf32x16 (&acc)[MI][NI], const float* factor, char* turn, int wm, int wn,
-                                             int w, int lane) {
+// Stores a tile's sums as write_tile does, in half precision times their channel's power of two.  factor: of the tile's channels, in LDS.  (The compiler would
+// rather fetch all 256 sums from the accumulation registers at once, which do not fit: the empty instructions hold each block back until it is its turn.)
+template <int TY, int MI, int NI>
+__device__ __forceinline__ void write_sums(const GroupedArgs& g, const Piece& p, gf32x16 (&acc)[MI][NI], const float* factor, char* turn, int wm, int wn, int w,
+                                           int lane) {
   const int r32 = lane & 31, half = lane >> 5;
-  if (p.partial != nullptr) {  // as write_tile
+  constexpr bool SCALED = TY == kElemF16;
+  if (p.partial != nullptr) {
     char* to = p.partial + w * (MI * NI * 4096) + lane * 16;
 #pragma unroll
     for (int a = 0; a < MI; ++a)
 #pragma unroll
-      for (int b = 0; b < NI; ++b)
+      for (int b = 0; b < NI; ++b) {
+        gf32x16& c = acc[a][b];
+        asm volatile("" : "+a"(c));
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const gf32x4 f = *(const gf32x4*)(factor + wn + b * 32 + 8 * q + 4 * half);
-          const gf32x16& c = acc[a][b];
-          *(gf32x4*)(to + ((a * NI + b) * 4 + q) * 1024) = gf32x4{c[4 * q] * f[0], c[4 * q + 1] * f[1], c[4 * q + 2] * f[2], c[4 * q + 3] * f[3]};
-          __builtin_amdgcn_sched_barrier(0);
+          gf32x4 v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+          if (SCALED) v *= *(const gf32x4*)(factor + wn + b * 32 + 8 * q + 4 * half);
+          *(gf32x4*)(to + ((a * NI + b) * 4 + q) * 1024) = v;
         }
+      }
     return;
   }
   constexpr int LPR = 16;  // 64 columns of 32 bits a row
@@ -194,21 +198,23 @@ __device__ __forceinline__ void write_scaled(const GroupedArgs& g, const Piece& 
 #pragma unroll
     for (int b0 = 0; b0 < NI; b0 += 2) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b) {
+        gf32x16& c = acc[a][b0 + b];
+        asm volatile("" : "+a"(c));
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const gf32x16& c = acc[a][b0 + b];
+        for (int q = 0; q < 4; ++q)
           *(gf32x4*)(turn + r32 * 256 + ((b * 8 + q * 2 + half) ^ (r32 & 15)) * 16) = gf32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-        }
+      }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
       const int ch = lane % LPR, c = wn + b0 * 32 + ch * 4;
-      const gf32x4 f = *(const gf32x4*)(factor + c);
+      gf32x4 f = {1, 1, 1, 1};
+      if (SCALED) f = *(const gf32x4*)(factor + c);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int rr = k * 4 + lane / LPR, r = wm + a * 32 + rr;
         const gf32x4 v = *(const gf32x4*)(turn + rr * 256 + (ch ^ (rr & 15)) * 16);
-        if (r < p.m_edge && c < p.n_edge) *(uint2*)(p.pc + r * g.c_row + (int64_t)c * 2) = make_uint2(pack2<kElemF16>(v[0] * f[0], v[1] * f[1]), pack2<kElemF16>(v[2] * f[2], v[3] * f[3]));
+        if (r < p.m_edge && c < p.n_edge) *(uint2*)(p.pc + r * g.c_row + (int64_t)c * 2) = make_uint2(pack2<TY>(v[0] * f[0], v[1] * f[1]), pack2<TY>(v[2] * f[2], v[3] * f[3]));
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -299,10 +305,8 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
 #pragma unroll
           for (int v = 0; v < 16; ++v) tile.acc[x][y][v] = 0;
       typename T::Frags f0, f1;
-      if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < T::READS; ++k) tile.read_k(f0, k, 0, 0, 0);
-      }
+      for (int k = 0; k < T::READS; ++k) tile.read_k(f0, k, 0, 0, 0);
       uint32_t ua = 0, ub = 0;  // of stage st
       // behind: stages behind this one, 3 for that many and more (each kind its own code: accumulators that come from two sides are copied)
       auto stage = [&](int st, auto behind) __attribute__((always_inline)) {
@@ -347,7 +351,7 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
       for (; st + 3 < n; ++st) stage(st, Const<3>());
       for (; st + 2 < n; ++st) stage(st, Const<2>());
       for (; st + 1 < n; ++st) stage(st, Const<1>());
-      for (; st < n; ++st) stage(st, Const<0>());
+      stage(st, Const<0>());
       float* factor = (float*)(lds + kWideB);  // (the first unit: nobody reads it any more)
       stage_barrier();
       if (TY == kElemF16) {
@@ -356,13 +360,14 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
       }
       if (more) first_loads(after);
       char* turn = lds + kTable + w * (kUnit / 4);
-      if constexpr (TY == kElemF16) {
-        write_scaled<MI, NI>(g, p, tile.acc, factor, turn, wm, wn, w, lane);
-        if (more) stage_barrier();  // (the factors are read)
-      } else {
-        write_tile<TY, TY, kOneProduct, MI, NI>(g, p, tile.acc, Factors<false, MI, NI>(), turn, wm, wn, w, lane, false);
-      }
+      write_sums<TY, MI, NI>(g, p, tile.acc, factor, turn, wm, wn, w, lane);
+      if (TY == kElemF16 && more) stage_barrier();  // (the factors are read)
     };
+    if (n == 0) {  // (the second half of a narrow tile's columns)
+      if (more) first_loads(after);
+      p = after;
+      continue;
+    }
     int mi, ni, wm, wn;
     tile_shape(p.m_edge, p.n_edge, false, false, w, mi, ni, wm, wn);
     bool done = false;
