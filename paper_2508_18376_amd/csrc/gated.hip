@@ -98,12 +98,14 @@ GroupedArgs dx_args(const GatedArgs& a) {
   g.partial = a.workspace + 2 * slope_bytes(a);
   return g;
 }
-GroupedArgs dw_args(const GatedArgs& a, bool second) {
+GroupedArgs dw_args(const GatedArgs& a) {
   const int64_t e = elem_bytes(a.type);
   GroupedArgs g = base(a);
   g.a = (const char*)a.x;
-  g.b = a.workspace + (second ? slope_bytes(a) : 0);
-  g.c = (char*)(second ? a.dw3 : a.dw1);
+  g.b = a.workspace;
+  g.b2 = a.workspace + slope_bytes(a);
+  g.c = (char*)a.dw1;
+  g.c2 = (char*)a.dw3;
   g.a_row = a.x_row * e;
   g.b_row = slope_row(a) * e;
   g.c_row = a.N * e;
@@ -118,7 +120,7 @@ GroupedArgs dw_args(const GatedArgs& a, bool second) {
 
 size_t gated_workspace_bytes(const GatedArgs& a) { return gated_pair_bytes(forward_args(a), a.type); }
 size_t gated_backward_workspace_bytes(const GatedArgs& a) {
-  const size_t dx = sum_of_two_bytes(dx_args(a), a.type), dw = grouped_dw_workspace_bytes(dw_args(a, false), a.type);
+  const size_t dx = sum_of_two_bytes(dx_args(a), a.type), dw = grouped_dw_workspace_bytes(dw_args(a), a.type);
   return (size_t)(2 * slope_bytes(a)) + (dx > dw ? dx : dw);
 }
 
@@ -133,9 +135,7 @@ hipError_t launch_gated_backward(const GatedArgs& a, hipStream_t s) {
                                : slopes<DSMOE_F16>(a, da, db, slope_row(a), s);
     if (e == hipSuccess) e = launch_sum_of_two(dx_args(a), a.type, s);
   }
-  if (e == hipSuccess) e = launch_grouped_dw(dw_args(a, false), a.type, s);
-  if (e == hipSuccess) e = launch_grouped_dw(dw_args(a, true), a.type, s);
-  return e;
+  return e == hipSuccess ? launch_grouped_dw(dw_args(a), a.type, s) : e;
 }
 
 }  // namespace dsmoe

@@ -16,13 +16,16 @@ bool tiles_fit(const GroupedArgs& g, int type) {
          rows_fit(g.c, g.c_row, g.N * 2ll) && ((uintptr_t)g.sums & 15) == 0;
 }
 
+// As for the single product (grouped_stream.hip), but that the weights are two.  Streams against tiles, rows on 16 bytes, as many rows in each group: 1 / 12 / 32
+// rows on 64 experts of 2048 x 1024 100 / 102 / 109 us against 106 / 106 / 108, on 8 of 4096 x 14336 307 / 314 / 341 against 344 / 344 / 348, on 64 of
+// 2048 x 1408 107 / 109 / 122 against 127 / 129 / 132; 1 / 32 rows of 2048 x 1024 in one group 11 / 18 against 23 / 23.
 bool stream_sizes(const GroupedArgs& g, int type, bool fit) {
   if (!launch_holds(g, type, false, fit)) return false;
   const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 63) / 64);
   if (type == kElemF32) return g.R <= 64 * (int64_t)g.G || tiles < 320;
   if (!fit) return g.R <= 16 * (int64_t)g.G || tiles < 64;
   const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
-  return g.R <= 12 * (int64_t)g.G && ((int64_t)g.K * 2 <= 16384 || pieces >= 128);
+  return g.R <= 24 * (int64_t)g.G && ((int64_t)g.K * 2 <= 16384 || pieces >= 128);
 }
 
 template <int TY>

@@ -15,12 +15,16 @@ bool tiles_fit(const GroupedArgs& g, int type) {
          (g.b_group & 15) == 0 && rows_fit(g.c, g.c_row, g.N * 2ll);
 }
 
+// Streams against tiles, the whole backward pass, as many rows in each group: 1 / 12 / 24 rows on 64 experts of 2048 x 1024 275 / 280 / 285 us against 282 / 288 /
+// 289, on 8 of 4096 x 14336 777 / 824 / 867 against 818 / 831 / 831, on 8 of 14336 x 4096 726 / 778 / 821 against 814 / 837 / 848; long sums in few
+// pieces keep too few compute units busy: 1 / 12 rows of 4096 x 14336 in one group 193 / 209 against 163 / 164.
 bool stream_sizes(const GroupedArgs& g, int type, bool fit) {
   if (!launch_holds(g, type, true, fit)) return false;
   const int64_t tiles = row_tiles_bound(g.R, g.G, g.off != nullptr, 128) * ((g.N + 127) / 128);
   if (type == kElemF32) return g.R <= 48 * (int64_t)g.G || tiles < 320;
   if (!fit) return g.R <= 8 * (int64_t)g.G && tiles < 256;
-  return g.R <= 2 * (int64_t)g.G && (int64_t)g.K * 2 <= 16384;
+  const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
+  return g.R <= 12 * (int64_t)g.G && ((int64_t)g.K * 2 <= 16384 || pieces >= 256);
 }
 
 template <int TY>

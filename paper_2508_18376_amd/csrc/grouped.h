@@ -35,6 +35,7 @@ struct GroupedArgs {
   int64_t bs_group;  // ... in values
   int32_t out_type;
   const char *a2, *b2;  // kSumOfTwo, kGatedPair: the second operands, strides as the first ones'
+  char* c2;             // over weights, plain path: where A_g^T B2_g goes too, or nullptr
   float* sums;          // kGatedPair: where both products go as they are, [2][R][N], or nullptr
   int32_t act;          // kGatedPair: the activation f
   char* partial;  // workspace for tiles whose contraction is split (grouped_workspace_bytes), or nullptr
@@ -232,7 +233,16 @@ inline size_t grouped_workspace_bytes(const GroupedArgs& g, int type, bool b_alo
   return type == kElemF32 || g.R == 0 || grouped_stream_sizes(g, type, b_along, true) ? 0 : grouped_split_bytes(g, type);
 }
 inline size_t grouped_dw_workspace_bytes(const GroupedArgs& g, int type) { return type == kElemF32 ? 0 : grouped_dw_split_bytes(g); }
+// g.b2 and g.c2: a second product with the same left operand.  (Tiles: a launch for each; in one, long ones would end no better.)
 inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t s) {
+  if (g.c2 != nullptr && grouped_dw_mfma_fits(g, type)) {
+    GroupedArgs one = g, two = g;
+    one.c2 = two.c2 = nullptr;
+    two.b = g.b2;
+    two.c = g.c2;
+    const hipError_t e = launch_grouped_dw_mfma(one, type, s);
+    return e != hipSuccess ? e : launch_grouped_dw_mfma(two, type, s);
+  }
   return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
 }
 

@@ -188,6 +188,8 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
   if (DW) {
     const int MT = (g.M + kPT - 1) / kPT;
     piece = blockIdx.x;
+    const bool second = g.c2 != nullptr && piece >= g.G * MT * NT;
+    if (second) piece -= g.G * MT * NT;
     const int grp = piece / (MT * NT), id = piece - grp * MT * NT;
     int mt, nt, row0;
     band_tile(id, MT, NT, mt, nt);
@@ -198,8 +200,8 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
     n0 = last_tile(nt, g.N);
     m_edge = min(kPT, g.M - m0);
     pa = g.a + (int64_t)row0 * g.a_row + (int64_t)m0 * E::bytes;
-    pb = g.b + (int64_t)row0 * g.b_row + (int64_t)n0 * E::bytes;
-    pc = g.c + grp * g.c_group;
+    pb = (second ? g.b2 : g.b) + (int64_t)row0 * g.b_row + (int64_t)n0 * E::bytes;
+    pc = (second ? g.c2 : g.c) + grp * g.c_group;
   } else {
     Segment s;
     Segments all;

@@ -14,7 +14,7 @@ hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hi
 }
 
 hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s) {
-  const int64_t blocks = (int64_t)g.G * ((g.M + kPT - 1) / kPT) * ((g.N + kPT - 1) / kPT);
+  const int64_t blocks = (int64_t)g.G * ((g.M + kPT - 1) / kPT) * ((g.N + kPT - 1) / kPT) * (g.c2 != nullptr ? 2 : 1);
   switch (type) {
     case kElemF32: return launch<kElemF32, true, true>(g, blocks, s);
     case kElemBF16: return launch<kElemBF16, true, true>(g, blocks, s);

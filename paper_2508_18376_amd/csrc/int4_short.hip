@@ -15,14 +15,14 @@ namespace dsmoe {
 namespace {
 
 constexpr int kCols = 256, kStage = 128, kWeights = kCols * kStage / 2;
-constexpr int kRoom = 80 * 1024;  // of a workgroup in LDS: two to a compute unit
 constexpr uint32_t kBeyond = 0x80000000u;
 
 template <int SPAN, int NR>
 struct Shape {
   static constexpr int SPANS = kStage / SPAN, WORDS = SPAN / 32, ROWS = 16 * NR;
   static constexpr int x_at = kWeights, s_at = x_at + ROWS * kStage * 2, bytes = s_at + SPANS * 2 * kCols * 4;
-  static constexpr int ring = kRoom / bytes < 4 ? kRoom / bytes : 4;  // stages
+  static constexpr int room = 160 * 1024 / (NR == 1 ? 3 : 2);              // of a workgroup in LDS: three (two) to a compute unit
+  static constexpr int ring = room / bytes < 2 ? 2 : room / bytes < 4 ? room / bytes : 4;  // stages
   static constexpr int loads = 4 + NR + 2 * SPANS;                    // of a wavefront and stage
 };
 
@@ -70,7 +70,7 @@ __device__ __forceinline__ bool place_of(const Int4Args& a, const Segments& all,
 }
 
 template <int TY, int SPAN, int NR, bool S32>
-__global__ __launch_bounds__(256, 2) void int4_short_kernel(Int4Args a) {
+__global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Args a) {
   extern __shared__ __align__(16) char ring[];
   typedef Shape<SPAN, NR> Sh;
   constexpr int J = 4, EB = S32 ? 4 : 2, RING = Sh::ring;

@@ -39,7 +39,7 @@ class _Int4Args(ctypes.Structure):
                                                  "zero_group_stride", "zero_row_stride")])
 
 
-class _Grad(ctypes.Structure):
+class _Grad(ctypes.Structure):  # (seven words of 64 bits, as which the binding fills them in)
     _fields_ = ([(n, ctypes.c_void_p) for n in ("grad", "out")] + [(n, ctypes.c_int64) for n in ("rows", "width", "grad_stride", "out_stride")]
                 + [(n, ctypes.c_int32) for n in ("dtype", "pad")])
 
@@ -63,8 +63,8 @@ def _declare(L):
     L.dsmoe_gated_workspace_bytes.argtypes = L.dsmoe_gated_backward_workspace_bytes.argtypes = [gated]
     L.moe_gated_matmul.argtypes = [gated] + [vp] * 8
     L.moe_gated_matmul_backward.argtypes = [gated] + [vp] * 11
-    L.moe_grad_norm.argtypes = [ctypes.POINTER(_Grad), i32, vp, vp, vp]
-    L.moe_clip_grads.argtypes = [ctypes.POINTER(_Grad), i32, ctypes.c_float, ctypes.c_float, vp, vp, vp]
+    L.moe_grad_norm.argtypes = [vp, i32, vp, vp, vp]
+    L.moe_clip_grads.argtypes = [vp, i32, ctypes.c_float, ctypes.c_float, vp, vp, vp]
     L.dsmoe_clip_workspace_bytes.argtypes = []
     L.dsmoe_int4_workspace_bytes.argtypes = [ctypes.POINTER(_Int4Args)]
     L.moe_int4_matmul.argtypes = [ctypes.POINTER(_Int4Args)] + [vp] * 8
@@ -77,6 +77,7 @@ def _declare(L):
 
 
 _declare(_lib)
+_CLIP_WORDS = _lib.dsmoe_clip_workspace_bytes() // 4
 
 
 def _refuse(where: str, what: str) -> None:
@@ -602,8 +603,8 @@ def moe_block_norm_backward(dy, dh, x, stats, *, branch, branch_weight, weight, 
 
 def _rows_of(f, name, t, out):
     """(rows, width, stride, stride of out): what the library takes a tensor as, and another one that is written value for value."""
-    if t.is_contiguous() and out.is_contiguous():
-        return 1, t.numel(), 0, 0
+    if t.numel() == 0:
+        return 1, 0, 0, 0
     dims = sorted(((s, o, n) for n, s, o in zip(t.shape, t.stride(), out.stride()) if n > 1), reverse=True)
     merged = []
     for s, o, n in dims:  # (s, o: strides; an outer dimension that goes on where the inner one ends is one with it)
@@ -632,23 +633,23 @@ def _grads(f, grads, out):
     if out is not grads:
         if not isinstance(out, (list, tuple)) or len(out) != len(grads):
             _refuse(f, "out must be a list of as many tensors as grads")
-    array = (_Grad * len(grads))()
-    device, elsewhere = grads[0].get_device(), False
-    for i, (e, t, o) in enumerate(zip(array, grads, out)):
+    device, elsewhere, fields = grads[0].get_device(), False, []
+    recorded = _grad_enabled() or _forward_mode._current_level >= 0
+    for i, (t, o) in enumerate(zip(grads, out)):
         dtype = _DTYPES.get(t.dtype)
         if dtype is None:
             _refuse(f, "gradients must be bfloat16, float16 or float32")
         if o is not t and (o.shape != t.shape or o.dtype is not t.dtype):
             _refuse(f, "out[%d] must have its gradient's shape and type" % i)
-        if _grad_enabled() and (t.requires_grad or o.requires_grad) or _forward_mode._current_level >= 0:
+        if recorded and (t.requires_grad or o.requires_grad or _forward_mode._current_level >= 0):
             _check_unrecorded(f, t, o)
-        e.rows, e.width, e.grad_stride, e.out_stride = _rows_of(f, "grads[%d]" % i, t, o)
-        if t.get_device() != device or o.get_device() != device:
+        rows, width, row, out_row = (1, t.numel(), 0, 0) if t.is_contiguous() and o.is_contiguous() else _rows_of(f, "grads[%d]" % i, t, o)
+        if t.get_device() != device or o is not t and o.get_device() != device:
             elsewhere = True
-        e.grad, e.out, e.dtype = t.data_ptr(), o.data_ptr(), dtype
+        fields += (t.data_ptr(), o.data_ptr(), rows, width, row, out_row, dtype)  # (dtype and pad: one of the seven words)
     if device < 0 or elsewhere:
         _not_one_gpu(f)
-    return array, device
+    return (ctypes.c_int64 * len(fields))(*fields), device
 
 
 def moe_grad_norm(grads, stream=None):
@@ -660,8 +661,8 @@ def moe_grad_norm(grads, stream=None):
     if stream is not None or device != _current_device():
         with _entered(f, device, stream):
             return moe_grad_norm(grads)
-    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
-    workspace = torch.empty(_lib.dsmoe_clip_workspace_bytes(), dtype=torch.uint8, device=norm.device)
+    norm = grads[0].new_empty((), dtype=torch.float32)
+    workspace = norm.new_empty(_CLIP_WORDS)
     rc = _lib.moe_grad_norm(array, len(grads), norm.data_ptr(), workspace.data_ptr(), _raw_stream(device))
     if rc:
         _failed(rc, f)
@@ -691,8 +692,8 @@ def moe_clip_grads(grads, max_norm, eps=1e-6, out=None, stream=None):
     if given is None:
         out = [torch.empty_like(t) for t in grads]
         array, _ = _grads(f, grads, out)
-    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
-    workspace = torch.empty(_lib.dsmoe_clip_workspace_bytes(), dtype=torch.uint8, device=norm.device)
+    norm = grads[0].new_empty((), dtype=torch.float32)
+    workspace = norm.new_empty(_CLIP_WORDS)
     rc = _lib.moe_clip_grads(array, len(grads), max_norm, eps, norm.data_ptr(), workspace.data_ptr(), _raw_stream(device))
     if rc:
         _failed(rc, f)
