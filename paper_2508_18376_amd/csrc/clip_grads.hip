@@ -15,6 +15,7 @@ namespace dsmoe {
 namespace {
 
 constexpr int kThreads = 256, kMost = 48;
+constexpr int64_t kLastLevelBytes = 256ll << 20;
 
 struct Entry {
   const char* in;
@@ -31,15 +32,19 @@ struct Entries {
 };
 static_assert(sizeof(Entries) + 64 <= 4096, "a launch takes 4 KiB of arguments");
 
+typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
+
 template <int TY>
 struct Vec {
   static constexpr int N = 16 / RowElem<TY>::bytes;
   float v[N];
   // n values exist
+  template <bool ONCE>
   __device__ __forceinline__ void load(const char* p, int n) {
     if (n >= N) {
+      const words_t x = ONCE ? __builtin_nontemporal_load((const words_t*)p) : *(const words_t*)p;
       uint32_t w[4];
-      __builtin_memcpy(w, p, 16);
+      __builtin_memcpy(w, &x, 16);
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = TY == DSMOE_F32 ? __uint_as_float(w[i * 4 / N]) : widen<TY>((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
     } else {
@@ -47,6 +52,7 @@ struct Vec {
       for (int i = 0; i < N; ++i) v[i] = i < n ? load1<TY>(p, i) : 0.f;
     }
   }
+  template <bool ONCE>
   __device__ __forceinline__ void store(char* p, int n) const {
     if (n >= N) {
       uint32_t w[4] = {0, 0, 0, 0};
@@ -57,7 +63,12 @@ struct Vec {
         else
           w[i >> 1] |= (uint32_t)narrow<TY>(v[i]) << (16 * (i & 1));
       }
-      __builtin_memcpy(p, w, 16);
+      words_t x;
+      __builtin_memcpy(&x, w, 16);
+      if (ONCE)
+        __builtin_nontemporal_store(x, (words_t*)p);
+      else
+        *(words_t*)p = x;
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -121,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(Entries t, double* 
       constexpr int TY = decltype(ty)::value;
       chunk_vectors<TY>(e, c, t.per_chunk, [&](const char* in, char*, int n) {
         Vec<TY> v;
-        v.load(in, n);
+        v.template load<false>(in, n);
 #pragma unroll
         for (int i = 0; i < Vec<TY>::N; ++i) sum = fma((double)v.v[i], (double)v.v[i], sum);
       });
@@ -149,7 +160,9 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double* sums, int 
   if (threadIdx.x == 0) *norm = v;
 }
 
-// Chunks are taken from the last one on: what the first pass read last is in the last-level cache still.
+// Chunks are taken from the last one on: what the first pass read last is in the last-level cache still.  ONCE: gradients that do not fit that cache are
+// loaded and stored past it (1.4 G values in bf16: both passes 1580 -> 1486 us; 5.9 TB/s in the first, 5.6 in the second).
+template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void clip_kernel(Entries t, const double* sums, int n, float max_norm, float eps, float* norm) {
   const float length = norm_of(sums, n), ratio = max_norm / (length + eps), factor = ratio >= 1.f ? 1.f : ratio;
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = length;
@@ -160,10 +173,10 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Entries t, const double*
       constexpr int TY = decltype(ty)::value;
       chunk_vectors<TY>(e, c, t.per_chunk, [&](const char* in, char* out, int k) {
         Vec<TY> v;
-        v.load(in, k);
+        v.template load<ONCE>(in, k);
 #pragma unroll
         for (int i = 0; i < Vec<TY>::N; ++i) v.v[i] *= factor;
-        v.store(out, k);
+        v.template store<ONCE>(out, k);
       });
     };
     if (e.type == DSMOE_F32)
@@ -229,7 +242,10 @@ hipError_t launch_clip_grads(const dsmoe_grad* grads, int count, bool clip, floa
   }
   for (int from = 0, to; from < count && e == hipSuccess; from = to) {
     fill(t, from, to);
-    clip_kernel<<<dim3(blocks), dim3(kThreads), 0, s>>>(t, sums, blocks, max_norm, eps, norm);
+    if (all * 16 > kLastLevelBytes)
+      clip_kernel<true><<<dim3(blocks), dim3(kThreads), 0, s>>>(t, sums, blocks, max_norm, eps, norm);
+    else
+      clip_kernel<false><<<dim3(blocks), dim3(kThreads), 0, s>>>(t, sums, blocks, max_norm, eps, norm);
     e = hipGetLastError();
   }
   return e;

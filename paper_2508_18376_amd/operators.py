@@ -683,8 +683,10 @@ def moe_clip_grads(grads, max_norm, eps=1e-6, out=None, stream=None):
             _refuse(f, "grads must be a list of tensors, of at least one")
         out = []  # filled below, on the stream that the call runs on
     else:
-        if isinstance(out, (list, tuple)) and len({t.data_ptr() for t in out if t.numel()}) != sum(1 for t in out if t.numel()):
-            _refuse(f, "out must not hold a tensor twice")
+        if isinstance(out, (list, tuple)) and len({t.data_ptr() for t in out}) != len(out):
+            places = [t.data_ptr() for t in out if t.numel()]  # (empty tensors lie nowhere)
+            if len(set(places)) != len(places):
+                _refuse(f, "out must not hold a tensor twice")
     array, device = _grads(f, grads, grads if given is None else out)
     if stream is not None or device != _current_device():
         with _entered(f, device, stream):
