@@ -2,13 +2,14 @@
 
     h       = norm in front of the block                                     (the second output of the last block's moe_block_norm)
     rows    = every token once for each of its Top-K experts, sorted by expert (moe_route_and_mask picks them)
-    branch  = sum over a token's experts of  g * (Swish(rows W1) * (rows W3)) W2            moe_grouped_matmul, three products
+    branch  = sum over a token's experts of  g * (Swish(rows W1) * (rows W3)) W2            moe_gated_matmul, moe_grouped_matmul
     y, h'   = x + scale * gate * norm(branch), norm(y)                                       moe_block_norm
 
-and the gradients of all of it: moe_block_norm_backward, moe_grouped_matmul with the weights transposed, moe_grouped_matmul_dw.  The elementwise steps
-in between are torch's.  `quantize` brings the trained weights to 8 bits, and `serve` runs the block with moe_int8_matmul.
+and the gradients of all of it: moe_block_norm_backward, moe_grouped_matmul with the weights transposed, moe_grouped_matmul_dw, moe_gated_matmul_backward,
+clipped by their norm (moe_clip_grads).  The elementwise steps in between are torch's.  `quantize` brings the trained weights to 8 bits or 4, and
+`serve` runs the block with moe_int8_matmul or moe_int4_matmul.
 
-    python examples/expert_block.py        # trains a small block for a few steps on the GPU, then compares it with its 8-bit form
+    python examples/expert_block.py        # trains a small block for a few steps on the GPU, then compares it with its 8-bit and 4-bit forms
 """
 import os
 import sys
@@ -17,8 +18,8 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2508_18376_amd import (DualSparseLayer, moe_block_norm, moe_block_norm_backward, moe_grouped_matmul, moe_grouped_matmul_dw,  # noqa: E402
-                                  moe_int8_matmul)
+from paper_2508_18376_amd import (DualSparseLayer, moe_block_norm, moe_block_norm_backward, moe_clip_grads, moe_gated_matmul,  # noqa: E402
+                                  moe_gated_matmul_backward, moe_grouped_matmul, moe_grouped_matmul_dw, moe_int4_matmul, moe_int8_matmul)
 
 
 class ExpertBlock:
@@ -49,39 +50,32 @@ class ExpertBlock:
         place[order] = torch.arange(order.shape[0], device="cuda")
         return order // self.K, offsets, w.flatten()[order], place.view(-1, self.K)
 
-    def experts(self, h, plan, products):
-        """branch [tokens][D] and what the backward pass takes; products: the three products, on grouped rows."""
-        token, offsets, w, place = plan
-        rows = h[token]
-        a, b = products("w1", rows, offsets), products("w3", rows, offsets)
-        act = (torch.nn.functional.silu(a.float()) * b.float()).to(h.dtype)
-        out = products("w2", act, offsets)
-        branch = (out.float() * w[:, None])[place].sum(1).to(h.dtype)
-        return branch, (rows, a, b, act)
+    def combine(self, out, plan, dtype):
+        """branch [tokens][D]: each token's rows of the experts' outputs, weighted."""
+        _, _, w, place = plan
+        return (out.float() * w[:, None])[place].sum(1).to(dtype)
 
     def norms(self, branch, gate):
         return dict(branch=branch, branch_weight=self.weights["branch_weight"], weight=self.weights["weight"], gate=gate, scale=self.scale)
 
     def forward(self, x, h, gate, plan):
-        branch, kept = self.experts(h, plan, lambda name, rows, offsets: moe_grouped_matmul(rows, self.weights[name], offsets))
+        token, offsets, _, _ = plan
+        rows = h[token]
+        act, both = moe_gated_matmul(rows, self.weights["w1"], self.weights["w3"], offsets, want_saved=True)
+        branch = self.combine(moe_grouped_matmul(act, self.weights["w2"], offsets), plan, h.dtype)
         y, h_next, stats = moe_block_norm(x, want_stats=True, **self.norms(branch, gate))
-        return y, h_next, (branch, stats) + kept
+        return y, h_next, (branch, stats, rows, act, both)
 
     def backward(self, dy, dh_next, x, gate, plan, saved):
         """Gradients of the weights, of x (through the residual connection), of h and of the gate.  Routing is taken as given."""
         token, offsets, w, place = plan
-        branch, stats, rows, a, b, act = saved
+        branch, stats, rows, act, both = saved
         g = moe_block_norm_backward(dy, dh_next, x, stats, **self.norms(branch, gate))
         dout = (g["dbranch"][token].float() * w[:, None]).to(x.dtype)
-        grads = {"branch_weight": g["dbranch_weight"], "weight": g["dweight"], "w2": moe_grouped_matmul_dw(act, dout, offsets)}
-        dact = moe_grouped_matmul(dout, self.weights["w2"], offsets, w_transposed=True).float()
-        s = torch.sigmoid(a.float())
-        da = (dact * b.float() * s * (1 + a.float() * (1 - s))).to(x.dtype)
-        db = (dact * a.float() * s).to(x.dtype)
-        grads["w1"], grads["w3"] = moe_grouped_matmul_dw(rows, da, offsets), moe_grouped_matmul_dw(rows, db, offsets)
-        drows = (moe_grouped_matmul(da, self.weights["w1"], offsets, w_transposed=True).float()
-                 + moe_grouped_matmul(db, self.weights["w3"], offsets, w_transposed=True).float())
-        return grads, g["dx"], drows[place].sum(1).to(x.dtype), g.get("dgate")
+        dact = moe_grouped_matmul(dout, self.weights["w2"], offsets, w_transposed=True)
+        half = moe_gated_matmul_backward(dact, rows, self.weights["w1"], self.weights["w3"], both, offsets)
+        grads = {"branch_weight": g["dbranch_weight"], "weight": g["dweight"], "w2": moe_grouped_matmul_dw(act, dout, offsets), "w1": half["dw1"], "w3": half["dw3"]}
+        return grads, g["dx"], half["dx"].float()[place].sum(1).to(x.dtype), g.get("dgate")
 
     def quantize(self):
         """8-bit weights [E][out][in] with a scale for each output channel, rows padded to 16 bytes."""
@@ -93,9 +87,29 @@ class ExpertBlock:
             padded[:, :, :w.shape[2]] = torch.round(w / scale[:, :, None]).to(torch.int8)
             self.int8[name] = padded[:, :, :w.shape[2]], scale
 
-    def serve(self, x, h, gate, plan):
-        branch, _ = self.experts(h, plan, lambda name, rows, offsets: moe_int8_matmul(rows, *self.int8[name], offsets))
-        return moe_block_norm(x, **self.norms(branch, gate))
+    def quantize4(self, block=64):
+        """4-bit weights [E][out][in / 2] with a scale and a zero point for each block of an output channel's weights."""
+        self.int4, self.block = {}, block
+        for name in ("w1", "w3", "w2"):
+            w = self.weights[name].float().transpose(1, 2)
+            parts = torch.nn.functional.pad(w, (0, -w.shape[2] % block)).unflatten(2, (-1, block))
+            low, high = parts.amin(3).clamp_max(0), parts.amax(3).clamp_min(0)
+            scale = ((high - low) / 15).clamp_min(1e-30)
+            zero = torch.round(-low / scale)
+            q = (torch.round(parts / scale[..., None]) + zero[..., None]).clamp(0, 15).flatten(2).to(torch.uint8)
+            self.int4[name] = (q[:, :, 0::2] | q[:, :, 1::2] << 4)[:, :, :(w.shape[2] + 1) // 2].contiguous(), scale.contiguous(), zero.to(torch.uint8).contiguous()
+
+    def serve(self, x, h, gate, plan, bits=8):
+        token, offsets, _, _ = plan
+
+        def product(name, rows):
+            if bits == 4:
+                return moe_int4_matmul(rows, *self.int4[name], offsets, block=self.block)
+            return moe_int8_matmul(rows, *self.int8[name], offsets)
+
+        rows = h[token]
+        act = (torch.nn.functional.silu(product("w1", rows).float()) * product("w3", rows).float()).to(h.dtype)
+        return moe_block_norm(x, **self.norms(self.combine(product("w2", act), plan, h.dtype), gate))
 
 
 def main(steps=20, tokens=512, D=256, F=512, E=8, K=2):
@@ -113,13 +127,14 @@ def main(steps=20, tokens=512, D=256, F=512, E=8, K=2):
         losses.append(float((err ** 2).mean()))
         dh = (2 * err / err.numel()).to(x.dtype)
         grads, _, _, _ = block.backward(torch.zeros_like(x), dh, x, gate, plan, saved)
+        grads = dict(zip(grads, moe_clip_grads(list(grads.values()), max_norm=1.0)[0]))
         for name, g in grads.items():
             block.weights[name] -= (40.0 * g.float()).to(x.dtype)
     block.quantize()
-    y8, h8 = block.serve(x, h, gate, plan)
+    block.quantize4()
     y, h_next, _ = block.forward(x, h, gate, plan)
-    rel = float((h8.float() - h_next.float()).norm() / h_next.float().norm())
-    print("loss %.4f -> %.4f over %d steps; 8-bit block differs by %.4f of the output" % (losses[0], losses[-1], steps, rel))
+    rel, rel4 = (float((block.serve(x, h, gate, plan, bits)[1].float() - h_next.float()).norm() / h_next.float().norm()) for bits in (8, 4))
+    print("loss %.4f -> %.4f over %d steps; the 8-bit block differs by %.4f of the output, the 4-bit one by %.4f" % (losses[0], losses[-1], steps, rel, rel4))
     return losses, rel
 
 

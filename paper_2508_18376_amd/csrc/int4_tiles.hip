@@ -331,7 +331,8 @@ __device__ __forceinline__ void do_int4_pieces(const GroupedArgs& g, const Int4A
             fb.put_table(coming, t);
             coming = -1;
           }
-          if (const int m = eights((st + 2) * 64); m != eights((st + 1) * 64) && (m + 1) * kTableBlocks < a.blocks) {
+          // (The weights of a part's first two stages, too, can be of two halves.)
+          if (const int m = eights((st + 2) * 64); m != eights(st > 0 ? (st + 1) * 64 : 0) && (m + 1) * kTableBlocks < a.blocks) {
             coming = m + 1;
             fb.load_table(coming);
           }
@@ -428,10 +429,6 @@ GroupedArgs grouped_args(const Int4Args& a) {
   g.partial = a.partial;
   return g;
 }
-inline int rows_of_tiles(const GroupedArgs& g) {
-  const int rows = tile_rows(g, kElemBF16);
-  return rows == kShortRows ? 128 : rows;
-}
 
 template <int TY, int BM, bool S32>
 hipError_t launch(GroupedArgs g, const Int4Args& a, hipStream_t s) {
@@ -453,8 +450,8 @@ hipError_t launch(GroupedArgs g, const Int4Args& a, hipStream_t s) {
 template <int TY>
 hipError_t launch_type(const Int4Args& a, hipStream_t s) {
   const GroupedArgs g = grouped_args(a);
-  if (a.scale_type == kElemF32) return rows_of_tiles(g) == 128 ? launch<TY, 128, true>(g, a, s) : launch<TY, kGT, true>(g, a, s);
-  return rows_of_tiles(g) == 128 ? launch<TY, 128, false>(g, a, s) : launch<TY, kGT, false>(g, a, s);
+  if (a.scale_type == kElemF32) return tile_rows(g, kElemBF16) == 128 ? launch<TY, 128, true>(g, a, s) : launch<TY, kGT, true>(g, a, s);
+  return tile_rows(g, kElemBF16) == 128 ? launch<TY, 128, false>(g, a, s) : launch<TY, kGT, false>(g, a, s);
 }
 
 }  // namespace
@@ -467,7 +464,7 @@ bool int4_tiles_fit(const Int4Args& a) {
 }
 size_t int4_tiles_bytes(const Int4Args& a) {
   const GroupedArgs g = grouped_args(a);
-  const int BM = rows_of_tiles(g);
+  const int BM = tile_rows(g, kElemBF16);
   return (size_t)(rows_room(g, kElemBF16, BM).parts * (kPartialBytes / kGT * BM));
 }
 hipError_t launch_int4_tiles(const Int4Args& a, hipStream_t s) { return a.type == kElemBF16 ? launch_type<kElemBF16>(a, s) : launch_type<kElemF16>(a, s); }
