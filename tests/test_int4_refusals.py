@@ -112,11 +112,12 @@ def test_pointers():
 
 
 def test_workspace_sizes():
-    """Few tiles of long sums are split; many, short sums, many rows and fp32 are not."""
+    """Few tiles of long sums are split, and the last ones of many; streams, short sums, many rows and fp32 are not."""
     def size(**kw):
         return _lib.dsmoe_int4_workspace_bytes(ops._Int4Args(**dict(ARGS, **kw)))
 
-    assert size(rows=1, groups=1, k=4096, n=4096) > 0 and size(rows=1, groups=1, k=256, n=4096) == 0 and size(rows=64, groups=8, k=4096, n=1 << 17) == 0
+    assert size(rows=1, groups=1, k=8192, n=4096) > 0 and size(rows=512, groups=1, k=4096, n=4096) > 0 and size(rows=8300, groups=1, k=2048, n=1808) > 0
+    assert size(rows=1, groups=1, k=4096, n=4096) == 0 and size(rows=512, groups=1, k=256, n=4096) == 0 and size(rows=64, groups=8, k=4096, n=1 << 17) == 0
     assert size(rows=1, groups=1, k=4096, n=4096, dtype=0, scale_dtype=0) == 0 and size(rows=-1) == 0 and size(block=48) == 0
     assert _lib.dsmoe_int4_workspace_bytes(None) == 0
 
