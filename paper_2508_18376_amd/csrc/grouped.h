@@ -235,15 +235,14 @@ inline size_t grouped_workspace_bytes(const GroupedArgs& g, int type, bool b_alo
 inline size_t grouped_dw_workspace_bytes(const GroupedArgs& g, int type) { return type == kElemF32 ? 0 : grouped_dw_split_bytes(g); }
 // g.b2 and g.c2: a second product with the same left operand.  (Tiles: a launch for each; in one, long ones would end no better.)
 inline hipError_t launch_grouped_dw(const GroupedArgs& g, int type, hipStream_t s) {
-  if (g.c2 != nullptr && grouped_dw_mfma_fits(g, type)) {
-    GroupedArgs one = g, two = g;
-    one.c2 = two.c2 = nullptr;
-    two.b = g.b2;
-    two.c = g.c2;
-    const hipError_t e = launch_grouped_dw_mfma(one, type, s);
-    return e != hipSuccess ? e : launch_grouped_dw_mfma(two, type, s);
-  }
-  return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
+  if (g.c2 == nullptr) return grouped_dw_mfma_fits(g, type) ? launch_grouped_dw_mfma(g, type, s) : launch_grouped_dw_plain(g, type, s);
+  GroupedArgs one = g, two = g;
+  one.c2 = two.c2 = nullptr;
+  two.b = g.b2;
+  two.c = g.c2;
+  if (!grouped_dw_mfma_fits(one, type) || !grouped_dw_mfma_fits(two, type)) return launch_grouped_dw_plain(g, type, s);
+  const hipError_t e = launch_grouped_dw_mfma(one, type, s);
+  return e != hipSuccess ? e : launch_grouped_dw_mfma(two, type, s);
 }
 
 // position of chunk `chunk` (0..7) of row `row` in a [rows][128 bytes] tile; its own inverse.  Two rows are a turn of the banks.

@@ -14,7 +14,15 @@ hipError_t launch_grouped_plain(const GroupedArgs& g, int type, bool b_along, hi
 }
 
 hipError_t launch_grouped_dw_plain(const GroupedArgs& g, int type, hipStream_t s) {
-  const int64_t blocks = (int64_t)g.G * ((g.M + kPT - 1) / kPT) * ((g.N + kPT - 1) / kPT) * (g.c2 != nullptr ? 2 : 1);
+  const int64_t each = (int64_t)g.G * ((g.M + kPT - 1) / kPT) * ((g.N + kPT - 1) / kPT), blocks = g.c2 != nullptr ? 2 * each : each;
+  if (g.c2 != nullptr && blocks * 256 >= (int64_t)1 << 32) {  // (a launch of 2^32 threads is silently cut short; of one product's tiles there are less)
+    GroupedArgs one = g, two = g;
+    one.c2 = two.c2 = nullptr;
+    two.b = g.b2;
+    two.c = g.c2;
+    const hipError_t e = launch_grouped_dw_plain(one, type, s);
+    return e != hipSuccess ? e : launch_grouped_dw_plain(two, type, s);
+  }
   switch (type) {
     case kElemF32: return launch<kElemF32, true, true>(g, blocks, s);
     case kElemBF16: return launch<kElemBF16, true, true>(g, blocks, s);

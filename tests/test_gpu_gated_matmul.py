@@ -339,3 +339,49 @@ def test_values_that_a_graph_kept_are_not_overwritten_in_silence():
     moe_gated_matmul(x, w, w, out=out)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_a_second_gradient_that_starts_anywhere():
+    """The C call with dw3 two bytes behind 16: the same values as on 16 bytes, within the products' bounds, and nothing around them."""
+    from paper_2508_18376_amd import operators as ops
+    counts, k, n = [70, 0, 129], 136, 200
+    off, R = offsets_of(counts), sum(counts)
+    x, w1, w3, dh = tensors(R, 3, k, n, torch.bfloat16, 60)
+    xd, ud, vd, dd, od = (t.to(DEV) for t in (x, w1, w3, dh, off))
+    _, saved = ops.moe_gated_matmul(xd, ud, vd, od, want_saved=True)
+    dx, dw1, wide = torch.empty_like(xd), torch.empty_like(ud), torch.full((3 * k * n + 2,), 7.0, dtype=torch.bfloat16, device=DEV)
+    args = ops._GatedArgs(R, 3, k, n, 1, 0, k, k * n, n, n)
+    size = ops._lib.dsmoe_gated_backward_workspace_bytes(args)
+    workspace = torch.empty(size, dtype=torch.uint8, device=DEV)
+    rc = ops._lib.moe_gated_matmul_backward(args, dd.data_ptr(), xd.data_ptr(), ud.data_ptr(), vd.data_ptr(), saved.data_ptr(), od.data_ptr(), dx.data_ptr(),
+                                            dw1.data_ptr(), wide.data_ptr() + 2, workspace.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0 and wide[0] == 7 and wide[-1] == 7
+    want = reference(x, w1, w3, off, "silu", dh)
+    for name, got in (("dx", dx), ("dw1", dw1), ("dw3", wide[1:-1].view(3, k, n))):
+        assert_within(got, *want[name], name)
+
+
+def test_as_many_tiles_of_gradients_as_there_may_be():
+    """2^23 tiles of 128 columns for each weight: 65536 groups of one value by 16384, of which three have rows."""
+    G, n, at = 65536, 16384, {0: 2, 40000: 1, 65535: 3}
+    ends = torch.zeros(G + 1, dtype=torch.int64)
+    for g, rows in at.items():
+        ends[g + 1:] += rows
+    x, dh = make((6, 1), torch.float16, 61), make((6, n), torch.float16, 62)
+    w1, w3 = (torch.zeros(G, 1, n, dtype=torch.float16, device=DEV) for _ in range(2))
+    some = {g: (make((1, n), torch.float16, 63 + g), make((1, n), torch.float16, 64 + g)) for g in at}
+    for g, (u, v) in some.items():
+        w1[g], w3[g] = u.to(DEV), v.to(DEV)
+    got = both(x.to(DEV), w1, w3, ends.int().to(DEV), "silu", dh.to(DEV))
+    small = torch.stack([u for u, _ in some.values()]), torch.stack([v for _, v in some.values()])
+    want = reference(x, *small, offsets_of(list(at.values())), "silu", dh)
+    for name in ("h", "dx"):
+        assert_within(got[name], *want[name], name)
+    for name in ("dw1", "dw3"):
+        for i, g in enumerate(at):
+            assert_within(got[name][g], want[name][0][i], want[name][1][i], name)
+            got[name][g] = 0
+        assert not got[name].any(), name
+    del got, w1, w3
+    torch.cuda.empty_cache()
