@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
   for (int t = 0; t < NR; ++t) {
     const int r = (w * NR + t) * 4 + (lane >> 4);
     x_chunk[t] = (lane & 15) ^ (r & 15);
-    x_off[t] = (uint32_t)min(r, p.rows - 1) * (uint32_t)a.x_row + x_chunk[t] * 16;
+    x_off[t] = r < p.rows ? (uint32_t)r * (uint32_t)a.x_row + x_chunk[t] * 16 : kBeyond;
   }
   s_off = (uint32_t)min(w * 64 + lane, p.cols - 1) * (uint32_t)a.s_row * EB;
   z_off = (uint32_t)min(w * 64 + lane, p.cols - 1) * (uint32_t)a.z_row;
@@ -134,15 +134,17 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
 #pragma unroll
     for (int j = 0; j < J; ++j) total[r][j] = qf32x4{0, 0, 0, 0};
   const uint32_t no_zeros = a.zero ? 0 : 8;
-  auto multiply = [&](const char* at) __attribute__((always_inline)) {
+  // BLOCKS of sixteen rows
+  auto multiply = [&](const char* at, auto blocks) __attribute__((always_inline)) {
+    constexpr int BLOCKS = decltype(blocks)::value;
     const int one = (int)Unit<TY>::one;
     const qi32x4 ones = {one, one, one, one};
     constexpr int WORDS = Sh::WORDS;
 #pragma unroll
     for (int s = 0; s < Sh::SPANS; ++s) {
-      qf32x4 sum[NR], acc[NR][J];
+      qf32x4 sum[BLOCKS], acc[BLOCKS][J];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
+      for (int r = 0; r < BLOCKS; ++r) {
         sum[r] = qf32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[r][j] = qf32x4{0, 0, 0, 0};
@@ -154,9 +156,9 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
         __builtin_memcpy(wd[j], __builtin_assume_aligned(at + w * 4096 + (16 * j + i) * 64 + ((o >> 4) ^ (i >> 2)) * 16 + (o & 15), WORDS * 4), WORDS * 4);
 #pragma unroll
       for (int m = 0; m < WORDS; ++m) {
-        qi32x4 x[NR];
+        qi32x4 x[BLOCKS];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
+        for (int r = 0; r < BLOCKS; ++r) {
           x[r] = paired(*(const qi32x4*)(at + Sh::x_at + (16 * r + i) * 256 + ((s * (SPAN / 8) + q * WORDS + m) ^ i) * 16));
           mac4<TY>(sum[r], x[r], ones);
         }
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
         for (int j = 0; j < J; ++j) {
           const qi32x4 v = widened<TY>(wd[j][m]);
 #pragma unroll
-          for (int r = 0; r < NR; ++r) mac4<TY>(acc[r][j], x[r], v);
+          for (int r = 0; r < BLOCKS; ++r) mac4<TY>(acc[r][j], x[r], v);
         }
       }
 #pragma unroll
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
         const uint32_t* sz = (const uint32_t*)(at + Sh::s_at) + s * 2 * kCols + w * 64 + 16 * j + i;
         const float f = scale_of<TY, S32>(sz[0]), z = zero_of(sz[kCols] | no_zeros);
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+        for (int r = 0; r < BLOCKS; ++r)
 #pragma unroll
           for (int v = 0; v < 4; ++v) total[r][j][v] += f * (acc[r][j][v] - z * sum[r][v]);
       }
@@ -182,19 +184,29 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
 #pragma unroll
   for (int st = 0; st < RING - 1; ++st)
     if (st < n) load(st);
-  for (int st = 0; st < n; ++st) {
-    // stage st is there for every wavefront, and every wavefront has read the one before, whose place stage st + RING - 1 takes
-    const int behind = min(RING - 2, n - 1 - st);
-    if (behind >= 2)
-      loads_but<2 * Sh::loads>();
-    else if (behind == 1)
-      loads_but<Sh::loads>();
-    else
-      loads_but<0>();
-    meet();
-    if (st + RING - 1 < n) load(st + RING - 1);
-    multiply(ring + (st % RING) * Sh::bytes);
+  auto stages_of = [&](auto blocks) __attribute__((always_inline)) {
+    for (int st = 0; st < n; ++st) {
+      // stage st is there for every wavefront, and every wavefront has read the one before, whose place stage st + RING - 1 takes
+      const int behind = min(RING - 2, n - 1 - st);
+      if (behind >= 2)
+        loads_but<2 * Sh::loads>();
+      else if (behind == 1)
+        loads_but<Sh::loads>();
+      else
+        loads_but<0>();
+      meet();
+      if (st + RING - 1 < n) load(st + RING - 1);
+      multiply(ring + (st % RING) * Sh::bytes, blocks);
+    }
+  };
+  const int blocks = (p.rows + 15) / 16;
+  if constexpr (NR >= 4) {
+    if (blocks == 4) stages_of(std::integral_constant<int, 4>());
+    if (blocks == 3) stages_of(std::integral_constant<int, 3>());
   }
+  if constexpr (NR >= 2)
+    if (blocks == 2) stages_of(std::integral_constant<int, 2>());
+  if (blocks == 1) stages_of(std::integral_constant<int, 1>());
   meet();
 
   // The wavefront turns sixteen rows of its 64 channels around in LDS at a time: rows of 256 bytes whose 64-byte blocks are rotated by a quarter of the row.
