@@ -133,15 +133,24 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
   for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int j = 0; j < J; ++j) total[r][j] = qf32x4{0, 0, 0, 0};
-  const uint32_t no_zeros = a.zero ? 0 : 8;
+  // What is taken off for the zero points, the sum of x times (16 + z) s, is a product over the spans itself: of four spans at a time, the q-th one's factors in
+  // lanes 16 q .., by the fp32 matrix instructions (by the vector units it is a quarter of their instructions: 1998 rows on 64 groups of 2048 x 1408 60.5 us
+  // instead of 58.5).
+  float xs[NR], zs[J];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) xs[r] = 0;
+#pragma unroll
+  for (int j = 0; j < J; ++j) zs[j] = 0;
+  const uint32_t no_zeros = a.zero ? 0 : 8, one = one_of<TY>();
   // BLOCKS of sixteen rows
-  auto multiply = [&](const char* at, auto blocks) __attribute__((always_inline)) {
+  auto multiply = [&](const char* at, int st, auto blocks) __attribute__((always_inline)) {
     constexpr int BLOCKS = decltype(blocks)::value;
-    const int one = (int)Unit<TY>::one;
-    const qi32x4 ones = {one, one, one, one};
+    const qi32x4 ones = {(int)one, (int)one, (int)one, (int)one};
     constexpr int WORDS = Sh::WORDS;
 #pragma unroll
     for (int s = 0; s < Sh::SPANS; ++s) {
+      const int place = (st * Sh::SPANS + s) & 3;
+      const float mine = q == place ? 1.f : 0.f;
       qf32x4 sum[BLOCKS], acc[BLOCKS][J];
 #pragma unroll
       for (int r = 0; r < BLOCKS; ++r) {
@@ -160,11 +169,11 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
 #pragma unroll
         for (int r = 0; r < BLOCKS; ++r) {
           x[r] = paired(*(const qi32x4*)(at + Sh::x_at + (16 * r + i) * 256 + ((s * (SPAN / 8) + q * WORDS + m) ^ i) * 16));
-          mac4<TY>(sum[r], x[r], ones);
+          mac4<TY>(sum[r], ones, x[r]);
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          const qi32x4 v = widened<TY>(wd[j][m]);
+          const qi32x4 v = widened<TY>(wd[j][m], one);
 #pragma unroll
           for (int r = 0; r < BLOCKS; ++r) mac4<TY>(acc[r][j], x[r], v);
         }
@@ -173,10 +182,24 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
       for (int j = 0; j < J; ++j) {
         const uint32_t* sz = (const uint32_t*)(at + Sh::s_at) + s * 2 * kCols + w * 64 + 16 * j + i;
         const float f = scale_of<TY, S32>(sz[0]), z = zero_of(sz[kCols] | no_zeros);
+        zs[j] = fmaf(-f * z, mine, zs[j]);
 #pragma unroll
         for (int r = 0; r < BLOCKS; ++r)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) total[r][j][v] += f * (acc[r][j][v] - z * sum[r][v]);
+          for (int v = 0; v < 4; ++v) total[r][j][v] = fmaf(f, acc[r][j][v], total[r][j][v]);
+      }
+#pragma unroll
+      for (int r = 0; r < BLOCKS; ++r)
+        xs[r] = fmaf(sum[r][0], mine, xs[r]);
+      if (place == 3 || (s == Sh::SPANS - 1 && st == n - 1)) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+#pragma unroll
+          for (int r = 0; r < BLOCKS; ++r) total[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xs[r], zs[j], total[r][j], 0, 0, 0);
+          zs[j] = 0;
+        }
+#pragma unroll
+        for (int r = 0; r < BLOCKS; ++r) xs[r] = 0;
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -196,7 +219,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
         loads_but<0>();
       meet();
       if (st + RING - 1 < n) load(st + RING - 1);
-      multiply(ring + (st % RING) * Sh::bytes, blocks);
+      if (w * 64 < p.cols) multiply(ring + (st % RING) * Sh::bytes, st, blocks);
     }
   };
   const int blocks = (p.rows + 15) / 16;

@@ -143,8 +143,8 @@ __global__ __launch_bounds__(64 * W, 2) void int4_stream_kernel(Int4Args a) {
     for (int j = 0; j < J; ++j) total[r][j] = qf32x4{0, 0, 0, 0};
   auto multiply = [&](const auto& t) __attribute__((always_inline)) {
     typedef std::remove_const_t<std::remove_reference_t<decltype(t)>> T;
-    const int one = (int)Unit<TY>::one;
-    const qi32x4 ones = {one, one, one, one};
+    const uint32_t one = one_of<TY>();
+    const qi32x4 ones = {(int)one, (int)one, (int)one, (int)one};
 #pragma unroll
     for (int p = 0; p < T::SPANS; ++p) {
       qf32x4 sum[NR], acc[NR][J];
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * W, 2) void int4_stream_kernel(Int4Args a) {
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          const qi32x4 w = widened<TY>(t.w[j][p][m]);
+          const qi32x4 w = widened<TY>(t.w[j][p][m], one);
 #pragma unroll
           for (int r = 0; r < NR; ++r) mac4<TY>(acc[r][j], x[r], w);
         }

@@ -32,14 +32,21 @@ __device__ __forceinline__ void mac4(qf32x4& c, const qi32x4& a, const qi32x4& b
     c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(qf16x8, a), __builtin_bit_cast(qf16x8, b), c, 0, 0, 0);
 }
 
+// Unit::one in a vector register: an and-or takes one constant from the scalar ones (left to itself the compiler makes it two instructions with literals).
+template <int TY>
+__device__ __forceinline__ uint32_t one_of() {
+  uint32_t one = Unit<TY>::one;
+  asm("" : "+v"(one));
+  return one;
+}
 // eight weights as 1 + q / 16, in pairs (j, j + 4)
 template <int TY>
-__device__ __forceinline__ qi32x4 widened(uint32_t w) {
+__device__ __forceinline__ qi32x4 widened(uint32_t w, uint32_t one) {
   qi32x4 v;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int by = 4 * j - Unit<TY>::up;
-    v[j] = (int)(((by < 0 ? w << -by : w >> by) & Unit<TY>::mask) | Unit<TY>::one);
+    v[j] = (int)(((by < 0 ? w << -by : w >> by) & Unit<TY>::mask) | one);
   }
   return v;
 }
