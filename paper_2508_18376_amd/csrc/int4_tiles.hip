@@ -13,6 +13,9 @@
 // channels' for every stage looked up more lines of them than of weights and x together (a compute unit looks up one a clock), and the loads that the
 // matrix instructions wait for queued behind.
 //
+// Bound by the matrix cores and the instructions between them: 4096 rows of 4096 x 14336 506 us, 950 TFLOP/s, the cores busy for 46 % of the time (without loads
+// 417, without loads and widening 347 us).
+//
 // The rounding of a weight is of the size of the result's own.  The exact way of the tiles of few rows (int4_widen.h) needs a second set of sums, so tiles of half
 // as many rows, at twice the weights' traffic and vector instructions.
 #include "grouped_tiles.h"
