@@ -401,7 +401,8 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
  * (groups = 1).  Rows of w on 16 bytes are faster.  Rows of no group: zeros.
  *   In 16-bit types calls of many rows, and those whose rows start anywhere, round each weight (q - z) s to dtype once (f16: after a power of two
  *   for each output channel has brought it into range); the others are exact but for their sums, of which they take two apart, 16 s times that of
- *   x (1 + q / 16) and (16 + z) s times that of x, so bf16 rows whose |x| add up to more than 2^126 can overflow.  Sums are in 32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
+ *   x (1 + q / 16) and (16 + z) s times that of x, so bf16 rows whose |x|, or |x| (16 + z) |s|, add up to 2^126 and more can overflow.  Sums are in
+ *   32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
  *   workspace as for moe_grouped_matmul, dsmoe_int4_workspace_bytes(args) bytes or NULL.
  * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
  */
