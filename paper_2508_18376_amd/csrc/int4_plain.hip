@@ -1,6 +1,7 @@
 // Products with weights in 4 bits, for every type, alignment and number of rows: the tiles of 128 x 128 of grouped_plain.h, whose weights are widened on their way
 // from registers to LDS.  16-bit types: (q - z) s is rounded to x's type once, which is what the matrix instructions take; fp32 products are fp32.
-// Bound by the matrix instructions in fp32 (4096 rows of 4096 x 14336 4033 us, 119 of 153 TFLOP/s), by the way through registers in 16 bits: weights that start
+// Sums of fp32 go in parts (see Parts); as one chain 4096 rows of 4096 x 14336 took 4030 us, 17 of 14336 x 4096 1135 instead of 1195.
+// Bound by the matrix instructions in fp32 (4096 rows of 4096 x 14336 4134 us, 116 of 154 TFLOP/s; few rows are tiles of 128 all the same), by the way through registers in 16 bits: weights that start
 // off 16 bytes 1129 us, 426 TFLOP/s, where int4_tiles.hip takes 506.
 #include "grouped_plain.h"
 #include "int4_matmul.h"
@@ -18,9 +19,10 @@ struct Weights4 {
   const uint8_t* p[kChunks];
   int64_t s_at[kChunks], z_at[kChunks];
   int first, column, row_bytes, exponent[kChunks];
+  // (z: in fp32 the third byte of q, whose weights are two; the register more each would not leave those that Parts takes)
   struct Stage {
-    uint32_t q[kChunks];
-    float s[kChunks], z[kChunks];
+    uint32_t q[kChunks], z[TY == kElemF32 ? 1 : kChunks];
+    float s[kChunks];
   };
 
   // n0: first output channel, of which `edge` exist; the last one again behind them
@@ -58,16 +60,21 @@ struct Weights4 {
           if (b < left) v.q[i] |= (uint32_t)p[i][at + b] << (8 * b);
       }
       v.s[i] = int4_scale(a, s_at[i] + block);
-      v.z[i] = a.zero ? (float)a.zero[z_at[i] + block] : 8.f;
+      const uint32_t z = a.zero ? a.zero[z_at[i] + block] : 8;
+      if (TY == kElemF32)
+        v.q[i] |= z << 16;
+      else
+        v.z[TY == kElemF32 ? 0 : i] = z;
     }
   }
   __device__ __forceinline__ void store(char* tile, const Stage& v) const {
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       const float s = TY == kElemF16 ? ldexpf(v.s[i], -exponent[i]) : v.s[i];
+      const float z = (float)(TY == kElemF32 ? v.q[i] >> 16 : v.z[TY == kElemF32 ? 0 : i]);
       float f[VALUES];
 #pragma unroll
-      for (int e = 0; e < VALUES; ++e) f[e] = ((float)(v.q[i] >> (4 * e) & 15) - v.z[i]) * s;
+      for (int e = 0; e < VALUES; ++e) f[e] = ((float)(v.q[i] >> (4 * e) & 15) - z) * s;
       pi32x4 out;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -99,6 +106,7 @@ __global__ __launch_bounds__(256, 2) void int4_plain_kernel(Int4Args a) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int q = 0; q < 16; ++q) acc[i >> 1][i & 1].v[q] = 0;
+  Parts<TY == kElemF32> parts;
   Operand<TY, false> oa;
   Weights4<TY> ob;
   oa.init(a.x + (int64_t)(s.row0 + m0) * a.x_row, a.x_row, m_edge, 0);
@@ -141,7 +149,9 @@ __global__ __launch_bounds__(256, 2) void int4_plain_kernel(Int4Args a) {
         for (int j = 0; j < 4; ++j) acc[j >> 1][j & 1].mac(fb[j & 1], fa[j >> 1]);
       }
     }
+    parts.step(acc);
   }
+  parts.end(acc);
   __syncthreads();
 
   // as grouped_plain_kernel stores its tile
