@@ -35,14 +35,15 @@ NO_SCRATCH = {
 }
 # ... and among the operators beside the layer.
 OPERATORS_NO_SCRATCH = {
+    "grouped_plain.hip": ("grouped_plain_kernel",),
     "grouped_mfma.hip": ("grouped_mfma_kernel", "grouped_dw_mfma_kernel"),
     "grouped_stream.hip": ("grouped_stream_kernel",),
-    "gated_pair.hip": ("grouped_mfma_kernel", "grouped_stream_kernel"),
+    "gated_pair.hip": ("grouped_mfma_kernel", "grouped_stream_kernel", "grouped_plain_kernel"),
     "int4_stream.hip": ("int4_stream_kernel",),
     "int4_plain.hip": ("int4_plain_kernel",),
     "int4_tiles.hip": ("int4_tiles_kernel",),
     "int4_short.hip": ("int4_short_kernel",),
-    "gated_sum.hip": ("grouped_mfma_kernel", "grouped_stream_kernel"),
+    "gated_sum.hip": ("grouped_mfma_kernel", "grouped_stream_kernel", "grouped_plain_kernel"),
 }
 
 

@@ -168,7 +168,8 @@ struct Acc<kElemI8> {
 
 // A wavefront's fp32 sums over a long contraction, in parts: after every eight steps of the main loop (two stages each, 512 values in all) what has come together
 // goes to a second set of sums.  In one chain the error grows with the square root of the length (products in 4 bits, 4096 / 14336 values 1.1e-6 / 2.0e-6 of the
-// result), in parts it hardly does (3.7e-7 / 4.1e-7).  Times: see int4_plain.hip.
+// result), in parts it hardly does (3.7e-7 / 4.1e-7).  Gated pairs and their gradients take no longer for it (4096 rows, 8 experts of 4096 x 14336: forward 7.3 ms,
+// backward 15.8 ms either way); products in 4 bits: see int4_plain.hip.
 template <bool ON>
 struct Parts {
   template <class A>
@@ -201,11 +202,12 @@ struct Parts<true> {
 __device__ __forceinline__ int last_tile(int t, int width, int tile = kPT) { return width >= tile ? min(t * tile, width - tile) : 0; }
 
 // DW: both operands across the contraction, which runs over the group's rows; else A along it, and B across (BX) or along.
-// MODE (not DW): one product; a gated pair (BX), whose tile is 64 columns of both; or a sum of two, one after the other.
+// MODE (not DW): one product; a gated pair (BX), whose tile is 64 columns of both; or a sum of two, one after the other.  DW: one product; a gated pair's two
+// gradients, whose fp32 sums go in parts.
 template <int TY, bool BX, bool DW, int MODE>
 __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
   using E = Elem<TY>;
-  constexpr bool PAIR = MODE == kGatedPair;
+  constexpr bool PAIR = !DW && MODE == kGatedPair;
   constexpr int COLS = PAIR ? kPT / 2 : kPT;
   __shared__ __align__(16) char lds[4 * kTileBytes];  // 64 KiB: two workgroups to a compute unit
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -258,6 +260,7 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int q = 0; q < 16; ++q) acc[i >> 1][i & 1].v[q] = 0;
+  Parts<TY == kElemF32 && MODE != kOneProduct> parts;
 
 #pragma unroll 1
   for (int half = 0; half < (MODE == kSumOfTwo ? 2 : 1); ++half) {
@@ -271,10 +274,12 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
     oa.init(pa, g.a_row, m_edge, m0);
     ob.init(ob.second() ? g.b2 + (pb - g.b) : pb, g.b_row, n_edge, n0);
     const int mw = (w & 1) * 64, nw = (w >> 1) * 64;
-    // two stages are under way: while one is multiplied, the next one's loads have that time, and the one's behind it too
-    pi32x4 va[2][kChunks], vb[2][kChunks];
+    // two stages are under way: while one is multiplied, the next one's loads have that time, and the one's behind it too (a sum of two in fp32 has registers for
+    // one only; fp32 stages take several times as long)
+    constexpr int AHEAD = MODE == kSumOfTwo && TY == kElemF32 ? 1 : 2;
+    pi32x4 va[AHEAD][kChunks], vb[AHEAD][kChunks];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < AHEAD; ++i)
       if (i * E::k_stage < K) {
         oa.load(va[i], K - i * E::k_stage);
         ob.load(vb[i], K - i * E::k_stage);
@@ -285,12 +290,12 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
         const int left = K - k - i * E::k_stage;
         if (left <= 0) break;
         char *ta = lds + i * 2 * kTileBytes, *tb = ta + kTileBytes;
-        oa.store(ta, va[i]);
-        ob.store(tb, vb[i]);
+        oa.store(ta, va[i % AHEAD]);
+        ob.store(tb, vb[i % AHEAD]);
         __syncthreads();  // (this buffer's last readers passed the barrier of the stage before)
-        if (left > 2 * E::k_stage) {
-          oa.load(va[i], left - 2 * E::k_stage);
-          ob.load(vb[i], left - 2 * E::k_stage);
+        if (left > AHEAD * E::k_stage) {
+          oa.load(va[i % AHEAD], left - AHEAD * E::k_stage);
+          ob.load(vb[i % AHEAD], left - AHEAD * E::k_stage);
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -304,9 +309,11 @@ __global__ __launch_bounds__(256, 2) void grouped_plain_kernel(GroupedArgs g) {
           for (int j = 0; j < 4; ++j) acc[j >> 1][j & 1].mac(fb[j & 1], fa[j >> 1]);
         }
       }
+      parts.step(acc);
     }
     __syncthreads();
   }
+  parts.end(acc);
 
   // A lane holds row lane % 32 of the block and, for q = 0 .. 3, the four columns 8 q + 4 (lane / 32) ..: a wavefront turns 32 rows of its 64 columns
   // around in LDS and stores them 16 bytes a lane (straight from the registers, 8 bytes of a row each, a dW of 33 x 1001 x 1409 took 81 us instead of 50).
