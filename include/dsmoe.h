@@ -400,9 +400,10 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
  * uint8, shaped like it, or NULL: 8 everywhere.  block: a power of two from 32 on.  offsets as above, or NULL for one group of all rows
  * (groups = 1).  Rows of w on 16 bytes are faster.  Rows of no group: zeros.
  *   In 16-bit types calls of many rows, and those whose rows start anywhere, round each weight (q - z) s to dtype once (f16: after a power of two
- *   for each output channel has brought it into range); the others are exact but for their sums, of which they take two apart, 16 s times that of
- *   x (1 + q / 16) and (16 + z) s times that of x, so bf16 rows whose |x|, or |x| (16 + z) |s|, add up to 2^126 and more can overflow.  Sums are in
- *   32 bits.  A row of x with an infinity or NaN has infinities or NaN in its outputs, which of the two is not said.
+ *   for each output channel has brought it into range); the others are exact but for their sums, which are in 32 bits.  Infinities and NaN in x go
+ *   through products and sums as they are (an infinity times a weight that is zero, or rounds to it, is NaN).  With few rows, outputs that come out
+ *   infinite or NaN are worked out once more, one by one: many of them make a call slow.  A scale of 2^120 and more, an infinity or NaN
+ *   among them, can make its channel's outputs infinite or NaN.
  *   workspace as for moe_grouped_matmul, dsmoe_int4_workspace_bytes(args) bytes or NULL.
  * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
  */

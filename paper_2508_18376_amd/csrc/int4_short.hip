@@ -241,12 +241,27 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void int4_short_kernel(Int4Ar
   char* sums = a.partial + (int64_t)p.seg.total * (Sh::ROWS * kCols * 4);
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
+    bool finite = true;
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) *(float*)(turn + (4 * q + v) * 256 + ((j ^ q) * 16 + i) * 4) = 16.f * total[r][j][v];
+      for (int v = 0; v < 4; ++v) {
+        const float sum = 16.f * total[r][j][v];
+        finite = finite && __builtin_isfinite(sum);
+        *(float*)(turn + (4 * q + v) * 256 + ((j ^ q) * 16 + i) * 4) = sum;
+      }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    if (__any(!finite)) {
+#pragma unroll 1
+      for (int row = 0; row < 16; ++row) {  // the lane's channel of each row
+        float* at = (float*)(turn + row * 256 + ((q ^ (row >> 2)) * 16 + i) * 4);
+        if (!__builtin_isfinite(*at) && r * 16 + row < p.rows && w * 64 + lane < p.cols)
+          *at = sum_again<TY>(a, p.seg.group, p.seg.row0 + p.m0 + r * 16 + row, p.n0 + w * 64 + lane, first * kStage, min(a.K, (first + n) * kStage));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int row = h * 8 + (lane >> 3), c = (lane & 7) * 8, rr = r * 16 + row;

@@ -232,7 +232,8 @@ __global__ __launch_bounds__(64 * W, 2) void int4_stream_kernel(Int4Args a) {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) v += ((const float*)lds)[w * (16 * kRowFloats4) + row * kRowFloats4 + col + p];
-        if (col + p < cols) y[p] = f32_to_16(16.f * v, TY);
+        v *= 16.f;
+        if (col + p < cols) y[p] = f32_to_16(__builtin_isfinite(v) ? v : sum_again<TY>(a, seg.group, seg.row0 + m0 + rr, n0 + col + p, 0, K), TY);
       }
     }
   }
