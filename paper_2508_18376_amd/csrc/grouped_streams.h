@@ -347,14 +347,15 @@ constexpr int64_t kLastLevelBytes = 256ll << 20;
 // 9.8 us).  Many: whole 256-byte rows of 128 columns across the contraction, in workgroups of 4 wavefronts of which two share a
 // compute unit, so that one's beginning and end lie in the other's stream (64 tokens on 8 of 4096 x 14336: 8 wavefronts 171, 4 167; 64
 // columns 176).
-// Rows that do not start on 16 bytes keep to 64 columns, 8 bytes a lane: loads of 16 bytes from elsewhere are slow.
+// Rows that do not start on 16 bytes, of either weight (b2: nullptr for one product), keep to 64 columns, 8 bytes a lane: loads of 16 bytes from elsewhere are slow
+// (a gated pair's weights as halves of rows of 2824 values, 64 tokens on 64 experts of 2048 x 1412: 259 us, like this 178).
 template <int TY, int OUT, bool BX, int MODE = kOneProduct>
 hipError_t launch_w(const GroupedArgs& g, hipStream_t s) {
   const int64_t pieces = row_tiles_bound(g.R, g.G, g.off != nullptr, kStreamTile) * ((g.N + 63) / 64);
   // (a gated pair in fp32 has no registers left for 16)
   if (pieces < 512) return launch<TY, OUT, BX, 4, MODE == kGatedPair && TY == kElemF32 ? 8 : 16, false, MODE>(g, s);
   constexpr bool WIDE = BX && TY != kElemF32;
-  if (WIDE && (((uintptr_t)g.b | g.b_row | g.b_group) & 15) != 0) return launch<TY, OUT, BX, 4, 8, false, MODE>(g, s);
+  if (WIDE && (((uintptr_t)g.b | (uintptr_t)g.b2 | g.b_row | g.b_group) & 15) != 0) return launch<TY, OUT, BX, 4, 8, false, MODE>(g, s);
   const bool once = (int64_t)(g.G < g.R ? g.G : g.R) * g.K * g.N * SElem<TY, BX>::bytes > kLastLevelBytes;
   return once ? launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, true, MODE>(g, s) : launch<TY, OUT, BX, WIDE ? 8 : 4, WIDE ? 4 : 8, false, MODE>(g, s);
 }
