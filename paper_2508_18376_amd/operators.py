@@ -625,15 +625,24 @@ def _rows_of(f, name, t, out):
     return rows, width, s, o
 
 
+def _check_tensors(f, name, tensors):
+    """(Without this a gradient that is None, as of a parameter that took no part, would end in an AttributeError.)"""
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.layout is not torch.strided:
+            _refuse(f, "%s must be a list of tensors, dense ones; leave out what has no gradient" % name)
+
+
 def _grads(f, grads, out):
     """The library's array of the tensors, and their GPU."""
     if not isinstance(grads, (list, tuple)) or not grads:
         _refuse(f, "grads must be a list of tensors, of at least one")
     if len(grads) > 1 << 20:
         _refuse(f, "at most 2^20 gradients")
+    _check_tensors(f, "grads", grads)
     if out is not grads:
         if not isinstance(out, (list, tuple)) or len(out) != len(grads):
             _refuse(f, "out must be a list of as many tensors as grads")
+        _check_tensors(f, "out", out)
     device, elsewhere, fields = grads[0].get_device(), False, []
     recorded = _grad_enabled() or _forward_mode._current_level >= 0
     for i, (t, o) in enumerate(zip(grads, out)):
@@ -683,8 +692,9 @@ def moe_clip_grads(grads, max_norm, eps=1e-6, out=None, stream=None):
         if not isinstance(grads, (list, tuple)):
             _refuse(f, "grads must be a list of tensors, of at least one")
         out = []  # filled below, on the stream that the call runs on
-    else:
-        if isinstance(out, (list, tuple)) and len({t.data_ptr() for t in out}) != len(out):
+    elif isinstance(out, (list, tuple)):
+        _check_tensors(f, "out" if out is not grads else "grads", out)
+        if len({t.data_ptr() for t in out}) != len(out):
             places = [t.data_ptr() for t in out if t.numel()]  # (empty tensors lie nowhere)
             if len(set(places)) != len(places):
                 _refuse(f, "out must not hold a tensor twice")
