@@ -19,6 +19,7 @@ from .binding import DsmoeError, _lib, _raw_stream
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _EINVAL, _EHIP = -1, -4
 _INT32, _INT32_MAX = torch.int32, (1 << 31) - 1
+_Tensor, _strided = torch.Tensor, torch.strided
 GATE_NONE, GATE_TOKEN, GATE_CHANNEL, GATE_FULL = 0, 1, 2, 3
 
 
@@ -625,11 +626,9 @@ def _rows_of(f, name, t, out):
     return rows, width, s, o
 
 
-def _check_tensors(f, name, tensors):
+def _no_tensor(f, name):
     """(Without this a gradient that is None, as of a parameter that took no part, would end in an AttributeError.)"""
-    for t in tensors:
-        if not isinstance(t, torch.Tensor) or t.layout is not torch.strided:
-            _refuse(f, "%s must be a list of tensors, dense ones; leave out what has no gradient" % name)
+    _refuse(f, "%s must be a list of tensors, dense ones; leave out what has no gradient" % name)
 
 
 def _grads(f, grads, out):
@@ -638,14 +637,16 @@ def _grads(f, grads, out):
         _refuse(f, "grads must be a list of tensors, of at least one")
     if len(grads) > 1 << 20:
         _refuse(f, "at most 2^20 gradients")
-    _check_tensors(f, "grads", grads)
     if out is not grads:
         if not isinstance(out, (list, tuple)) or len(out) != len(grads):
             _refuse(f, "out must be a list of as many tensors as grads")
-        _check_tensors(f, "out", out)
-    device, elsewhere, fields = grads[0].get_device(), False, []
+    device, elsewhere, fields = None, False, []
     recorded = _grad_enabled() or _forward_mode._current_level >= 0
     for i, (t, o) in enumerate(zip(grads, out)):
+        if not isinstance(t, _Tensor) or t.layout is not _strided:
+            _no_tensor(f, "grads")
+        if o is not t and (not isinstance(o, _Tensor) or o.layout is not _strided):
+            _no_tensor(f, "out")
         dtype = _DTYPES.get(t.dtype)
         if dtype is None:
             _refuse(f, "gradients must be bfloat16, float16 or float32")
@@ -654,12 +655,18 @@ def _grads(f, grads, out):
         if recorded and (t.requires_grad or o.requires_grad or _forward_mode._current_level >= 0):
             _check_unrecorded(f, t, o)
         rows, width, row, out_row = (1, t.numel(), 0, 0) if t.is_contiguous() and o.is_contiguous() else _rows_of(f, "grads[%d]" % i, t, o)
+        if device is None:
+            device = t.get_device()
         if t.get_device() != device or o is not t and o.get_device() != device:
             elsewhere = True
         fields += (t.data_ptr(), o.data_ptr(), rows, width, row, out_row, dtype)  # (dtype and pad: one of the seven words)
-    if device < 0 or elsewhere:
+    return fields, device, elsewhere or device < 0
+
+
+def _array_of(f, fields, elsewhere):
+    if elsewhere:
         _not_one_gpu(f)
-    return (ctypes.c_int64 * len(fields))(*fields), device
+    return (ctypes.c_int64 * len(fields))(*fields)
 
 
 def moe_grad_norm(grads, stream=None):
@@ -667,7 +674,8 @@ def moe_grad_norm(grads, stream=None):
 
     grads: a list of tensors on one GPU, bf16, f16 or f32 in any mixture, each dense or rows of values next to each other."""
     f = "moe_grad_norm"
-    array, device = _grads(f, grads, grads)
+    fields, device, elsewhere = _grads(f, grads, grads)
+    array = _array_of(f, fields, elsewhere)
     if stream is not None or device != _current_device():
         with _entered(f, device, stream):
             return moe_grad_norm(grads)
@@ -688,23 +696,18 @@ def moe_clip_grads(grads, max_norm, eps=1e-6, out=None, stream=None):
     if not max_norm >= 0 or not eps >= 0:
         _refuse(f, "max_norm and eps must not be negative")
     given = out
-    if out is None:
-        if not isinstance(grads, (list, tuple)):
-            _refuse(f, "grads must be a list of tensors, of at least one")
-        out = []  # filled below, on the stream that the call runs on
-    elif isinstance(out, (list, tuple)):
-        _check_tensors(f, "out" if out is not grads else "grads", out)
-        if len({t.data_ptr() for t in out}) != len(out):
-            places = [t.data_ptr() for t in out if t.numel()]  # (empty tensors lie nowhere)
-            if len(set(places)) != len(places):
-                _refuse(f, "out must not hold a tensor twice")
-    array, device = _grads(f, grads, grads if given is None else out)
+    fields, device, elsewhere = _grads(f, grads, grads if out is None else out)
+    if given is not None and len(set(fields[1::7])) != len(grads):
+        places = [fields[i + 1] for i in range(0, len(fields), 7) if fields[i + 3]]  # (of a width; empty tensors lie nowhere)
+        if len(set(places)) != len(places):
+            _refuse(f, "out must not hold a tensor twice")
+    array = _array_of(f, fields, elsewhere)
     if stream is not None or device != _current_device():
         with _entered(f, device, stream):
             return moe_clip_grads(grads, max_norm, eps, given)
     if given is None:
-        out = [torch.empty_like(t) for t in grads]
-        array, _ = _grads(f, grads, out)
+        out = [torch.empty_like(t) for t in grads]  # (on the stream that the call runs on)
+        array = _array_of(f, *_grads(f, grads, out)[::2])
     norm = grads[0].new_empty((), dtype=torch.float32)
     workspace = norm.new_empty(_CLIP_WORDS)
     rc = _lib.moe_clip_grads(array, len(grads), max_norm, eps, norm.data_ptr(), workspace.data_ptr(), _raw_stream(device))
