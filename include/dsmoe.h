@@ -404,6 +404,7 @@ int moe_block_norm_backward(const dsmoe_block_norm_args* args, const void* dy, c
  *   through products and sums as they are (an infinity times a weight that is zero, or rounds to it, is NaN).  With few rows, outputs that come out
  *   infinite or NaN are worked out once more, one by one: many of them make a call slow.  A scale of 2^120 and more, an infinity or NaN
  *   among them, can make its channel's outputs infinite or NaN.
+ *   In fp32 a call takes no less time than one of 128 rows: few rows are fast in 16-bit types only.
  *   workspace as for moe_grouped_matmul, dsmoe_int4_workspace_bytes(args) bytes or NULL.
  * rows 0 .. 2^23, groups 1 .. 65536, k and n 1 .. 2^24, and at most 2^23 tiles of 128 x 128 in all.
  */
@@ -448,7 +449,7 @@ int moe_gated_matmul_backward(const dsmoe_gated_args* args, const void* dh, cons
  * The norm over all gradients together, and clipping by it:
  *   norm = sqrt(sum over all values of grad^2)      out = grad * min(1, max_norm / (norm + eps)), rounded to dtype once
  * Squares and sums are in 64 bits, norm device float.  An infinity or NaN among the gradients shows in norm (infinity: finite values become zero,
- * infinite ones NaN; NaN: everything becomes NaN).
+ * infinite ones NaN; NaN, or an infinity where max_norm is infinite too: everything becomes NaN).
  *   grads HOST array of `count` tensors: rows of `width` values next to each other, grad_stride (out_stride) values from row to row; a
  *   tensor without gaps is one row.  out may be grad itself, with the same strides; apart from that outputs must overlap neither each
  *   other nor gradients.  The array is read before the call returns.

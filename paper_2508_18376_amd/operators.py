@@ -431,8 +431,8 @@ def moe_int4_matmul(x, w, w_scale, w_zero=None, offsets=None, block=128, out=Non
     x [rows][k] bf16, f16 or f32; w uint8 [groups][n][(k + 1) // 2], the weight of an even k in a byte's low half, of an odd one in its high half;
     w_scale [groups][n][ceil(k / block)] of x's type or float32; w_zero uint8 of that shape, or None for 8 everywhere; block a power of two
     from 32 on; offsets int32 [groups + 1] on the GPU, or None for one group of all rows.  y has x's type.  Weights whose rows start on
-    16 bytes are faster.  Many outputs that are infinite or NaN make a call of few rows slow.  out as in
-    moe_grouped_matmul."""
+    16 bytes are faster.  Few rows are fast in 16-bit types only, and slow if many of their outputs are infinite or
+    NaN.  out as in moe_grouped_matmul."""
     f = "moe_int4_matmul"
     if x.dim() != 2 or w.dim() != 3:
         _refuse(f, "x must have 2 dimensions and w 3")
