@@ -1,8 +1,8 @@
 // Products with weights in 4 bits, for every type, alignment and number of rows: the tiles of 128 x 128 of grouped_plain.h, whose weights are widened on their way
 // from registers to LDS.  16-bit types: (q - z) s is rounded to x's type once, which is what the matrix instructions take; fp32 products are fp32.
 // Sums of fp32 go in parts (see Parts); as one chain 4096 rows of 4096 x 14336 took 4030 us, 17 of 14336 x 4096 1135 instead of 1195.
-// Bound by the matrix instructions in fp32 (4096 rows of 4096 x 14336 4134 us, 116 of 154 TFLOP/s; few rows are tiles of 128 all the same), by the way through registers in 16 bits: weights that start
-// off 16 bytes 1088 us, 442 TFLOP/s, where int4_tiles.hip takes 471.
+// Bound by the matrix instructions in fp32 (4096 rows of 4096 x 14336 4134 us, 116 of 153 TFLOP/s; few rows are tiles of 128 all the same, 342 us), by the way
+// through registers in 16 bits: weights that start off 16 bytes 1088 us, 442 TFLOP/s, where int4_tiles.hip takes 471.
 #include "grouped_plain.h"
 #include "int4_matmul.h"
 
